@@ -17,6 +17,14 @@
  *   cast_accept_stochastic  the same section's rule at T > 0, with residual resampling
  *   cast_compact_kv      accepted KV rows made contiguous
  *
+ * Two additions for caches that bound the step (not in the paper):
+ *   cast_store_kv_q4, cast_load_kv_q4, cast_tree_attention_q4, cast_compact_kv_q4
+ *                        a cache held in 4 bits: rows quantised into it and read back, the attention over it,
+ *                        its compaction
+ *   cast_attention_mass[_q4], cast_evict_kv[_q4]
+ *                        the attention weight that every cached position has drawn, and the eviction of the
+ *                        positions that drew least
+ *
  * Conventions
  *  - Plain C. Every tensor pointer is a DEVICE pointer owned by the caller
  *    unless its comment says "host". The library owns only what cast_create
@@ -368,6 +376,125 @@ CAST_API cast_status cast_accept_static(const void* target_logits, cast_dtype dt
                                         int max_depth, const int32_t* tokens, const int32_t* parent,
                                         const int32_t* n_tree, int32_t* accept_len, int32_t* accept_path,
                                         int32_t* bonus_token, void* stream);
+
+/*
+ * ---- The cache in 4 bits ----------------------------------------------------------------------
+ * A row (one position of one kv-head) is D codes of 4 bits and a pair (step, low); dimension d stands for
+ * low + step * code[d]. Layouts, for every q4 call:
+ *   k_codes, v_codes  [num_pages, Hkv, page_size, D/2] bytes; byte i of a row holds dimension 2i in its low and
+ *                     2i + 1 in its high half
+ *   k_range, v_range  [num_pages, Hkv, page_size, 2] bf16: step, low
+ *   page_size = 0: one run of seq_capacity positions per sequence, [B, Hkv, seq_capacity, ...]
+ *   page_table, seq_capacity, num_pages as for cast_tree_attention; page_size any positive number.
+ * (The kv-heads lie outside the positions of a page, unlike in the 16-bit cache: a 64-byte row between the rows of the
+ * other heads would be read in pieces.) The codes of layer l start code_stride_bytes * l after the base pointers, the
+ * pairs range_stride_bytes * l; calls that take one layer take the layer's pointers.
+ * Codes 16-byte aligned (code_stride_bytes a multiple of 16), pairs 4-byte aligned; D in {64, 128}.
+ *
+ * cast_store_kv_q4: rows t < n_rows[b] of k, v [n_layers, B, rows, Hkv, D] (dtype `dtype`) to positions
+ * start[b] + t (start NULL: 0). Per row, in fp32: lo, hi its least and largest value, low = bf16(lo),
+ * step = bf16((hi - lo) / 15), code = clamp(round-half-even((x - low) / step), 0, 15), or 0 where step is 0. A row with a
+ * value that is not finite, or whose hi - lo or low is not, stores step = low = NaN and codes 0: who attends to it gets NaN, as
+ * from a 16-bit cache.
+ * n_rows[b] is clamped to [0, rows]. Device error: BAD_PAGE (a position past the sequence's capacity, a negative start,
+ * or a page id out of range: that row is not stored).
+ */
+CAST_API cast_status cast_store_kv_q4(cast_ctx* ctx, const void* k, const void* v, cast_dtype dtype, int B, int n_layers,
+                                      int rows, int Hkv, int D, int page_size, const int32_t* page_table,
+                                      int seq_capacity, int num_pages, const int32_t* start, const int32_t* n_rows,
+                                      void* k_codes, void* k_range, void* v_codes, void* v_range,
+                                      size_t code_stride_bytes, size_t range_stride_bytes, void* stream);
+
+/*
+ * The other way: rows t < n_rows[b] of k, v [n_layers, B, rows, Hkv, D] become the values low + step * code (fp32, rounded
+ * once to `dtype`) of positions start[b] + t; rows t >= n_rows[b] are left untouched. Errors as for cast_store_kv_q4 (a row
+ * whose place is refused is left untouched).
+ */
+CAST_API cast_status cast_load_kv_q4(cast_ctx* ctx, const void* k_codes, const void* k_range, const void* v_codes,
+                                     const void* v_range, size_t code_stride_bytes, size_t range_stride_bytes,
+                                     cast_dtype dtype, int B, int n_layers, int rows, int Hkv, int D, int page_size,
+                                     const int32_t* page_table, int seq_capacity, int num_pages, const int32_t* start,
+                                     const int32_t* n_rows, void* k, void* v, void* stream);
+
+/* Set-up call, as cast_reserve_attention, for calls of cast_tree_attention_q4 with these arguments. */
+CAST_API cast_status cast_reserve_attention_q4(cast_ctx* ctx, cast_dtype dtype, int B, int Hq, int Hkv, int D,
+                                               int page_size, int seq_capacity);
+
+/*
+ * cast_tree_attention_rows over a 4-bit cache (first_row NULL: all rows). q, out [B, Ncap, Hq, D] of type `dtype`; the rows
+ * of the tree tokens are already stored at positions kv_len[b] + j. Sums and softmax in fp32; with bf16 queries the codes
+ * enter the matrix products as exact small integers, step and low are applied in fp32 outside them, and the weights
+ * (times the row's step) are rounded to bf16 once. A masked row of the cache reaches no output, NaN included; a query row
+ * that sees nothing gives zeros. Needs Hq % Hkv == 0 and a workspace reserved for this shape; never reads early (see
+ * cast_set_attention_early_reads). Device errors: BAD_TREE, BAD_PAGE (the position counts as masked).
+ */
+CAST_API cast_status cast_tree_attention_q4(cast_ctx* ctx, const void* q, const void* k_codes, const void* k_range,
+                                            const void* v_codes, const void* v_range, cast_dtype dtype, int B, int Hq,
+                                            int Hkv, int D, int page_size, const int32_t* page_table, int seq_capacity,
+                                            int num_pages, const int32_t* kv_len, const uint32_t* anc_mask,
+                                            const int32_t* n_tree, const int32_t* first_row, float scale, void* out,
+                                            void* stream);
+
+/* cast_compact_kv on a 4-bit cache: the same rows, conditions and errors. */
+CAST_API cast_status cast_compact_kv_q4(cast_ctx* ctx, void* k_codes, void* k_range, void* v_codes, void* v_range,
+                                        size_t code_stride_bytes, size_t range_stride_bytes, int B, int n_layers, int Hkv,
+                                        int D, int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                        const int32_t* accept_path, const int32_t* accept_len, int32_t* kv_len /* in/out */,
+                                        void* stream);
+
+/*
+ * ---- Eviction by accumulated attention weight ---------------------------------------------------
+ * cast_attention_mass adds, for every layer, sequence, kv-head and position p, the attention weight that the step's accepted
+ * rows gave the position:
+ *   mass[l, b, kvh, p] += sum over accepted rows i and heads h of the group of softmax_p(q[l, b, path_i, h] . k_p * scale).
+ * It is called behind the compaction, when the accepted rows stand at the end of the sequence: with n = accept_len[b] + 1, row
+ * i = 0..n-1 sees the positions p < kv_len[b] - n + i + 1.
+ *   q            [n_layers, B, Ncap, Hq, D], layer l at q_stride_bytes * l
+ *   k_cache      as for cast_tree_attention, layer l at layer_stride_bytes * l (q4: the codes and pairs of K alone)
+ *   accept_path  [B, H+1], the row of q of every accepted token, as cast_accept writes it; NULL: rows 0..accept_len[b]
+ *   accept_len   [B]; below 0: nothing is added for the sequence
+ *   kv_len       [B], after the compaction
+ *   mass         [n_layers, B, Hkv, P] fp32, in/out, P = the sequence's capacity in positions (seq_capacity times page_size,
+ *                or seq_capacity); positions that no row sees are left untouched
+ * Rows are added in a fixed order: the same inputs give the same bits. Needs a workspace (cast_reserve_attention_mass,
+ * max_rows >= H+1, or Ncap where accept_path is NULL). bf16 products on the tensor cores, sums in fp32.
+ * Device errors: BAD_TREE (more rows than the path or Ncap holds, a path entry outside [0, Ncap), kv_len[b] < n), BAD_PAGE
+ * (kv_len[b] past the capacity): nothing is added for the sequence; a page id out of range: its positions count as masked.
+ */
+CAST_API cast_status cast_reserve_attention_mass(cast_ctx* ctx, cast_dtype dtype, int B, int n_layers, int max_rows, int Hq,
+                                                 int Hkv, int D, int page_size, int seq_capacity);
+CAST_API cast_status cast_attention_mass(cast_ctx* ctx, const void* q, const void* k_cache, cast_dtype dtype, int B,
+                                         int n_layers, size_t q_stride_bytes, size_t layer_stride_bytes, int Hq, int Hkv,
+                                         int D, int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                         const int32_t* accept_path, const int32_t* accept_len, const int32_t* kv_len,
+                                         float scale, float* mass, void* stream);
+CAST_API cast_status cast_attention_mass_q4(cast_ctx* ctx, const void* q, const void* k_codes, const void* k_range,
+                                            cast_dtype dtype, int B, int n_layers, size_t q_stride_bytes,
+                                            size_t code_stride_bytes, size_t range_stride_bytes, int Hq, int Hkv, int D,
+                                            int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                            const int32_t* accept_path, const int32_t* accept_len, const int32_t* kv_len,
+                                            float scale, float* mass, void* stream);
+
+/*
+ * Cuts every sequence longer than `budget` positions to `budget`: per layer and kv-head the last `recent` positions stay, and
+ * of those before them the budget - recent with the largest mass (ties: the lower position; NaN counts as least). What stays
+ * keeps its order and moves to the front of the sequence, K, V and mass; mass behind it is zeroed up to the old length;
+ * kv_len[b] = min(kv_len[b], budget). Sequences of at most `budget` positions are left alone.
+ *   kept   [n_layers, B, Hkv, budget] int32 out: the old positions of the rows, ascending, -1 beyond them
+ *   mass   as for cast_attention_mass, in/out
+ * The cache rows behind the new length keep what they hold. Positions of a sequence must not share a page slot.
+ * Errors: INVALID_ARG (budget < 1, recent outside [0, budget]); device: BAD_PAGE (a page id of the sequence out of range, or
+ * kv_len[b] outside [0, capacity]: the sequence is left alone, its kept is -1).
+ */
+CAST_API cast_status cast_evict_kv(cast_ctx* ctx, void* k_cache, void* v_cache, cast_dtype dtype, int B, int n_layers,
+                                   size_t layer_stride_bytes, int Hkv, int D, int page_size, const int32_t* page_table,
+                                   int seq_capacity, int num_pages, int budget, int recent, float* mass, int32_t* kept,
+                                   int32_t* kv_len /* in/out */, void* stream);
+CAST_API cast_status cast_evict_kv_q4(cast_ctx* ctx, void* k_codes, void* k_range, void* v_codes, void* v_range,
+                                      size_t code_stride_bytes, size_t range_stride_bytes, int B, int n_layers, int Hkv,
+                                      int D, int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                      int budget, int recent, float* mass, int32_t* kept, int32_t* kv_len /* in/out */,
+                                      void* stream);
 
 /* Synchronises `stream`, returns the device status word and clears it.
  * detail: an index that identifies the offending row/entry (meaning per status). */

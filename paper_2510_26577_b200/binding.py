@@ -34,7 +34,9 @@ EXPORTS = [
     "cast_state_import", "cast_step_begin", "cast_tree_expand", "cast_select_nodes", "cast_tree_attention",
     "cast_accept", "cast_compact_kv", "cast_poll_status", "cast_step_info", "cast_accept_static",
     "cast_accept_stochastic", "cast_accept_stochastic_plan", "cast_tree_attention_rows", "cast_reserve_attention",
-    "cast_set_attention_early_reads",
+    "cast_set_attention_early_reads", "cast_store_kv_q4", "cast_load_kv_q4", "cast_reserve_attention_q4",
+    "cast_tree_attention_q4", "cast_compact_kv_q4", "cast_reserve_attention_mass", "cast_attention_mass",
+    "cast_attention_mass_q4", "cast_evict_kv", "cast_evict_kv_q4",
 ]
 
 
@@ -83,6 +85,8 @@ def load_library() -> C.CDLL:
         "cast_state_import": [vp, vp, C.c_size_t],
         "cast_reserve_attention": [vp, i32, i32, i32, i32, i32, i32, i32],
         "cast_set_attention_early_reads": [vp, i32],
+        "cast_reserve_attention_q4": [vp, i32, i32, i32, i32, i32, i32, i32],
+        "cast_reserve_attention_mass": [vp, i32, i32, i32, i32, i32, i32, i32, i32, i32],
         "cast_accept_stochastic_plan": [vp, i32, C.POINTER(C.c_int), C.POINTER(C.c_int)],
         "cast_poll_status": [vp, vp, C.POINTER(C.c_int), C.POINTER(C.c_int32)],
         "cast_step_info": [vp, vp, C.POINTER(C.c_int32)],
@@ -168,6 +172,18 @@ class CastContext:
         _check(self.lib.cast_reserve_attention(self.handle, code, B, Hq, Hkv, D, page_size, seq_capacity),
                "cast_reserve_attention")
 
+    def cast_reserve_attention_q4(self, dtype, B, Hq, Hkv, D, page_size, seq_capacity):
+        """The same for cast_tree_attention_q4."""
+        code = CAST_F32 if dtype == torch.float32 else CAST_BF16
+        _check(self.lib.cast_reserve_attention_q4(self.handle, code, B, Hq, Hkv, D, page_size, seq_capacity),
+               "cast_reserve_attention_q4")
+
+    def cast_reserve_attention_mass(self, dtype, B, n_layers, max_rows, Hq, Hkv, D, page_size, seq_capacity):
+        """The same for cast_attention_mass and cast_attention_mass_q4."""
+        code = CAST_F32 if dtype == torch.float32 else CAST_BF16
+        _check(self.lib.cast_reserve_attention_mass(self.handle, code, B, n_layers, max_rows, Hq, Hkv, D, page_size,
+                                                    seq_capacity), "cast_reserve_attention_mass")
+
     def cast_set_attention_early_reads(self, promise: bool):
         """The caller's promise that only q and the tree tokens' cache rows come from the operation right before an
         attention call (see include/cast.h)."""
@@ -213,6 +229,56 @@ class CastContext:
                         seq_capacity, num_pages, accept_path, accept_len, kv_len, stream=None):
         _check(_calls.compact_kv(self._ctx, k_cache, v_cache, B, n_layers, layer_stride_bytes, Hkv, D, page_size, page_table,
                                  seq_capacity, num_pages, accept_path, accept_len, kv_len, stream), "cast_compact_kv")
+
+    # --- the cache in 4 bits --------------------------------------------------
+    def cast_store_kv_q4(self, k, v, B, n_layers, rows, Hkv, D, page_size, page_table, seq_capacity, num_pages, start, n_rows,
+                         k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, stream=None):
+        _check(_calls.store_kv_q4(self._ctx, k, v, B, n_layers, rows, Hkv, D, page_size, page_table, seq_capacity, num_pages,
+                                  start, n_rows, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes,
+                                  stream), "cast_store_kv_q4")
+
+    def cast_load_kv_q4(self, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B, n_layers, rows, Hkv,
+                        D, page_size, page_table, seq_capacity, num_pages, start, n_rows, k, v, stream=None):
+        _check(_calls.load_kv_q4(self._ctx, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B,
+                                 n_layers, rows, Hkv, D, page_size, page_table, seq_capacity, num_pages, start, n_rows, k, v,
+                                 stream), "cast_load_kv_q4")
+
+    def cast_tree_attention_q4(self, q, k_codes, k_range, v_codes, v_range, B, Hq, Hkv, D, page_size, page_table, seq_capacity,
+                               num_pages, kv_len, anc_mask, n_tree, first_row, scale, out, stream=None):
+        _check(_calls.tree_attention_q4(self._ctx, q, k_codes, k_range, v_codes, v_range, B, Hq, Hkv, D, page_size, page_table,
+                                        seq_capacity, num_pages, kv_len, anc_mask, n_tree, first_row, scale, out, stream),
+               "cast_tree_attention_q4")
+
+    def cast_compact_kv_q4(self, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B, n_layers, Hkv, D,
+                           page_size, page_table, seq_capacity, num_pages, accept_path, accept_len, kv_len, stream=None):
+        _check(_calls.compact_kv_q4(self._ctx, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B,
+                                    n_layers, Hkv, D, page_size, page_table, seq_capacity, num_pages, accept_path, accept_len,
+                                    kv_len, stream), "cast_compact_kv_q4")
+
+    # --- eviction by accumulated attention weight -----------------------------
+    def cast_attention_mass(self, q, k_cache, B, n_layers, q_stride_bytes, layer_stride_bytes, Hq, Hkv, D, page_size, page_table,
+                            seq_capacity, num_pages, accept_path, accept_len, kv_len, scale, mass, stream=None):
+        _check(_calls.attention_mass(self._ctx, q, k_cache, B, n_layers, q_stride_bytes, layer_stride_bytes, Hq, Hkv, D,
+                                     page_size, page_table, seq_capacity, num_pages, accept_path, accept_len, kv_len, scale,
+                                     mass, stream), "cast_attention_mass")
+
+    def cast_attention_mass_q4(self, q, k_codes, k_range, B, n_layers, q_stride_bytes, code_stride_bytes, range_stride_bytes, Hq,
+                               Hkv, D, page_size, page_table, seq_capacity, num_pages, accept_path, accept_len, kv_len, scale,
+                               mass, stream=None):
+        _check(_calls.attention_mass_q4(self._ctx, q, k_codes, k_range, B, n_layers, q_stride_bytes, code_stride_bytes,
+                                        range_stride_bytes, Hq, Hkv, D, page_size, page_table, seq_capacity, num_pages,
+                                        accept_path, accept_len, kv_len, scale, mass, stream), "cast_attention_mass_q4")
+
+    def cast_evict_kv(self, k_cache, v_cache, B, n_layers, layer_stride_bytes, Hkv, D, page_size, page_table, seq_capacity,
+                      num_pages, budget, recent, mass, kept, kv_len, stream=None):
+        _check(_calls.evict_kv(self._ctx, k_cache, v_cache, B, n_layers, layer_stride_bytes, Hkv, D, page_size, page_table,
+                               seq_capacity, num_pages, budget, recent, mass, kept, kv_len, stream), "cast_evict_kv")
+
+    def cast_evict_kv_q4(self, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B, n_layers, Hkv, D,
+                         page_size, page_table, seq_capacity, num_pages, budget, recent, mass, kept, kv_len, stream=None):
+        _check(_calls.evict_kv_q4(self._ctx, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B,
+                                  n_layers, Hkv, D, page_size, page_table, seq_capacity, num_pages, budget, recent, mass, kept,
+                                  kv_len, stream), "cast_evict_kv_q4")
 
     def cast_accept_stochastic_plan(self, dtype):
         """(cluster size, slices cached in shared memory?) for logits of torch dtype `dtype`."""

@@ -82,6 +82,20 @@ struct Args {
     }
     return static_cast<T*>(t.data_ptr());
   }
+  // the same for an argument of one type
+  void* tensor_of(at::ScalarType type) {
+    PyObject* o = ok && at < n ? a[at] : nullptr;
+    if (o != nullptr && THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() != type) {
+      PyErr_Format(PyExc_TypeError, "%s tensor expected", c10::toString(type));
+      ok = false;
+      return nullptr;
+    }
+    return tensor();
+  }
+  // codes and pairs of a 4-bit cache
+  void* codes() { return tensor_of(at::kByte); }
+  void* range() { return tensor_of(at::kBFloat16); }
+  int32_t* ints() { return static_cast<int32_t*>(tensor_of(at::kInt)); }
   // the last argument: a torch stream, or None for the current one
   void* stream() {
     PyObject* o = next();
@@ -249,6 +263,160 @@ PyObject* compact_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   CALL(cast_compact_kv(c, k, v, dt, B, layers, stride, Hkv, D, page, table, cap, pages, path, len, kv_len, s));
 }
 
+// Values `k` and `v` of a store or a load, of one type.
+void both(Args& g, cast_dtype* dtype, void** k, void** v) {
+  cast_dtype other = CAST_F32;
+  *k = g.tensor(dtype);
+  *v = g.tensor(&other);
+  if (g.ok && other != *dtype) g.known_dtype = false;
+}
+
+PyObject* store_kv_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32;
+  cast_ctx* c = g.context();
+  void *k, *v;
+  both(g, &dt, &k, &v);
+  const int B = g.integer(), layers = g.integer(), rows = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* start = g.ints();
+  auto* n_rows = g.ints();
+  auto* kc = g.codes();
+  auto* kr = g.range();
+  auto* vc = g.codes();
+  auto* vr = g.range();
+  const size_t cs = g.size(), rs = g.size();
+  void* s = g.stream();
+  CALL(cast_store_kv_q4(c, k, v, dt, B, layers, rows, Hkv, D, page, table, cap, pages, start, n_rows, kc, kr, vc, vr, cs, rs, s));
+}
+
+PyObject* load_kv_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32;
+  cast_ctx* c = g.context();
+  auto* kc = g.codes();
+  auto* kr = g.range();
+  auto* vc = g.codes();
+  auto* vr = g.range();
+  const size_t cs = g.size(), rs = g.size();
+  const int B = g.integer(), layers = g.integer(), rows = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* start = g.ints();
+  auto* n_rows = g.ints();
+  void *k, *v;
+  both(g, &dt, &k, &v);
+  void* s = g.stream();
+  CALL(cast_load_kv_q4(c, kc, kr, vc, vr, cs, rs, dt, B, layers, rows, Hkv, D, page, table, cap, pages, start, n_rows, k, v, s));
+}
+
+PyObject* tree_attention_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32, dt_out = CAST_F32;
+  cast_ctx* c = g.context();
+  auto* q = g.tensor(&dt);
+  auto* kc = g.codes();
+  auto* kr = g.range();
+  auto* vc = g.codes();
+  auto* vr = g.range();
+  const int B = g.integer(), Hq = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* kv_len = g.ints();
+  auto* anc = g.tensor<uint32_t>();
+  auto* n_tree = g.ints();
+  auto* first = g.ints();
+  const float scale = (float)g.real();
+  auto* out = g.tensor(&dt_out);
+  if (g.ok && dt_out != dt) g.known_dtype = false;
+  void* s = g.stream();
+  CALL(cast_tree_attention_q4(c, q, kc, kr, vc, vr, dt, B, Hq, Hkv, D, page, table, cap, pages, kv_len, anc, n_tree, first, scale,
+                              out, s));
+}
+
+PyObject* compact_kv_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_ctx* c = g.context();
+  auto* kc = g.codes();
+  auto* kr = g.range();
+  auto* vc = g.codes();
+  auto* vr = g.range();
+  const size_t cs = g.size(), rs = g.size();
+  const int B = g.integer(), layers = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* path = g.ints();
+  auto* len = g.ints();
+  auto* kv_len = g.ints();
+  void* s = g.stream();
+  CALL(cast_compact_kv_q4(c, kc, kr, vc, vr, cs, rs, B, layers, Hkv, D, page, table, cap, pages, path, len, kv_len, s));
+}
+
+// cast_attention_mass and, with kQ4, cast_attention_mass_q4
+template <bool kQ4>
+PyObject* attention_mass(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32, dt_k = CAST_F32;
+  cast_ctx* c = g.context();
+  auto* q = g.tensor(&dt);
+  void* k = kQ4 ? g.codes() : g.tensor(&dt_k);
+  void* range = kQ4 ? g.range() : nullptr;
+  if (!kQ4 && g.ok && dt_k != dt) g.known_dtype = false;
+  const int B = g.integer(), layers = g.integer();
+  const size_t qs = g.size(), ks = g.size(), rs = kQ4 ? g.size() : 0;
+  const int Hq = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* path = g.ints();
+  auto* len = g.ints();
+  auto* kv_len = g.ints();
+  const float scale = (float)g.real();
+  auto* mass = static_cast<float*>(g.tensor_of(at::kFloat));
+  void* s = g.stream();
+  CALL(kQ4 ? cast_attention_mass_q4(c, q, k, range, dt, B, layers, qs, ks, rs, Hq, Hkv, D, page, table, cap, pages, path, len,
+                                    kv_len, scale, mass, s)
+           : cast_attention_mass(c, q, k, dt, B, layers, qs, ks, Hq, Hkv, D, page, table, cap, pages, path, len, kv_len, scale,
+                                 mass, s));
+}
+
+PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32;
+  cast_ctx* c = g.context();
+  void *k, *v;
+  both(g, &dt, &k, &v);
+  const int B = g.integer(), layers = g.integer();
+  const size_t stride = g.size();
+  const int Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer(), budget = g.integer(), recent = g.integer();
+  auto* mass = static_cast<float*>(g.tensor_of(at::kFloat));
+  auto* kept = g.ints();
+  auto* kv_len = g.ints();
+  void* s = g.stream();
+  CALL(cast_evict_kv(c, k, v, dt, B, layers, stride, Hkv, D, page, table, cap, pages, budget, recent, mass, kept, kv_len, s));
+}
+
+PyObject* evict_kv_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_ctx* c = g.context();
+  auto* kc = g.codes();
+  auto* kr = g.range();
+  auto* vc = g.codes();
+  auto* vr = g.range();
+  const size_t cs = g.size(), rs = g.size();
+  const int B = g.integer(), layers = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer(), budget = g.integer(), recent = g.integer();
+  auto* mass = static_cast<float*>(g.tensor_of(at::kFloat));
+  auto* kept = g.ints();
+  auto* kv_len = g.ints();
+  void* s = g.stream();
+  CALL(cast_evict_kv_q4(c, kc, kr, vc, vr, cs, rs, B, layers, Hkv, D, page, table, cap, pages, budget, recent, mass, kept, kv_len,
+                        s));
+}
+
 #define METHOD(name, fn) {name, (PyCFunction)(void (*)())(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     METHOD("step_begin", step_begin),
@@ -260,6 +428,14 @@ PyMethodDef methods[] = {
     METHOD("accept_stochastic", accept_stochastic),
     METHOD("accept_static", accept_static),
     METHOD("compact_kv", compact_kv),
+    METHOD("store_kv_q4", store_kv_q4),
+    METHOD("load_kv_q4", load_kv_q4),
+    METHOD("tree_attention_q4", tree_attention_q4),
+    METHOD("compact_kv_q4", compact_kv_q4),
+    METHOD("attention_mass", attention_mass<false>),
+    METHOD("attention_mass_q4", attention_mass<true>),
+    METHOD("evict_kv", evict_kv),
+    METHOD("evict_kv_q4", evict_kv_q4),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

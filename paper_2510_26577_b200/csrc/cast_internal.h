@@ -105,6 +105,12 @@ struct cast_ctx {
   size_t attn_tc_ws_bytes;
   int attn_attr_set[2][2];  // its kernels' attributes have been set on the context's device (heads of 128 dims, of 64)
 
+  // workspaces of the 4-bit cache's attention and of the attention mass (cast_reserve_attention_q4, _mass)
+  void* q4_ws;
+  size_t q4_ws_bytes;
+  void* mass_ws;
+  size_t mass_ws_bytes;
+
   // stochastic acceptance, per logits dtype (0 fp32, 1 bf16): cluster size found to be launchable
   // (0: not looked up yet), whether a CTA's vocabulary slice is cached on chip, and how many such clusters run at once
   int sto_cs[2];
@@ -135,6 +141,25 @@ namespace cast {
     cudaError_t _e = (expr);                    \
     if (_e != cudaSuccess) return CAST_ERR_CUDA; \
   } while (0)
+
+// The context's buffers and its status word lie on the device that was current when it was created.
+inline bool on_device(const cast_ctx* c) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
+// Grows a workspace (set-up time only: synchronises and allocates); its first `zeroed` bytes start at zero.
+inline cast_status grow_workspace(void** ws, size_t* have, size_t need, size_t zeroed) {
+  if (need <= *have) return CAST_OK;
+  CAST_CUDA_OK(cudaDeviceSynchronize());
+  if (*ws) cudaFree(*ws);
+  *ws = nullptr;
+  *have = 0;
+  CAST_CUDA_OK(cudaMalloc(ws, need));
+  if (zeroed) CAST_CUDA_OK(cudaMemset(*ws, 0, zeroed));
+  *have = need;
+  return CAST_OK;
+}
 
 inline cast_status launch_status() { return cudaGetLastError() == cudaSuccess ? CAST_OK : CAST_ERR_CUDA; }
 

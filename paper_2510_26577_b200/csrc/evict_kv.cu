@@ -1,0 +1,325 @@
+// cast_evict_kv, cast_evict_kv_q4: the positions with the least accumulated attention weight leave the cache.
+//
+// Two launches. evict_select_kernel, one CTA per (layer, sequence, kv-head), finds the (budget - recent)-th largest weight
+// of the positions before the recent ones by a radix selection over the order-preserving integers of the weights (11 + 11 + 10
+// bits: three histograms in shared memory), then writes the kept positions in ascending order and moves their weights to the
+// front in one pass of block-wide counting. evict_gather_kernel moves the rows: a CTA takes one (layer, sequence, kv-head), K or V,
+// and up to 128 bytes of the row, and walks the list in order, many rows in flight. A row never moves up, so all sources of a
+// group of rows lie at or behind the group's own destinations: its loads come before its stores, and nothing later is lost.
+// Bound by memory: the weights once, the moved rows once each way.
+#include "kv_q4.h"
+
+using namespace cast;
+
+namespace {
+
+constexpr int kSelThreads = 512;
+constexpr int kSelItems = 4;                       // positions per thread and round of the counting pass
+constexpr int kBins = 2048;
+constexpr int kMoveThreads = 256;
+
+struct EvictParams {
+  Paging g;
+  int B, n_layers, Hkv, budget, recent;
+  float* mass;   // [n_layers][B][Hkv][max_pos]
+  int32_t* kept; // [n_layers][B][Hkv][budget]
+  int32_t* kv_len;
+  int32_t* ticket;
+  DevState* st;
+};
+
+// Larger key, larger weight; NaN below everything.
+__device__ __forceinline__ uint32_t mass_key(float m) { return m != m ? 0u : ordered_bits(m); }
+
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictParams p) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t part_s[kSelThreads / 32];
+  __shared__ uint32_t found_s[2];
+  __shared__ uint2 count_s[2][kSelThreads / 32];
+  const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const long long max_pos = p.g.max_pos();
+  const size_t seg = ((size_t)layer * p.B + b) * p.Hkv + h;
+  float* const mass = p.mass + seg * (size_t)max_pos;
+  int32_t* const kept = p.kept + seg * (size_t)p.budget;
+  const int len = p.kv_len[b];
+  bool bad = len < 0 || len > max_pos;
+  if (!bad && p.g.page_size > 0) {
+    const int pages = (int)(((long long)len + p.g.page_size - 1) / p.g.page_size);
+    for (int e = tid; e < pages; e += kSelThreads) {
+      const int id = p.g.table[(size_t)b * p.g.seq_capacity + e];
+      bad = bad || id < 0 || id >= p.g.num_pages;
+    }
+  }
+  if (__syncthreads_or(bad ? 1 : 0)) {
+    if (tid == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
+    for (int j = tid; j < p.budget; j += kSelThreads) kept[j] = -1;
+    return;
+  }
+  if (len <= p.budget) {
+    for (int j = tid; j < p.budget; j += kSelThreads) kept[j] = j < len ? j : -1;
+    return;
+  }
+  const int cand = len - p.recent;           // positions that compete, more than `want`
+  const int want = p.budget - p.recent;
+  // the want-th largest key, and how many of the positions that hold it stay
+  uint32_t key = 0, ties = 0;
+  bool none = want == 0;
+  if (!none) {
+    uint32_t left = (uint32_t)want, mask = 0;
+    const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = shifts[pass], n = 1 << bits[pass];
+      for (int i = tid; i < n; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < cand; i += kSelThreads) {
+        const uint32_t k = mass_key(mass[i]);
+        if ((k & mask) == key) atomicAdd(&hist[(k >> shift) & (n - 1)], 1u);
+      }
+      __syncthreads();
+      // from the top: thread t sums the n / kSelThreads bins below those of thread t - 1
+      const int per = n / kSelThreads;
+      uint32_t mine = 0;
+      for (int i = 0; i < per; ++i) mine += hist[n - 1 - (tid * per + i)];
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      if (lane == 31) part_s[warp] = upto;
+      __syncthreads();
+      for (int w = 0; w < warp; ++w) upto += part_s[w];
+      if (upto >= left && upto - mine < left) {  // one thread: the counts add up to at least `left`
+        uint32_t above = upto - mine;
+        int i = 0;
+        while (above + hist[n - 1 - (tid * per + i)] < left) above += hist[n - 1 - (tid * per + i++)];
+        found_s[0] = (uint32_t)(n - 1 - (tid * per + i));
+        found_s[1] = left - above;
+      }
+      __syncthreads();
+      key |= found_s[0] << shift;
+      left = found_s[1];
+      mask |= (uint32_t)(n - 1) << shift;
+    }
+    ties = left;
+  }
+  // Kept positions in order. Counts so far: of keys above `key` (and of recent positions), and of keys equal to it.
+  uint32_t above0 = 0, equal0 = 0;
+  int round = 0;
+  for (int base = 0; base < len; base += kSelThreads * kSelItems, ++round) {
+    float m[kSelItems];
+    bool up[kSelItems], eq[kSelItems];
+    const int i0 = base + tid * kSelItems;
+    uint32_t n_up = 0, n_eq = 0;
+#pragma unroll
+    for (int e = 0; e < kSelItems; ++e) {
+      const int i = i0 + e;
+      m[e] = i < len ? mass[i] : 0.f;
+      const uint32_t k = mass_key(m[e]);
+      up[e] = i < len && (i >= cand || (!none && k > key));
+      eq[e] = i < cand && !none && k == key;
+      n_up += up[e];
+      n_eq += eq[e];
+    }
+    uint2 upto = make_uint2(n_up, n_eq);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto.x, o), y = __shfl_up_sync(0xffffffffu, upto.y, o);
+      if (lane >= o) {
+        upto.x += x;
+        upto.y += y;
+      }
+    }
+    if (lane == 31) count_s[round & 1][warp] = upto;
+    __syncthreads();  // (and: every weight of this round is in registers before any is overwritten)
+    uint2 before = make_uint2(above0, equal0), all = make_uint2(0u, 0u);
+#pragma unroll
+    for (int w = 0; w < kSelThreads / 32; ++w) {
+      const uint2 c = count_s[round & 1][w];
+      if (w < warp) {
+        before.x += c.x;
+        before.y += c.y;
+      }
+      all.x += c.x;
+      all.y += c.y;
+    }
+    uint32_t nu = before.x + upto.x - n_up, ne = before.y + upto.y - n_eq;
+#pragma unroll
+    for (int e = 0; e < kSelItems; ++e) {
+      const uint32_t at = nu + min(ne, ties);
+      if (up[e] || (eq[e] && ne < ties)) {
+        kept[at] = i0 + e;
+        mass[at] = m[e];
+      }
+      nu += up[e];
+      ne += eq[e];
+    }
+    above0 += all.x;
+    equal0 += all.y;
+  }
+  __syncthreads();
+  for (int i = p.budget + tid; i < len; i += kSelThreads) mass[i] = 0.f;
+}
+
+struct MoveParams {
+  EvictParams e;
+  unsigned char* base[4];   // 16-bit caches: K, V; 4-bit: K codes, V codes, K pairs, V pairs
+  size_t stride[4];         // bytes per layer
+  int row_bytes[4];
+  int q4;
+};
+
+// Bytes [col, col + VPR * sizeof(V)) of the rows of one (layer, sequence, kv-head) of one buffer.
+template <typename V, int VPR, int U>
+__device__ __forceinline__ void move_rows(const MoveParams& p, int which, int layer, int b, int h, int col) {
+  constexpr int RPS = kMoveThreads / VPR;  // rows per step
+  const EvictParams& e = p.e;
+  const int tid = threadIdx.x, sub = tid % VPR, r = tid / VPR;
+  const size_t seg = ((size_t)layer * e.B + b) * e.Hkv + h;
+  const int32_t* const kept = e.kept + seg * (size_t)e.budget;
+  unsigned char* const base = p.base[which] + p.stride[which] * layer + col + sub * sizeof(V);
+  const size_t row_bytes = p.row_bytes[which];
+  const int slots = e.g.page_size;
+  auto place = [&](int pos) {
+    int page, slot;
+    find_place(e.g, b, pos, page, slot);  // (the selection has checked the ids)
+    if (p.q4) return (size_t)q4_row(e.g, e.Hkv, h, page, slot) * row_bytes;
+    return (((size_t)page * (slots == 0 ? e.g.seq_capacity : slots) + slot) * e.Hkv + h) * row_bytes;
+  };
+  // the rows in front of the first that moves lie where they belong (kept[j] - j never falls)
+  int lo = 0, hi = e.budget;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldcg(kept + mid) > mid) hi = mid; else lo = mid + 1;
+  }
+  V cur[U], nxt[U];
+  auto load = [&](int j0, V (&v)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * RPS + r;
+      if (j < e.budget) v[u] = __ldcg(reinterpret_cast<const V*>(base + place(__ldcg(kept + j))));
+    }
+  };
+  int j0 = lo;
+  if (j0 < e.budget) load(j0, cur);
+  while (j0 < e.budget) {
+    const int j1 = j0 + U * RPS;
+    if (j1 < e.budget) load(j1, nxt);
+    __syncthreads();  // the sources of [j0, j1) have been read by all
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * RPS + r;
+      if (j < e.budget) __stcg(reinterpret_cast<V*>(base + place(j)), cur[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) cur[u] = nxt[u];
+    j0 = j1;
+  }
+}
+
+// blockIdx.x: kv-head and piece (buffer, 128 bytes of the row) of a (sequence, layer)
+template <int RB, bool kQ4>  // bytes of a 16-bit cache's row, or of a 4-bit row's codes
+__global__ void __launch_bounds__(kMoveThreads) evict_gather_kernel(const MoveParams p) {
+  constexpr int kCols = RB > 128 ? RB / 128 : 1, kPieces = (kQ4 ? 4 : 2 * kCols);
+  const int piece = blockIdx.x % kPieces, h = blockIdx.x / kPieces, b = blockIdx.y, layer = blockIdx.z;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const EvictParams& e = p.e;
+  const int len = e.kv_len[b];
+  const size_t seg = ((size_t)layer * e.B + b) * e.Hkv + h;
+  const bool cut = len > e.budget && e.kept[seg * (size_t)e.budget] >= 0;
+  __syncthreads();  // the whole CTA has read the length
+  if (threadIdx.x == 0) {
+    // the last CTA of the sequence to have read its length publishes the new one
+    const int t = atomicAdd(&e.ticket[b], 1);
+    if (t == (int)(gridDim.x * gridDim.z) - 1) {
+      e.ticket[b] = 0;
+      if (cut) e.kv_len[b] = e.budget;
+    }
+  }
+  if (!cut) return;
+  if constexpr (kQ4) {
+    if (piece < 2) move_rows<uint4, RB / 16, 4>(p, piece, layer, b, h, 0);
+    else move_rows<uint32_t, 1, 4>(p, piece, layer, b, h, 0);
+  } else {
+    move_rows<uint4, 8, 4>(p, piece / kCols, layer, b, h, piece % kCols * 128);
+  }
+}
+
+cast_status launch_evict(cast_ctx* c, MoveParams& p, int n_layers, int B, int Hkv, int D, int pieces, void* kern, cudaStream_t s) {
+  if (n_layers > 65535 || (long long)Hkv * pieces > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  c->tree_inputs_fresh = 1;  // kv_len and cache rows: an attention call that follows reads them after its dependency wait
+  p.e.ticket = c->compact_ticket;
+  p.e.st = c->state;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(Hkv, B, n_layers);
+  cfg.blockDim = dim3(kSelThreads, 1, 1);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // launched while its predecessor drains; waits for it
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p.e);
+  if (e == cudaSuccess) {
+    cfg.gridDim = dim3(Hkv * pieces, B, n_layers);
+    cfg.blockDim = dim3(kMoveThreads, 1, 1);
+    void* args[] = {&p};
+    e = cudaLaunchKernelExC(&cfg, kern, args);
+  }
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return CAST_ERR_CUDA;
+  }
+  return CAST_OK;
+}
+
+}  // namespace
+
+extern "C" cast_status cast_evict_kv(cast_ctx* c, void* k_cache, void* v_cache, cast_dtype dtype, int B, int n_layers,
+                                     size_t layer_stride_bytes, int Hkv, int D, int page_size, const int32_t* page_table,
+                                     int seq_capacity, int num_pages, int budget, int recent, float* mass, int32_t* kept,
+                                     int32_t* kv_len, void* stream) {
+  const Paging g = {page_table, page_size, seq_capacity, num_pages};
+  if (!c || !k_cache || !v_cache || !mass || !kept || !kv_len || B < 1 || n_layers < 1 || Hkv < 1 || page_size < 0 ||
+      seq_capacity < 1 || (page_size > 0 && (!page_table || num_pages < 1)) || budget < 1 || recent < 0 || recent > budget ||
+      !on_device(c))
+    return CAST_ERR_INVALID_ARG;
+  if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
+  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  if (D != 64 && D != 128) return CAST_ERR_SHAPE;
+  if (((uintptr_t)k_cache | (uintptr_t)v_cache | layer_stride_bytes) & 15) return CAST_ERR_SHAPE;
+  const int rb = D * (dtype == CAST_F32 ? 4 : 2);
+  MoveParams p = {};
+  p.e.g = g; p.e.B = B; p.e.n_layers = n_layers; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
+  p.e.mass = mass; p.e.kept = kept; p.e.kv_len = kv_len;
+  p.base[0] = (unsigned char*)k_cache; p.base[1] = (unsigned char*)v_cache;
+  p.stride[0] = p.stride[1] = layer_stride_bytes;
+  p.row_bytes[0] = p.row_bytes[1] = rb;
+  void* kern = rb == 128 ? (void*)evict_gather_kernel<128, false> : rb == 256 ? (void*)evict_gather_kernel<256, false>
+                                                                              : (void*)evict_gather_kernel<512, false>;
+  return launch_evict(c, p, n_layers, B, Hkv, D, 2 * (rb / 128), kern, (cudaStream_t)stream);
+}
+
+extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_range, void* v_codes, void* v_range,
+                                        size_t code_stride_bytes, size_t range_stride_bytes, int B, int n_layers, int Hkv, int D,
+                                        int page_size, const int32_t* page_table, int seq_capacity, int num_pages, int budget,
+                                        int recent, float* mass, int32_t* kept, int32_t* kv_len, void* stream) {
+  const Paging g = {page_table, page_size, seq_capacity, num_pages};
+  if (!mass || !kept || !kv_len || n_layers < 1 || budget < 1 || recent < 0 || recent > budget) return CAST_ERR_INVALID_ARG;
+  const cast_status st = check_q4(c, B, Hkv, D, g, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes);
+  if (st != CAST_OK) return st;
+  MoveParams p = {};
+  p.e.g = g; p.e.B = B; p.e.n_layers = n_layers; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
+  p.e.mass = mass; p.e.kept = kept; p.e.kv_len = kv_len;
+  p.base[0] = (unsigned char*)k_codes; p.base[1] = (unsigned char*)v_codes;
+  p.base[2] = (unsigned char*)k_range; p.base[3] = (unsigned char*)v_range;
+  p.stride[0] = p.stride[1] = code_stride_bytes;
+  p.stride[2] = p.stride[3] = range_stride_bytes;
+  p.row_bytes[0] = p.row_bytes[1] = D / 2;
+  p.row_bytes[2] = p.row_bytes[3] = 4;
+  p.q4 = 1;
+  void* kern = D == 64 ? (void*)evict_gather_kernel<32, true> : (void*)evict_gather_kernel<64, true>;
+  return launch_evict(c, p, n_layers, B, Hkv, D, 4, kern, (cudaStream_t)stream);
+}

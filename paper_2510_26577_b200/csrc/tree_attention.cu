@@ -11,9 +11,10 @@
 // Bound by instruction issue, shared-memory reads of the products first: both go by 16-byte vectors, the first product by
 // packed multiply-adds (60 tokens, 4 sequences of 2048, 32/8 heads of 64: 233 us, 276 without the packing; 128 dims 450 and
 // 511). A 64-row tile of 8 x 4 per thread is as fast from 200 rows per kv-head on and up to twice as slow below.
+// The same kernel serves 4-bit caches with fp32 queries: their rows become fp32 on the way to shared memory.
 #include <math.h>
 
-#include "cast_internal.h"
+#include "kv_q4.h"
 
 using namespace cast;
 
@@ -54,9 +55,17 @@ struct AttnParams {
   float* part_o;    // [B][Hkv][nrowblk][nsplit][kRB][D]
   float* part_ml;   // [B][Hkv][nrowblk][nsplit][kRB][2]
   DevState* st;
+  const uint32_t* k_range;  // 4-bit caches: the rows' pairs; k and v are their codes
+  const uint32_t* v_range;
 };
 
 template <typename T> __device__ __forceinline__ void load_chunk(const T* p, float* out);
+// Sixteen codes of a 4-bit row as fp32 values.
+__device__ __forceinline__ void load_codes(const unsigned char* p, float step, float low, float* out) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) out[e] = fmaf(step, (float)(((e < 8 ? w.x : w.y) >> (4 * (e % 8))) & 15u), low);
+}
 template <> __device__ __forceinline__ void load_chunk<float>(const float* p, float* out) {
   const float4 a = *reinterpret_cast<const float4*>(p);
   out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w;
@@ -171,7 +180,7 @@ __device__ __forceinline__ void merge_splits(const AttnParams& p, int b, int kvh
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kQ4 = false>
 __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams p) {
   constexpr int KS = D + 4;          // padded row stride of Qs / Ks (floats)
   constexpr int SS = kPT + 4;        // row stride of Ss: rows 16-byte aligned
@@ -186,6 +195,7 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
   __shared__ float row_m[kRB], row_l[kRB], row_alpha[kRB];
   __shared__ uint32_t anc_s[kRB][CAST_MAX_TREE / 32];
   __shared__ long long slot_s[2][kPT];
+  __shared__ uint64_t nan_s;  // 4-bit caches: the tile's rows without a value
   __shared__ int s_last;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -221,7 +231,12 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
     const int pos = tile * kPT + tid;
     long long slot = -1;
     if (tile < t1 && pos < total) {
-      if (p.page_size == 0) {
+      if constexpr (kQ4) {
+        const Paging g = {p.page_table, p.page_size, p.seq_capacity, p.num_pages};
+        int page, in_page;
+        if (find_place(g, b, pos, page, in_page)) slot = q4_row(g, p.Hkv, kvh, page, in_page);
+        else report(p.st, CAST_ERR_BAD_PAGE, b);
+      } else if (p.page_size == 0) {
         slot = (long long)b * p.seq_capacity + pos;
       } else {
         const int page = p.page_table[(size_t)b * p.seq_capacity + pos / p.page_size];
@@ -267,8 +282,31 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
   for (int tile = t0; tile < t1; ++tile) {
     const int pbase = tile * kPT;
     __syncthreads();  // previous tile fully consumed; the slots (and Qs, anc_s on the first pass) visible
+    if constexpr (kQ4) {
+      constexpr int TPR = D / 16;  // threads per row; a row without a value lies as zeros, and is remembered
+      if (tid == 0) nan_s = 0;
+      __syncthreads();
+#pragma unroll 2
+      for (int i = tid; i < kPT * TPR; i += kThreads) {
+        const int pl = i / TPR, ch = i % TPR;
+        const long long row = slot_s[tile & 1][pl];
+        float f[16] = {}, g[16] = {};
+        if (row >= 0) {
+          const uint32_t kr = p.k_range[row], vr = p.v_range[row];
+          load_codes(reinterpret_cast<const unsigned char*>(p.k) + row * (D / 2) + ch * 8, q4_step(kr), q4_low(kr), f);
+          if (q4_low(vr) == q4_low(vr))
+            load_codes(reinterpret_cast<const unsigned char*>(p.v) + row * (D / 2) + ch * 8, q4_step(vr), q4_low(vr), g);
+          else if (ch == 0) atomicOr(reinterpret_cast<unsigned long long*>(&nan_s), 1ull << pl);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          *reinterpret_cast<float4*>(Ks + pl * KS + ch * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+          *reinterpret_cast<float4*>(Vs + pl * D + ch * 16 + e) = make_float4(g[e], g[e + 1], g[e + 2], g[e + 3]);
+        }
+      }
+    }
 #pragma unroll 4
-    for (int i = tid; i < kPT * CPR; i += kThreads) {
+    for (int i = kQ4 ? kPT * CPR : tid; i < kPT * CPR; i += kThreads) {
       const int pl = i / CPR, ch = i % CPR;
       const long long slot = slot_s[tile & 1][pl];
       float fk[CH], fv[CH];
@@ -314,7 +352,7 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int pl = tx + 16 * j, pos = pbase + pl;
-          bool vis = row_ok && pos < total;
+          bool vis = row_ok && pos < total && (!kQ4 || slot_s[tile & 1][pl] >= 0);
           if (vis && pos >= L) {
             const int jt = pos - L;
             vis = (anc_s[r][jt >> 5] >> (jt & 31)) & 1u;
@@ -343,6 +381,11 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
       float sum = p0 + p1;
 #pragma unroll
       for (int of = 16; of > 0; of >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, of);
+      if constexpr (kQ4) {  // a row without a value reaches the rows that see it, and no other
+        const uint64_t nans = nan_s;
+        const bool hit = (s0 != -INFINITY && ((nans >> lane) & 1)) || (s1 != -INFINITY && ((nans >> (lane + 32)) & 1));
+        if (__any_sync(0xffffffffu, hit)) sum = alpha = __int_as_float(0x7fffffff);
+      }
       __syncwarp();
       Ss[r * SS + lane] = p0;
       Ss[r * SS + lane + 32] = p1;
@@ -478,10 +521,10 @@ CcPlan cc_plan(const cast_ctx* c, int per_sm, int B, int Hq, int Hkv, int D, int
   return pl;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kQ4 = false>
 cast_status launch_cc(cast_ctx* c, AttnParams& p, int per_sm, cudaStream_t s) {
   const CcPlan pl = cc_plan(c, per_sm, p.B, p.Hq, p.Hkv, D, p.page_size, p.seq_capacity);
-  // compute calls never allocate: the workspace comes from cast_reserve_attention
+  // compute calls never allocate: the workspace comes from cast_reserve_attention (or _q4: the same one)
   if (pl.bytes > c->attn_ws_bytes) return CAST_ERR_CAPACITY;
   p.nsplit = pl.nsplit;
   p.nrowblk = pl.nrowblk;
@@ -491,7 +534,7 @@ cast_status launch_cc(cast_ctx* c, AttnParams& p, int per_sm, cudaStream_t s) {
     p.part_ml = p.part_o + (size_t)p.B * p.Hkv * pl.nrowblk * pl.nsplit * kRB * D;
   }
   const size_t smem = (size_t)(kRB * (D + 4) + kPT * (D + 4) + kPT * D + kRB * (kPT + 4)) * sizeof(float);
-  auto kern = tree_attn_cc_kernel<T, D>;
+  auto kern = tree_attn_cc_kernel<T, D, kQ4>;
   CAST_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(pl.nsplit * pl.nrowblk, p.Hkv, p.B);
@@ -517,6 +560,41 @@ cast_status launch_cc(cast_ctx* c, AttnParams& p, int per_sm, cudaStream_t s) {
 }
 
 }  // namespace
+
+extern "C" cast_status cast_reserve_attention_q4(cast_ctx* c, cast_dtype dtype, int B, int Hq, int Hkv, int D, int page_size,
+                                                 int seq_capacity) {
+  if (!c || B < 1 || Hq < 1 || Hkv < 1 || page_size < 0 || seq_capacity < 1 || !on_device(c)) return CAST_ERR_INVALID_ARG;
+  if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
+  const Paging g = {nullptr, page_size, seq_capacity, 0};
+  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
+  // tickets start at zero; every merge leaves its ticket at zero again
+  return grow_workspace(&c->attn_ws, &c->attn_ws_bytes, cc_plan(c, kOwn, B, Hq, Hkv, D, page_size, seq_capacity).bytes, kCcTicketBytes);
+}
+
+extern "C" cast_status cast_tree_attention_q4(cast_ctx* c, const void* q, const void* k_codes, const void* k_range,
+                                              const void* v_codes, const void* v_range, cast_dtype dtype, int B, int Hq, int Hkv,
+                                              int D, int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                              const int32_t* kv_len, const uint32_t* anc_mask, const int32_t* n_tree,
+                                              const int32_t* first_row, float scale, void* out, void* stream) {
+  const Paging g = {page_table, page_size, seq_capacity, num_pages};
+  if (!q || !kv_len || !anc_mask || !n_tree || !out || Hq < 1) return CAST_ERR_INVALID_ARG;
+  if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
+  const cast_status st = check_q4(c, B, Hkv, D, g, k_codes, k_range, v_codes, v_range, 0, 0);
+  if (st != CAST_OK) return st;
+  if (Hq % Hkv != 0 || (((uintptr_t)q | (uintptr_t)out) & 15)) return CAST_ERR_SHAPE;
+  if (scale == 0.f) scale = 1.0f / sqrtf((float)D);
+  cudaStream_t s = (cudaStream_t)stream;
+  AttnParams p;
+  p.q = q; p.k = k_codes; p.v = v_codes; p.out = out;
+  p.B = B; p.Ncap = c->cfg.max_tree; p.Nmax = c->cfg.total_token; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
+  p.page_size = page_size; p.seq_capacity = seq_capacity; p.num_pages = num_pages; p.words = c->words;
+  p.page_table = page_table; p.kv_len = kv_len; p.n_tree = n_tree; p.first_row = first_row; p.anc = anc_mask;
+  p.scale = scale; p.ticket = nullptr; p.part_o = nullptr; p.part_ml = nullptr; p.st = c->state;
+  p.k_range = (const uint32_t*)k_range; p.v_range = (const uint32_t*)v_range;
+  if (dtype == CAST_F32) return D == 64 ? launch_cc<float, 64, true>(c, p, kOwn, s) : launch_cc<float, 128, true>(c, p, kOwn, s);
+  return D == 64 ? launch_cc<__nv_bfloat16, 64, true>(c, p, kOwn, s) : launch_cc<__nv_bfloat16, 128, true>(c, p, kOwn, s);
+}
 
 extern "C" cast_status cast_set_attention_early_reads(cast_ctx* c, int promise) {
   if (!c) return CAST_ERR_INVALID_ARG;
@@ -584,6 +662,7 @@ extern "C" cast_status cast_tree_attention_rows(cast_ctx* c, const void* q, cons
   p.page_size = page_size; p.seq_capacity = seq_capacity; p.num_pages = num_pages; p.words = c->words;
   p.page_table = page_table; p.kv_len = kv_len; p.n_tree = n_tree; p.first_row = first_row; p.anc = anc_mask;
   p.scale = scale; p.ticket = nullptr; p.part_o = nullptr; p.part_ml = nullptr; p.st = c->state;
+  p.k_range = p.v_range = nullptr;
   if (dtype == CAST_F32) return D == 64 ? launch_cc<float, 64>(c, p, kOwn, s) : launch_cc<float, 128>(c, p, kOwn, s);
   const int per_sm = tree_attention_tc_takes(c, B, Hq, Hkv, D, page_size, seq_capacity) ? kFallback : kOwn;
   return D == 64 ? launch_cc<__nv_bfloat16, 64>(c, p, per_sm, s) : launch_cc<__nv_bfloat16, 128>(c, p, per_sm, s);

@@ -1,0 +1,465 @@
+"""The cache held in 4 bits: rows in and out bit by bit, attention and compaction over it against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import q4_oracle as o4
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}  # half a step, relative to the value
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2510_26577_b200 import build
+    build.build()
+    from paper_2510_26577_b200 import binding as b
+    b.load_library()
+    return b
+
+
+def dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def context(binding, B, tokens=8, depth=6):
+    return binding.CastContext(max_batch=B, vocab=1000, top_k=4, max_depth=depth, total_token=tokens, max_tree=tokens)
+
+
+class Cache:
+    """A 4-bit cache of random rows, on the host (codes [layers, pages, Hkv, slots, D], pairs fp32) and on the device."""
+
+    def __init__(self, rng, paged, nl, Hkv, D):
+        pages, slots = paged.shape
+        self.paged, self.nl, self.Hkv, self.D = paged, nl, Hkv, D
+        self.code, self.pair = {}, {}
+        for w in "kv":
+            self.code[w] = rng.integers(0, 16, (nl, pages, Hkv, slots, D)).astype(np.uint8)
+            step = o4.bf16(rng.uniform(0.05, 0.4, (nl, pages, Hkv, slots, 1)).astype(np.float32))
+            self.pair[w] = np.concatenate([step, o4.bf16(-7.5 * step + rng.normal(0, 0.1, step.shape).astype(np.float32))], -1)
+        self.upload()
+
+    def upload(self):
+        self.kc, self.vc = (dev(o4.pack(self.code[w])) for w in "kv")
+        self.kr, self.vr = (dev(self.pair[w]).to(torch.bfloat16) for w in "kv")
+        self.strides = (self.kc[0].numel(), self.kr[0].numel() * 2)
+
+    def where(self):
+        p = self.paged
+        return (p.page, dev(p.table), p.cap, p.pages)
+
+    def bits(self):
+        return [t.view(torch.int16).cpu().numpy() if t.dtype == torch.bfloat16 else t.cpu().numpy()
+                for t in (self.kc, self.kr, self.vc, self.vr)]
+
+    def host_bits(self):
+        pairs = {w: (self.pair[w].view(np.uint32) >> 16).astype(np.uint16).view(np.int16) for w in "kv"}
+        return [o4.pack(self.code["k"]), pairs["k"], o4.pack(self.code["v"]), pairs["v"]]
+
+    def rows(self, which, layer, b, h, n):
+        """Values and |step (code - 8)| of the first n positions of a sequence."""
+        page, slot = self.paged.at(b, np.arange(n))
+        code, pair = self.code[which][layer][page, h, slot], self.pair[which][layer][page, h, slot]
+        return o4.values(code, pair), np.abs(pair[..., :1].astype(np.float64) * (code.astype(np.float64) - 8))
+
+
+# ------------------------------------------------------------------------------------------------ rows in and out
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,page,Hkv,rows", [(128, 16, 8, 61), (64, 24, 3, 17), (128, 0, 1, 5), (64, 1, 2, 130), (128, 7, 2, 1)])
+def test_store_and_load(binding, dtype, D, page, Hkv, rows):
+    rng = np.random.default_rng(D + page + rows)
+    B, nl = 4, 2
+    paged = o4.Paged(rng, B, rows + 40, page)
+    cache = Cache(rng, paged, nl, Hkv, D)
+    x = {w: dev(rng.normal(0, 2, (nl, B, rows, Hkv, D)).astype(np.float32)).to(DT[dtype]) for w in "kv"}
+    x["k"][0, 0, 0] = 3.0                     # a constant row: step 0
+    x["v"][1, 1, 0, 0, 3] = float("inf")      # rows without a value
+    x["v"][0, 1, 0, 0, 5] = float("nan")
+    x["k"][1, 0, 0, 0, :] = torch.arange(D, device="cuda").to(DT[dtype]) / 2  # quotients that lie halfway
+    x["k"][0, 1, 0, 0, :] *= 1e-39            # steps far below the normal numbers
+    x["v"][0, 0, 0, 0, :2] = torch.tensor([3.3e38, -3.3e38])  # a span out of range
+    start = np.array([0, 37, 5, 11], np.int32)
+    n_rows = np.array([rows, rows + 9, 0, rows // 2], np.int32)
+    for w in "kv":
+        code, pair = o4.quantise(x[w].float().cpu().numpy())
+        for b in range(B):
+            n = min(n_rows[b], rows)
+            pg, sl = paged.at(b, start[b] + np.arange(n))
+            cache.code[w][:, pg, :, sl] = code[:, b, :n].swapaxes(0, 1)
+            cache.pair[w][:, pg, :, sl] = pair[:, b, :n].swapaxes(0, 1)
+    ctx = context(binding, B)
+    ctx.cast_store_kv_q4(x["k"], x["v"], B, nl, rows, Hkv, D, *cache.where(), dev(start), dev(n_rows), cache.kc, cache.kr, cache.vc,
+                         cache.vr, *cache.strides)
+    back = {w: torch.full_like(x[w], -77.0) for w in "kv"}
+    ctx.cast_load_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, B, nl, rows, Hkv, D, *cache.where(), dev(start),
+                        dev(n_rows), back["k"], back["v"])
+    assert ctx.cast_poll_status()[0] == 0
+    for got, want in zip(cache.bits(), cache.host_bits()):  # everything else in the cache included
+        np.testing.assert_array_equal(got, want) if got.dtype != np.int16 else np.testing.assert_array_equal(
+            np.where((got & 0x7FFF) > 0x7F80, 0x7FC0, got), np.where((want & 0x7FFF) > 0x7F80, 0x7FC0, want))
+    for w in "kv":
+        for b in range(B):
+            n = min(n_rows[b], rows)
+            pg, sl = paged.at(b, start[b] + np.arange(n))
+            want = o4.values(cache.code[w][:, pg, :, sl], cache.pair[w][:, pg, :, sl]).swapaxes(0, 1)
+            want = torch.from_numpy(want.astype(np.float32)).to(DT[dtype])  # (4 + 8 bits plus 8: one rounding each)
+            np.testing.assert_allclose(back[w][:, b, :n].float().cpu().numpy(), want.float().numpy(), rtol=2 * HALF[dtype], atol=1e-44)
+            assert bool((back[w][:, b, n:] == -77.0).all())
+
+
+def test_store_without_start_and_twice(binding):
+    rng = np.random.default_rng(3)
+    paged = o4.Paged(rng, 2, 33, 8)
+    cache = Cache(rng, paged, 1, 2, 64)
+    ctx = context(binding, 2)
+    n = dev(np.array([33, 20], np.int32))
+    for seed in range(2):  # the second call's rows replace the first's
+        x = torch.randn((1, 2, 33, 2, 64), generator=torch.Generator("cuda").manual_seed(seed), device="cuda")
+        ctx.cast_store_kv_q4(x, x, 2, 1, 33, 2, 64, *cache.where(), None, n, cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides)
+    back = torch.zeros_like(x)
+    ctx.cast_load_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, 2, 1, 33, 2, 64, *cache.where(), None, n, back, back.clone())
+    code, pair = o4.quantise(x.cpu().numpy())
+    want = o4.values(code, pair)
+    np.testing.assert_allclose(back[0, 0].cpu().numpy(), want[0, 0], rtol=2.0 ** -23, atol=0)
+    np.testing.assert_allclose(back[0, 1, :20].cpu().numpy(), want[0, 1, :20], rtol=2.0 ** -23, atol=0)
+    assert bool((back[0, 1, 20:] == 0).all()) and ctx.cast_poll_status()[0] == 0
+
+
+def test_store_refuses_places_outside(binding):
+    rng = np.random.default_rng(4)
+    paged = o4.Paged(rng, 3, 32, 8)
+    paged.table[1, 2], paged.table[2, 0] = paged.pages, -1
+    cache = Cache(rng, paged, 1, 2, 64)
+    before = cache.bits()
+    x = torch.randn((1, 3, 16, 2, 64), device="cuda")
+    ctx = context(binding, 3)
+    # sequence 0 runs past its capacity, 1 into a page id beyond the pool, 2 into a negative one
+    ctx.cast_store_kv_q4(x, x, 3, 1, 16, 2, 64, *cache.where(), dev(np.array([24, 12, 2], np.int32)), dev(np.array([16, 8, 4], np.int32)),
+                         cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides)
+    assert ctx.cast_poll_status()[0] == 7
+    code, pair = o4.quantise(x.cpu().numpy())
+    for b, first, n in ((0, 24, 8), (1, 12, 4)):
+        pg, sl = paged.at(b, first + np.arange(n))
+        for w in "kv":
+            cache.code[w][:, pg, :, sl] = code[:, b, :n].swapaxes(0, 1)
+            cache.pair[w][:, pg, :, sl] = pair[:, b, :n].swapaxes(0, 1)
+    for got, want, old in zip(cache.bits(), cache.host_bits(), before):
+        np.testing.assert_array_equal(got, want)
+        assert not np.array_equal(got, old)
+    ctx.cast_load_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, 3, 1, 16, 2, 64, *cache.where(),
+                        dev(np.array([-1, 0, 0], np.int32)), dev(np.array([1, 0, 0], np.int32)), x, x.clone())
+    assert ctx.cast_poll_status()[0] == 7
+
+
+# ------------------------------------------------------------------------------------------------ attention
+def random_masks(rng, N, cap):
+    anc = np.zeros((cap, (cap + 31) // 32), np.uint32)
+    vis = np.zeros((cap, cap), bool)
+    for t in range(N):
+        if t:
+            vis[t] = vis[int(rng.integers(0, t))]
+        vis[t, t] = True
+        for j in np.flatnonzero(vis[t]):
+            anc[t, j >> 5] |= np.uint32(1 << (j & 31))
+    return anc, vis
+
+
+def run_attention(ctx, cache, q, kv_len, anc, n_tree, first=None, scale=0.0, layer=0):
+    B, Hq, D = q.shape[0], q.shape[2], q.shape[3]
+    out = torch.full_like(q, float("nan"))
+    p = cache.paged
+    ctx.cast_reserve_attention_q4(q.dtype, B, Hq, cache.Hkv, D, p.page, p.cap)
+    ctx.cast_tree_attention_q4(q, cache.kc[layer], cache.kr[layer], cache.vc[layer], cache.vr[layer], B, Hq, cache.Hkv, D,
+                               *cache.where(), dev(kv_len), dev(anc.view(np.int32)), dev(n_tree), dev(first), scale, out)
+    return out
+
+
+def check_attention(out, cache, q, kv_len, vis, n_tree, dtype, first=None, scale=0.0, layer=0):
+    """Within: half a step of the output; half a bf16 step of every weight (bf16 queries), which moves an output by
+    sum_p w_p step_p |code_p - 8| of that; and 32-bit sums: a score is off by at most D 2^-24 sum |q_d k_d| (scaled), twice that is
+    the weights' relative error, and weights that are off by e move an output by at most 2 e max |v|."""
+    got = out.double().cpu().numpy()
+    x = q.double().cpu().numpy()
+    B, T, Hq, D = x.shape
+    G = Hq // cache.Hkv
+    sc = scale or D ** -0.5
+    for b in range(B):
+        N, L = int(n_tree[b]), int(kv_len[b])
+        F = min(int(first[b]), N) if first is not None else 0
+        assert np.isnan(got[b, N:]).all() and np.isnan(got[b, :F]).all()  # left untouched
+        for h in range(cache.Hkv):
+            k, _ = cache.rows("k", layer, b, h, L + N)
+            v, spread = cache.rows("v", layer, b, h, L + N)
+            qh = x[b, F:N, h * G:(h + 1) * G]
+            want, per = o4.attend(qh, k, v, spread, L, vis[b][F:N, :N], sc)
+            if not want.size:
+                continue
+            have = got[b, F:N, h * G:(h + 1) * G]
+            np.testing.assert_array_equal(np.isnan(have), np.isnan(want))
+            fin = np.abs(np.where(np.isfinite(k), k, 0)).max() if k.size else 0.0
+            s_err = D * 2.0 ** -24 * np.abs(qh).sum(-1).max() * fin * abs(sc) + 2.0 ** -20
+            vmax = np.abs(np.where(np.isfinite(v), v, 0)).max() if v.size else 0.0
+            tol = HALF[dtype] * np.abs(want) + (HALF[dtype] * per if dtype == "bf16" else 0) + 4 * s_err * vmax
+            err = np.abs(have - want)
+            assert not (err > tol * 1.001 + 1e-30).any(), (b, h, np.nanmax(err - tol), np.nanmax(err))
+
+
+SHAPES = [  # dtype, Hq, Hkv, D, page, tokens, prefix lengths
+    ("bf16", 8, 2, 128, 16, 12, [70, 200, 0, 1]),
+    ("bf16", 4, 4, 64, 0, 7, [63, 64, 65, 127]),
+    ("bf16", 7, 1, 128, 24, 33, [300, 0, 129, 511]),
+    ("bf16", 14, 2, 64, 1, 20, [5, 17, 40]),
+    ("bf16", 16, 2, 128, 64, 128, [900, 1]),
+    ("bf16", 32, 8, 128, 16, 60, [2048]),
+    ("bf16", 8, 8, 128, 8, 1, [1000, 31, 0, 2, 400, 7]),
+    ("bf16", 64, 2, 128, 32, 5, [333, 66]),
+    ("bf16", 130, 1, 64, 16, 3, [90]),
+    ("f32", 8, 8, 64, 24, 33, [300, 1111, 0]),
+    ("f32", 6, 2, 128, 0, 9, [64, 1, 200]),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,page,tokens,lens", SHAPES)
+def test_attention(binding, dtype, Hq, Hkv, D, page, tokens, lens):
+    rng = np.random.default_rng(Hq * 1000 + tokens)
+    B = len(lens)
+    cache = Cache(rng, o4.Paged(rng, B, max(lens) + tokens, page), 2, Hkv, D)
+    n_tree = rng.integers(1, tokens + 1, B).astype(np.int32)
+    n_tree[0] = tokens
+    anc, vis = zip(*(random_masks(rng, n_tree[b], tokens) for b in range(B)))
+    q = torch.randn((B, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(tokens), device="cuda").to(DT[dtype])
+    for b in range(B):
+        q[b, n_tree[b]:] = float("nan")  # rows past the tree may hold anything
+    ctx = context(binding, B, tokens)
+    kv_len = np.array(lens, np.int32)
+    out = run_attention(ctx, cache, q, kv_len, np.stack(anc), n_tree, layer=1)
+    assert ctx.cast_poll_status()[0] == 0
+    check_attention(out, cache, q, kv_len, vis, n_tree, dtype, layer=1)
+    again = run_attention(ctx, cache, q, kv_len, np.stack(anc), n_tree, layer=1)
+    assert torch.equal(out.view(torch.uint8), again.view(torch.uint8))  # the same bits every time
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.3, 4.0, -0.5])
+def test_attention_window_scale_and_odd_masks(binding, dtype, scale):
+    """Output rows from first_row on; scales that make scores large or turn them around; rows that see nothing, or only a
+    later tile; rows without a value in masked places, and one that some rows see."""
+    rng = np.random.default_rng(11)
+    B, tokens, Hq, Hkv, D = 4, 40, 8, 2, 128
+    lens = np.array([0, 100, 0, 513], np.int32)
+    cache = Cache(rng, o4.Paged(rng, B, 560, 16), 1, Hkv, D)
+    n_tree = np.array([40, 31, 40, 0], np.int32)
+    first = np.array([3, 31, 0, 0], np.int32)
+    anc, vis = (list(z) for z in zip(*(random_masks(rng, n_tree[b], tokens) for b in range(B))))
+    vis[0][5], anc[0][5] = False, 0                     # sees nothing
+    vis[0][6], anc[0][6] = False, 0                     # sees the last token alone
+    vis[0][6, 39], anc[0][6, 1] = True, np.uint32(1 << 7)
+    for b, token in ((0, 20), (2, 39)):                 # masked for most rows
+        pg, sl = cache.paged.at(b, np.array([lens[b] + token]))
+        cache.pair["v"][:, pg, :, sl] = np.nan
+        cache.pair["k"][:, pg, :, sl] = np.nan if b == 2 else 0.5
+    for b in range(B):                                  # whatever lies behind the sequence
+        pg, sl = cache.paged.at(b, np.arange(lens[b] + n_tree[b], cache.paged.positions))
+        cache.pair["v"][:, pg, :, sl], cache.pair["k"][:, pg, :, sl] = np.nan, np.nan
+    cache.upload()
+    q = torch.randn((B, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(DT[dtype])
+    ctx = context(binding, B, tokens)
+    out = run_attention(ctx, cache, q, lens, np.stack(anc), n_tree, first, scale)
+    assert ctx.cast_poll_status()[0] == 0
+    check_attention(out, cache, q, lens, vis, n_tree, dtype, first, scale)
+    assert bool((out[0, 5] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_far_scores(binding, dtype):
+    """Scores that climb by hundreds from tile to tile, and fall again: the running reference has to follow."""
+    rng = np.random.default_rng(12)
+    B, tokens, Hq, Hkv, D = 2, 6, 4, 2, 128
+    lens = np.array([1000, 517], np.int32)
+    cache = Cache(rng, o4.Paged(rng, B, 1010, 16), 1, Hkv, D)
+    for b in range(B):
+        pg, sl = cache.paged.at(b, np.arange(1006))
+        lift = np.where(np.arange(1006) % 700 < 350, np.arange(1006) % 350, 0) * 0.25
+        cache.pair["k"][0, pg, :, sl, 1] += lift[:, None]
+        cache.pair["k"] = o4.bf16(cache.pair["k"])
+    cache.upload()
+    q = torch.rand((B, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(2), device="cuda").to(DT[dtype])
+    anc, vis = zip(*(random_masks(rng, tokens, tokens) for b in range(B)))
+    n_tree = np.full(B, tokens, np.int32)
+    ctx = context(binding, B, tokens)
+    out = run_attention(ctx, cache, q, lens, np.stack(anc), n_tree)
+    check_attention(out, cache, q, lens, vis, n_tree, dtype)
+    assert ctx.cast_poll_status()[0] == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_reports_and_masks_bad_pages(binding, dtype):
+    rng = np.random.default_rng(13)
+    cache = Cache(rng, o4.Paged(rng, 2, 200, 16), 1, 2, 128)
+    q = torch.randn((2, 5, 4, 128), generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(DT[dtype])
+    anc, vis = zip(*(random_masks(rng, 5, 5) for b in range(2)))
+    lens, n_tree = np.array([150, 90], np.int32), np.array([5, 5], np.int32)
+    good = cache.paged.table.copy()
+    cache.paged.table[0, 3] = cache.paged.pages + 5
+    ctx = context(binding, 2, 5)
+    out = run_attention(ctx, cache, q, lens, np.stack(anc), n_tree)
+    status = ctx.cast_poll_status()
+    assert status[0] == 7 and status[1] == 0
+    cache.paged.table = good
+    # the other sequence is what it is; of the first, the positions of the bad page count as masked
+    keep = np.setdiff1d(np.arange(155), np.arange(48, 64))
+    for h in range(2):
+        k, _ = cache.rows("k", 0, 0, h, 155)
+        v, spread = cache.rows("v", 0, 0, h, 155)
+        want, _ = o4.attend(q[0, :, h * 2:h * 2 + 2].double().cpu().numpy(), k[keep], v[keep], spread[keep], 134, vis[0], 128 ** -0.5)
+        assert np.abs(out[0, :, h * 2:h * 2 + 2].double().cpu().numpy() - want).max() < 2e-2
+    one = np.array([0, 5], np.int32)
+    ref = run_attention(ctx, cache, q, lens, np.stack(anc), one)
+    assert torch.equal(out[1], ref[1])
+    # more positions than the sequence has room for; more tokens than the context verifies
+    run_attention(ctx, cache, q, np.array([204, 90], np.int32), np.stack(anc), n_tree)
+    assert ctx.cast_poll_status()[0] == 7
+    run_attention(ctx, cache, q, lens, np.stack(anc), np.array([5, 6], np.int32))
+    assert ctx.cast_poll_status() == (6, 1)
+
+
+def test_attention_needs_its_workspace_and_shapes(binding):
+    rng = np.random.default_rng(14)
+    cache = Cache(rng, o4.Paged(rng, 1, 4096, 16), 1, 2, 128)
+    ctx = context(binding, 1, 8)
+    q = torch.zeros((1, 8, 4, 128), dtype=torch.bfloat16, device="cuda")
+    anc, n, L = torch.zeros((1, 8, 1), dtype=torch.int32, device="cuda"), dev(np.array([8], np.int32)), dev(np.array([4000], np.int32))
+
+    def call(c=ctx, q=q, codes=cache.kc[0], B=1, Hq=4, Hkv=2, D=128, out=None):
+        c.cast_tree_attention_q4(q, codes, cache.kr[0], cache.vc[0], cache.vr[0], B, Hq, Hkv, D, *cache.where(), L, anc, n, None, 0.0,
+                                 q.clone() if out is None else out)
+
+    def code(**kw):
+        with pytest.raises(binding.CastError) as e:
+            call(**kw)
+        return e.value.code
+
+    assert code() == 3  # nothing reserved
+    ctx.cast_reserve_attention_q4(torch.bfloat16, 1, 4, 2, 128, 16, cache.paged.cap)
+    call()
+    assert code(B=2) == 3
+    assert code(Hq=3) == 2
+    assert code(D=96) == 2
+    assert code(Hkv=0) == 1
+    assert code(out=q.float()) == 4  # another type than the queries'
+    assert code(codes=cache.kc[0].reshape(-1)[8:]) == 2  # alignment
+    with pytest.raises(TypeError):
+        call(codes=cache.kc[0].view(torch.int8))
+    with pytest.raises(AssertionError):
+        call(q=q.transpose(1, 2))
+    with pytest.raises(binding.CastError):
+        ctx.cast_reserve_attention_q4(torch.bfloat16, 1, 4, 2, 100, 16, 4)
+    assert ctx.cast_poll_status()[0] == 0
+
+
+# ------------------------------------------------------------------------------------------------ compaction
+@pytest.mark.parametrize("D,page,Hkv", [(128, 16, 8), (64, 0, 2), (128, 5, 1)])
+def test_compaction(binding, D, page, Hkv):
+    rng = np.random.default_rng(page + D)
+    B, nl, H = 3, 3, 6
+    cache = Cache(rng, o4.Paged(rng, B, 90, page), nl, Hkv, D)
+    path = np.full((B, H + 1), -1, np.int32)
+    path[0, :4], path[1, :1], path[2] = [0, 2, 5, 9], [0], np.arange(7)
+    n = np.array([3, 0, 6], np.int32)
+    lens = np.array([60, 31, 47], np.int32)
+    for b in range(B):
+        src, to = cache.paged.at(b, lens[b] + path[b, :n[b] + 1]), cache.paged.at(b, lens[b] + np.arange(n[b] + 1))
+        for w in "kv":
+            for a in (cache.code[w], cache.pair[w]):
+                a[:, to[0], :, to[1]] = a[:, src[0], :, src[1]]
+    ctx = context(binding, B, 16, H)
+    kv_len = dev(lens)
+    ctx.cast_compact_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, B, nl, Hkv, D, *cache.where(), dev(path), dev(n), kv_len)
+    assert ctx.cast_poll_status()[0] == 0
+    np.testing.assert_array_equal(kv_len.cpu().numpy(), lens + n + 1)
+    for got, want in zip(cache.bits(), cache.host_bits()):
+        np.testing.assert_array_equal(got, want)
+    # a path that goes back, or past the capacity: nothing moves, the length stays
+    bad = path.copy()
+    bad[0, 2], bad[1, 0] = 1, 80
+    before, lens2 = cache.bits(), dev(lens)
+    ctx.cast_compact_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, B, nl, Hkv, D, *cache.where(), dev(bad),
+                           dev(np.array([3, 0, -1], np.int32)), lens2)
+    assert ctx.cast_poll_status()[0] == 7
+    np.testing.assert_array_equal(lens2.cpu().numpy()[:2], lens[:2])
+    for got, want in zip(cache.bits(), before):
+        np.testing.assert_array_equal(got, want)
+
+
+# ------------------------------------------------------------------------------------------------ as a program uses it
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_step_on_the_4_bit_cache(binding, captured):
+    """Prefill, then two steps: the tree's rows stored, attention of two layers, compaction - on another stream, and captured and
+    replayed with new inputs."""
+    rng = np.random.default_rng(21)
+    B, nl, T, Hq, Hkv, D, H = 2, 2, 12, 8, 2, 128, 4
+    paged = o4.Paged(rng, B, 260, 16)
+    cache = Cache(rng, paged, nl, Hkv, D)
+    ctx = context(binding, B, T, H)
+    ctx.cast_reserve_attention_q4(torch.bfloat16, B, Hq, Hkv, D, paged.page, paged.cap)
+    prompt = torch.randn((2, nl, B, 200, Hkv, D), device="cuda", dtype=torch.bfloat16)
+    n0 = np.array([200, 77], np.int32)
+    where, kv_len, n_rows = cache.where(), dev(n0), dev(np.array([T, T], np.int32))
+    new = torch.randn((2, nl, B, T, Hkv, D), device="cuda", dtype=torch.bfloat16)
+    q = torch.randn((nl, B, T, Hq, D), device="cuda", dtype=torch.bfloat16)
+    out = torch.full_like(q, float("nan"))
+    anc, vis = zip(*(random_masks(rng, T, T) for b in range(B)))
+    anc_d = dev(np.stack(anc).view(np.int32))
+    path, alen = torch.zeros((B, H + 1), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+
+    def step():
+        ctx.cast_store_kv_q4(new[0], new[1], B, nl, T, Hkv, D, *where, kv_len, n_rows, cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides)
+        for l in range(nl):
+            ctx.cast_tree_attention_q4(q[l], cache.kc[l], cache.kr[l], cache.vc[l], cache.vr[l], B, Hq, Hkv, D, *where, kv_len, anc_d,
+                                       n_rows, None, 0.0, out[l])
+        ctx.cast_compact_kv_q4(cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides, B, nl, Hkv, D, *where, path, alen, kv_len)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ctx.cast_store_kv_q4(prompt[0], prompt[1], B, nl, 200, Hkv, D, *where, None, kv_len, cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides)
+        graph = None
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+    host = {w: [[np.zeros((0, Hkv, D + 2))] * B for _ in range(nl)] for w in "kv"}
+    for i, w in enumerate("kv"):  # the rows every sequence holds: codes and pairs side by side
+        code, pair = o4.quantise(prompt[i].float().cpu().numpy())
+        rows = np.concatenate([code.astype(np.float64), pair], -1)
+        host[w] = [[rows[l, b, :n0[b]] for b in range(B)] for l in range(nl)]
+    lens = n0.copy()
+    for k in range(2):
+        g = torch.Generator("cuda").manual_seed(50 + k)
+        with torch.cuda.stream(side):
+            new.normal_(generator=g)
+            q.normal_(generator=g)
+            p = np.zeros((B, H + 1), np.int32)
+            p[0, :3], p[1, :2] = [0, 3, 7], [0, 1 + k]
+            path.copy_(torch.from_numpy(p))
+            alen.copy_(torch.from_numpy(np.array([2, 1], np.int32)))
+            graph.replay() if captured else step()
+        side.synchronize()
+        tree = {w: o4.quantise(new[i].float().cpu().numpy()) for i, w in enumerate("kv")}
+        for l in range(nl):
+            for b in range(B):
+                both = {w: np.concatenate([host[w][l][b], np.concatenate([tree[w][0][l, b], tree[w][1][l, b]], -1)]) for w in "kv"}
+                for h in range(Hkv):
+                    kk, vv = (o4.values(both[w][:, h, :D], both[w][:, h, D:]) for w in "kv")
+                    spread = np.abs(both["v"][:, h, D:D + 1] * (both["v"][:, h, :D] - 8))
+                    want, per = o4.attend(q[l, b, :, h * 4:h * 4 + 4].double().cpu().numpy(), kk, vv, spread, lens[b], vis[b], D ** -0.5)
+                    err = np.abs(out[l, b, :, h * 4:h * 4 + 4].double().cpu().numpy() - want)
+                    assert (err <= HALF["bf16"] * (np.abs(want) + per) + 1e-3).all()
+                for w in "kv":
+                    tr = both[w][lens[b]:]
+                    host[w][l][b] = np.concatenate([host[w][l][b], tr[p[b, :(3 if b == 0 else 2)]]])
+        lens = lens + np.array([3, 2], np.int32)
+        np.testing.assert_array_equal(kv_len.cpu().numpy(), lens)
+    assert ctx.cast_poll_status()[0] == 0
