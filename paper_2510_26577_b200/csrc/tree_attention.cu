@@ -27,6 +27,12 @@ bool tree_attention_tc_launch(cast_ctx* c, const void* q, const void* k, const v
 bool tree_attention_tc_takes(const cast_ctx* c, int B, int Hq, int Hkv, int D, int page_size, int seq_capacity);
 size_t tree_attention_tc_workspace(const cast_ctx* c, int B, int Hq, int Hkv, int D, int page_size, int seq_capacity);
 cast_status tree_attention_tc_reserve(cast_ctx* c, size_t bytes);
+// implemented in tree_attention_q4.cu: bf16 queries over 4-bit caches
+cast_status tree_attention_q4_reserve(cast_ctx* c, int B, int Hq, int Hkv);
+cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_codes, const void* k_range, const void* v_codes,
+                                     const void* v_range, int B, int Hq, int Hkv, int D, const Paging& g, const int32_t* kv_len,
+                                     const uint32_t* anc, const int32_t* n_tree, const int32_t* first_row, float scale, void* out,
+                                     cudaStream_t stream);
 }
 
 namespace {
@@ -568,6 +574,7 @@ extern "C" cast_status cast_reserve_attention_q4(cast_ctx* c, cast_dtype dtype, 
   const Paging g = {nullptr, page_size, seq_capacity, 0};
   if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
+  if (dtype == CAST_BF16) return tree_attention_q4_reserve(c, B, Hq, Hkv);
   // tickets start at zero; every merge leaves its ticket at zero again
   return grow_workspace(&c->attn_ws, &c->attn_ws_bytes, cc_plan(c, kOwn, B, Hq, Hkv, D, page_size, seq_capacity).bytes, kCcTicketBytes);
 }
@@ -585,6 +592,9 @@ extern "C" cast_status cast_tree_attention_q4(cast_ctx* c, const void* q, const 
   if (Hq % Hkv != 0 || (((uintptr_t)q | (uintptr_t)out) & 15)) return CAST_ERR_SHAPE;
   if (scale == 0.f) scale = 1.0f / sqrtf((float)D);
   cudaStream_t s = (cudaStream_t)stream;
+  if (dtype == CAST_BF16)
+    return tree_attention_q4_launch(c, q, k_codes, k_range, v_codes, v_range, B, Hq, Hkv, D, g, kv_len, anc_mask, n_tree, first_row,
+                                    scale, out, s);
   AttnParams p;
   p.q = q; p.k = k_codes; p.v = v_codes; p.out = out;
   p.B = B; p.Ncap = c->cfg.max_tree; p.Nmax = c->cfg.total_token; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
@@ -592,8 +602,7 @@ extern "C" cast_status cast_tree_attention_q4(cast_ctx* c, const void* q, const 
   p.page_table = page_table; p.kv_len = kv_len; p.n_tree = n_tree; p.first_row = first_row; p.anc = anc_mask;
   p.scale = scale; p.ticket = nullptr; p.part_o = nullptr; p.part_ml = nullptr; p.st = c->state;
   p.k_range = (const uint32_t*)k_range; p.v_range = (const uint32_t*)v_range;
-  if (dtype == CAST_F32) return D == 64 ? launch_cc<float, 64, true>(c, p, kOwn, s) : launch_cc<float, 128, true>(c, p, kOwn, s);
-  return D == 64 ? launch_cc<__nv_bfloat16, 64, true>(c, p, kOwn, s) : launch_cc<__nv_bfloat16, 128, true>(c, p, kOwn, s);
+  return D == 64 ? launch_cc<float, 64, true>(c, p, kOwn, s) : launch_cc<float, 128, true>(c, p, kOwn, s);
 }
 
 extern "C" cast_status cast_set_attention_early_reads(cast_ctx* c, int promise) {
