@@ -6,20 +6,21 @@
 // so a score carries no rounding but the accumulation's, and a weight (times its row's step) one to bf16; the last sum stays in fp32.
 //
 // Positions are the rows of both products, queries the columns: S^T = C_k Q^T (128 positions x N queries) and
-// O^T = C_v^T P^T (dims x N). A query column is a (tree token, head of the GQA group) pair, up to 64 per work item, N rounded up to
+// O^T = C_v^T P^T (dims x N). A query column is a (tree token, head of the GQA group) pair, up to 48 per work item, N rounded up to
 // 16: a small tree costs what it has, not a block of 128 rows, and its exponentials spread over all lanes. A thread of the softmax
 // owns one position: step and low are scalars of its own, masks are one word per position, and sums run in registers over
 // all its tiles, reduced across lanes once per item. What is paid for that: the maximum of a column lies across lanes, so the
 // running reference of a column is not its maximum but the first visible tile's, moved when a weight reaches 2^60 (bf16 and fp32 have
 // the range), which one vote per tile finds.
 //
-// Roles of a CTA's 17 warps (one CTA per SM):
-//   K producers (4): codes from global memory to registers two tiles ahead, unpacked to 16 + c, written to tensor memory as the
-//                    A operand (the dims in the order the quad of lanes holds them; Q is staged in the same order)
-//   V producers (4): the same codes to c - 8, 128-byte-swizzled rows in shared memory, the MN-major A operand as they lie
-//   MMA issuer (1) : S^T of tile i+1 before O^T of tile i
-//   softmax (8)    : two groups of four warps, a half of the columns each
-// Work is one line of tiles, item after item (sequence, kv-head, block of 64 rows), cut into equal pieces, one per CTA: ragged
+// Eight warps, two CTAs per SM, every warp with the same work: in a tile, its 16 rows of V codes to shared memory (c - 8, 128-byte
+// swizzled: the MN-major A operand as they lie), the softmax of 32 positions x half of the columns, its 16 rows of the next
+// tile's K codes to tensor memory (16 + c, the A operand; the dims in the order the quad of lanes holds them, and Q in the same order);
+// then the CTA meets, a warp issues S^T of the next tile and O^T of this one, and the products run under the next tile's V codes
+// and under the other CTA. Codes and pairs are requested a tile ahead, into registers. (Warps of their own for K, V, pairs, the MMAs and
+// the softmax, 18 in one CTA per SM, took six times as long: five streams of unrolled code on one SM's instruction cache, every
+// instruction about ten cycles apart.)
+// Work is one line of tiles, item after item (sequence, kv-head, block of 48 rows), cut into equal pieces, one per CTA: ragged
 // batches load the machine evenly. An item that lies across CTAs leaves partials in the workspace; the last CTA to finish it
 // (an atomic ticket, nothing spins) merges them in CTA order. All mbarrier waits are bounded: on expiry the CTA records
 // CAST_ERR_TIMEOUT, stops touching the operands and runs out.
@@ -33,15 +34,10 @@ namespace cast {
 namespace {
 
 constexpr int kTile = 128;       // positions per tile (UMMA M)
-constexpr int kRows = 64;        // query columns per item at most (UMMA N)
-constexpr int kSoftThreads = 256;
-constexpr int kWarpK = 8, kWarpV = 12, kWarpMma = 16;
-constexpr int kThreadsQ4 = 640;  // (registers are allotted per four warps: the issuer's group has three idle ones)
-// Registers per thread: 96 at launch (640 threads), then the groups of four warps take what they need of the 61440.
-constexpr int kRegsSoft = 136, kRegsProduce = 88, kRegsIssue = 24;
-static_assert(256 * kRegsSoft + 256 * kRegsProduce + 128 * kRegsIssue <= 640 * 96, "the shares add up to no more than the launch has");
-constexpr int kAhead = 2;        // tiles of codes in registers ahead of the one in work
-constexpr int kMaxGrid = 256;
+constexpr int kRows = 48;        // query columns per item at most (UMMA N): half of them, three times eight, are a thread's
+constexpr int kHalf = kRows / 2;
+constexpr int kThreadsQ4 = 256;
+constexpr int kMaxGrid = 512;
 constexpr int kMaxJoin = 32;     // CTAs that share an item, about
 constexpr float kFar = 1.15292150460684698e18f;  // 2^60
 
@@ -69,35 +65,49 @@ struct Q4Params {
 template <int HD>
 struct Lay {
   static constexpr int kW = HD / 32;                 // words of codes per thread and row (four threads to a row)
-  static constexpr int kSmemQ = 0;                   // HD / 64 regions [64 rows][64] bf16
+  static constexpr int kSmemQ = 0;                   // HD / 64 regions [48 rows][64] bf16
   static constexpr int kRegionQ = kRows * 128;
   static constexpr int kSmemV = kSmemQ + HD / 64 * kRegionQ;
   static constexpr int kRegionV = kTile * 128;       // [128 positions][64] bf16
   static constexpr int kBufV = HD / 64 * kRegionV;
-  static constexpr int kSmemP = kSmemV + 2 * kBufV;  // [128 positions][64 rows] bf16
+  static constexpr int kSmemP = kSmemV + 2 * kBufV;  // [128 positions][64] bf16, 48 of them used
   static constexpr int kBufP = kTile * 128;
-  static constexpr int kSmemMisc = kSmemP + 2 * kBufP;
+  static constexpr int kSmemMisc = kSmemP + kBufP;
 };
 
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+
+// A place on the line of tiles.
+struct Walk {
+  int b, h, rb, t;  // sequence, kv-head, row block, tile of the item
+  int left;         // tiles from here to the end of the CTA's piece, this one included; behind the end the place stays the last
+};
 struct Misc {
-  uint64_t bar_ka[2], bar_s[2], bar_v[2], bar_p[2], bar_o[2], bar_q;
+  uint64_t bar_s, bar_o;
   uint32_t tmem;
-  int last;
+  int last, workers;
+  long long piece;                     // tiles of a CTA, rounded down; the first `rest` CTAs take one more
+  int rest;
+  Walk seg;                            // the item in work, from its first tile here on
+  Walk ahead;                          // the furthest tile in `step`
+  alignas(16) int4 step[8];            // tile i of the CTA at i % 8: sequence, kv-head, first position, positions of the sequence
   long long pre[CAST_MAX_BATCH + 1];   // tiles of the sequences before
   long long bound[kMaxGrid + 1];       // first tile of every CTA
   int L[CAST_MAX_BATCH], N[CAST_MAX_BATCH], F[CAST_MAX_BATCH], tl[CAST_MAX_BATCH], nr[CAST_MAX_BATCH], total[CAST_MAX_BATCH];
-  int workers;
-  int b0, hr0, t0;                     // where this CTA starts
   alignas(16) float sq[kRows];         // sums of the query rows
-  alignas(16) float m[kRows];          // references, log2 units; -inf: none yet
-  alignas(16) float tot_l[kRows];
-  alignas(16) float tot_z[kRows];
+  alignas(16) float nm[kRows];         // references, log2 units, negated; inf: none yet
+  alignas(16) float alpha[kRows];      // what a moved reference scales by
+  alignas(16) uint32_t at[kRows];      // a query row's first element in q and out
+  float tot_l[kRows], tot_z[kRows];
   float red_l[4][kRows], red_z[4][kRows];
-  float colmax[8][kRows / 2];
-  uint32_t vis[2][CAST_MAX_TREE];      // columns (32 + 32) that see a tree token
+  float colmax[8][kHalf];
+  uint32_t vis[2][CAST_MAX_TREE];      // columns (32 + 16) that see a tree token
 };
 
-constexpr int kTmemK = 0, kTmemS = 128, kTmemO = 256, kTmemCols = 512;  // K codes 2 x 64, scores 2 x 64, output 64 (of 512: one CTA per SM)
+constexpr int kTmemK = 0, kTmemS = 64, kTmemO = 128, kTmemCols = 256;  // K codes 64, scores 48, output 48
 
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ bool named_or(int id, int threads, bool pred) {
@@ -144,55 +154,79 @@ __device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const uint32_t (&r
           "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ unsigned long long mul_f2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
+// (x & mask) | base in one instruction: written with operators it became two.
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(base));
+  return r;
+}
 // Codes i and i + 4 of a word (its nibbles) as a pair of bf16. 16 + c: the code in the upper mantissa bits of 16, whose step is 1 / 8
 // there and 1 with the code three bits up. 128 + c: the code in the lowest bits.
 template <int I>
 __device__ __forceinline__ uint32_t pair_plus16(uint32_t w) {
-  const uint32_t s = I == 0 ? w << 3 : I == 1 ? w >> 1 : I == 2 ? w >> 5 : w >> 9;
-  return (s & 0x00780078u) | 0x41804180u;
+  return and_or(I == 0 ? w << 3 : I == 1 ? w >> 1 : I == 2 ? w >> 5 : w >> 9, 0x00780078u, 0x41804180u);
 }
 template <int I>
 __device__ __forceinline__ uint32_t pair_minus8(uint32_t w) {
-  const uint32_t x = ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;
+  const uint32_t x = and_or(w >> (4 * I), 0x000f000fu, 0x43004300u);
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), __floats2bfloat162_rn(136.f, 136.f));  // exact
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 
-// A place on the line of tiles.
-struct Walk {
-  int b, hr, t;   // sequence, kv-head * row blocks + row block, tile of the item
-  int left;       // tiles from here to the end of the CTA's piece, this one included
-};
 __device__ __forceinline__ void advance(Walk& w, const Misc& s, const Q4Params& p) {
-  --w.left;
-  if (++w.t < s.tl[w.b] || w.left <= 0) return;
+  if (--w.left <= 0 || ++w.t < s.tl[w.b]) return;
   w.t = 0;
-  if (++w.hr < p.Hkv * s.nr[w.b]) return;
-  w.hr = 0;
+  if (++w.rb < s.nr[w.b]) return;
+  w.rb = 0;
+  if (++w.h < p.Hkv) return;
+  w.h = 0;
   do ++w.b;
   while (s.tl[w.b] == 0);  // (tiles are left, so a sequence with tiles follows)
 }
 
-// Page of a position (-1: none, or an id out of range) and its row among the 4-bit rows.
-__device__ __forceinline__ int page_of(const Q4Params& p, int b, int pos, int total) {
-  if (pos >= total) return -1;
-  if (p.g.page_size == 0) return b;
-  const int id = p.g.table[(size_t)b * p.g.seq_capacity + (int)(((uint64_t)(uint32_t)pos * p.page_mul) >> p.page_shift)];
-  return id < 0 || id >= p.g.num_pages ? -2 : id;
+// Loads that stay where they are written: left to itself the compiler moves a load down to its use, a tile later.
+__device__ __forceinline__ int ld_here(const int32_t* p) {
+  int r;
+  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(r) : "l"(p));
+  return r;
 }
-__device__ __forceinline__ long long row_of(const Q4Params& p, int page, int h, int pos) {
-  const int ps = p.g.page_size;
-  if (ps == 0) return ((long long)page * p.Hkv + h) * p.g.seq_capacity + pos;
-  return ((long long)page * p.Hkv + h) * ps + (pos - (int)(((uint64_t)(uint32_t)pos * p.page_mul) >> p.page_shift) * ps);
+__device__ __forceinline__ void ld_here(uint32_t (&r)[4], const unsigned char* p) {
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+}
+__device__ __forceinline__ void ld_here(uint32_t (&r)[2], const unsigned char* p) {
+  asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
 }
 
-// A column's two sums over the 32 lanes, for 32 columns: lane l returns column l's.
+// Pages, rows and pairs are requested tiles ahead of their use: nothing between the request and the use may look at what has
+// been requested, so places without a row request another's (position total - 1, page 0) and are told apart when they are used.
+// (Branches around the loads made every one of them a wait: 7 us a tile instead of less than one.)
+template <bool kPaged>
+__device__ __forceinline__ int request_page(const Q4Params& p, int b, int pos, int total) {
+  if (!kPaged) return b;
+  const int at = min(pos, total - 1);
+  return ld_here(p.g.table + (size_t)b * p.g.seq_capacity + (uint32_t)(((uint64_t)(uint32_t)at * p.page_mul) >> p.page_shift));
+}
+// Index of the row of a position: below 2^32, as the host has checked.
+template <bool kPaged>
+__device__ __forceinline__ uint32_t row_of(const Q4Params& p, int page, int h, int pos, int total) {
+  const uint32_t at = min(pos, total - 1);
+  if (!kPaged) return (uint32_t)(page * p.Hkv + h) * (uint32_t)p.g.seq_capacity + at;
+  const uint32_t ps = p.g.page_size, slot = at - (uint32_t)(((uint64_t)at * p.page_mul) >> p.page_shift) * ps;
+  return ((uint32_t)((uint32_t)page < (uint32_t)p.g.num_pages ? page : 0) * (uint32_t)p.Hkv + (uint32_t)h) * ps + slot;
+}
+template <bool kPaged>
+__device__ __forceinline__ bool page_ok(const Q4Params& p, int page) {
+  return !kPaged || (uint32_t)page < (uint32_t)p.g.num_pages;
+}
+
+// A value per column (32 of them, in every lane), added or maximised over the lanes: lane l returns column l's.
+template <bool kMax>
 __device__ __forceinline__ float reduce_columns(float (&v)[32]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -200,200 +234,49 @@ __device__ __forceinline__ float reduce_columns(float (&v)[32]) {
 #pragma unroll
     for (int i = 0; i < o; ++i) {
       const bool up = (lane & o) != 0;
-      const float mine = up ? v[i + o] : v[i], other = up ? v[i] : v[i + o];
-      v[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+      const float mine = up ? v[i + o] : v[i], other = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + o], o);
+      v[i] = kMax ? fmaxf(mine, other) : mine + other;
     }
   }
   return v[0];
 }
 
-// ---- producers: kV = false: K codes to tensor memory; true: V codes to shared memory
-template <int HD, bool kV>
-__device__ __forceinline__ void produce(const Q4Params& p, Misc& s, unsigned char* smem, Walk start, uint32_t tmem) {
-  using LY = Lay<HD>;
-  constexpr int W = LY::kW;
-  const int lane = threadIdx.x & 31, pw = ((int)threadIdx.x >> 5) & 3, r = lane >> 2, tq = lane & 3;
-  uint32_t code[kAhead][4][W];
-  int page[kAhead][4];
-  Walk wi = start, wc = start;
-  auto load_pages = [&](int (&pg)[4]) {
-    if (wi.left <= 0) return;
+// ---- softmax of half of the columns (kMasked: `vm` says which of them see the position). Scores become weights.
+template <int NH, bool kMasked>
+__device__ __forceinline__ void weights(float (&p)[NH], const float* sq, const float* nm, float ks, float kl, uint32_t vm) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) pg[j] = page_of(p, wi.b, wi.t * kTile + pw * 32 + 8 * j + r, s.total[wi.b]);
-    advance(wi, s, p);
-  };
-  auto load_codes = [&](uint32_t (&c)[4][W], const int (&pg)[4]) {
-    if (wc.left <= 0) return;
-    const int h = wc.hr / s.nr[wc.b];
-    const unsigned char* base = (kV ? p.vc : p.kc) + tq * (4 * W);
+  for (int c = 0; c < NH; c += 4) {
+    const float4 q4 = *reinterpret_cast<const float4*>(sq + c), m4 = *reinterpret_cast<const float4*>(nm + c);
+    const float q[4] = {q4.x, q4.y, q4.z, q4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-      for (int w = 0; w < W; ++w) c[j][w] = 0u;
-      if (pg[j] >= 0) {
-        const unsigned char* at = base + row_of(p, pg[j], h, wc.t * kTile + pw * 32 + 8 * j + r) * (HD / 2);
-        if constexpr (W == 4) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(at));
-          c[j][0] = x.x; c[j][1] = x.y; c[j][2] = x.z; c[j][3] = x.w;
-        } else {
-          const uint2 x = __ldg(reinterpret_cast<const uint2*>(at));
-          c[j][0] = x.x; c[j][1] = x.y;
-        }
-      } else if (!kV && pg[j] == -2 && tq == 0) {
-        report(p.st, CAST_ERR_BAD_PAGE, wc.b);
-      }
-    }
-    advance(wc, s, p);
-  };
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) load_pages(page[d]);
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) load_codes(code[d], page[d]);
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) load_pages(page[d]);
-  bool ok = true;
-  for (int it0 = 0; it0 < start.left; it0 += kAhead) {
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d) {
-      const int it = it0 + d;
-      if (it >= start.left) break;
-      static_assert(kAhead == 2, "buffer d is tile it's");
-      // the buffer's last reader: S^T (K) or O^T (V) of tile it - 2
-      if (it >= 2 && ok) {
-        ok = mbar_wait(kV ? &s.bar_o[d] : &s.bar_s[d], (uint32_t)(((it >> 1) - 1) & 1));
-        if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, start.b);
-      }
-      if (ok) {
-        if constexpr (kV) {
-          unsigned char* buf = smem + LY::kSmemV + d * LY::kBufV;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int row = pw * 32 + 8 * j + r;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-              const uint32_t c = code[d][j][w];
-              const int region = W == 4 ? w >> 1 : 0, chunk = 2 * tq + (w & 1);
-              *reinterpret_cast<uint4*>(buf + region * LY::kRegionV + swz(row, chunk)) =
-                  make_uint4(pair_minus8<0>(c), pair_minus8<1>(c), pair_minus8<2>(c), pair_minus8<3>(c));
-            }
-          }
-          fence_proxy_async();
-        } else {
-          tc_fence_after();
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            uint32_t out[8 * W];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int w = 0; w < W; ++w) {  // word w's pairs 0, 1 go to the group of 16 dims 2 w, pairs 2, 3 to 2 w + 1
-                const uint32_t c = code[d][2 * hf + j][w];
-                out[8 * w + 2 * j] = pair_plus16<0>(c);
-                out[8 * w + 2 * j + 1] = pair_plus16<1>(c);
-                out[8 * w + 4 + 2 * j] = pair_plus16<2>(c);
-                out[8 * w + 4 + 2 * j + 1] = pair_plus16<3>(c);
-              }
-            tmem_st_quads<2 * W>(tmem + kTmemK + d * 64 + ((uint32_t)(pw * 32 + hf * 16) << 16), out);
-          }
-          tmem_wait_st();
-          tc_fence_before();
-        }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(kV ? &s.bar_v[d] : &s.bar_ka[d]);
-      load_codes(code[d], page[d]);
-      load_pages(page[d]);
+    for (int e = 0; e < 4; ++e) {
+      const float y = fast_exp2(fmaf(ks, p[c + e], fmaf(kl, q[e], m[e])));
+      p[c + e] = kMasked && !((vm >> (c + e)) & 1u) ? 0.f : y;
     }
   }
 }
-
-// ---- the MMA issuer (the whole warp, converged)
-template <int HD>
-__device__ __forceinline__ void issue(const Q4Params& p, Misc& s, unsigned char* smem, Walk w, uint32_t tmem) {
-  using LY = Lay<HD>;
-  const uint32_t tm = __reduce_or_sync(0xffffffffu, tmem);
-  const uint64_t dq = umma_desc(smem_u32(smem + LY::kSmemQ), 16, 1024);
-  const uint64_t dv = umma_desc(smem_u32(smem + LY::kSmemV), HD == 128 ? LY::kRegionV : 0, 1024);  // 64 dims: both halves of M alike
-  const uint64_t dp = umma_desc(smem_u32(smem + LY::kSmemP), 0, 1024);
-  int it = 0;
-  uint32_t q_phase = 0;
-  bool ok = true;
-  while (w.left > 0 && ok) {
-    const int tl = s.tl[w.b], n = __reduce_max_sync(0xffffffffu, min(w.left, tl - w.t));
-    const int rows = min((s.N[w.b] - s.F[w.b]) * p.G - w.hr % s.nr[w.b] * kRows, kRows), N = __reduce_max_sync(0xffffffffu, (rows + 15) & -16);
-    const uint32_t shape = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-    const uint32_t idesc_s = shape, idesc_o = shape | (1u << 15) | (1u << 16);  // both operands of the second product are MN-major
-    auto scores = [&](int i) -> bool {
-      if (!mbar_wait(&s.bar_ka[i & 1], (uint32_t)(i >> 1) & 1u)) return false;
-      tc_fence_after();
+// Sums on, weights times step to the B operand.
+template <int NH, bool kMasked>
+__device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], float (&z)[NH],
+                                          unsigned char* row, int r7, int chunk0, float vs, float vl, uint32_t vm) {
 #pragma unroll
-      for (int ks = 0; ks < HD / 16; ++ks)
-        umma_bf16_ts(tm + kTmemS + (i & 1) * 64, tm + kTmemK + (i & 1) * 64 + ks * 8,
-                     dq + (uint64_t)((ks >> 2) * (LY::kRegionQ >> 4) + (ks & 3) * 2), idesc_s, ks > 0);
-      umma_commit(&s.bar_s[i & 1]);
-      return true;
-    };
-    ok = mbar_wait(&s.bar_q, q_phase) && scores(it);
-    q_phase ^= 1;
-    for (int i = 0; ok && i < n; ++i, ++it) {
-      if (i + 1 < n) ok = scores(it + 1);
-      ok = ok && mbar_wait(&s.bar_p[it & 1], (uint32_t)(it >> 1) & 1u) && mbar_wait(&s.bar_v[it & 1], (uint32_t)(it >> 1) & 1u);
-      if (!ok) break;
-      tc_fence_after();
-      const uint64_t a = dv + (uint64_t)((it & 1) * (LY::kBufV >> 4)), bb = dp + (uint64_t)((it & 1) * (LY::kBufP >> 4));
-#pragma unroll
-      for (int ks = 0; ks < kTile / 16; ++ks)
-        umma_bf16(tm + kTmemO, a + (uint64_t)(ks * (2048 >> 4)), bb + (uint64_t)(ks * (2048 >> 4)), idesc_o, (i > 0 || ks > 0) ? 1u : 0u);
-      umma_commit(&s.bar_o[it & 1]);
-    }
-    for (int i = 0; i < n; ++i) advance(w, s, p);
-  }
-  if (!ok && (threadIdx.x & 31) == 0) report(p.st, CAST_ERR_TIMEOUT, w.b);
-}
-
-// ---- softmax of half of the columns (kMasked: `vm` says which of them see the position)
-template <bool kMasked>
-__device__ __forceinline__ void weights(float (&p)[32], const Misc& s, int c0, int nh, float ks, float kl, uint32_t vm) {
-  const unsigned long long ks2 = pack_f2(ks, ks), kl2 = pack_f2(kl, kl);
-#pragma unroll
-  for (int c8 = 0; c8 < 4; ++c8) {
-    if (c8 * 8 >= nh) break;
-#pragma unroll
-    for (int c = c8 * 8; c < c8 * 8 + 8; c += 4) {
-      const float4 sq = *reinterpret_cast<const float4*>(&s.sq[c0 + c]), m = *reinterpret_cast<const float4*>(&s.m[c0 + c]);
-      float x[4];
-      unpack_f2(fma_f2(ks2, pack_f2(p[c], p[c + 1]), fma_f2(kl2, pack_f2(sq.x, sq.y), pack_f2(-m.x, -m.y))), x[0], x[1]);
-      unpack_f2(fma_f2(ks2, pack_f2(p[c + 2], p[c + 3]), fma_f2(kl2, pack_f2(sq.z, sq.w), pack_f2(-m.z, -m.w))), x[2], x[3]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float y = fast_exp2(x[e]);
-        p[c + e] = kMasked && !((vm >> (c + e)) & 1u) ? 0.f : y;
-      }
-    }
-  }
-}
-template <bool kMasked>
-__device__ __forceinline__ void hand_over(const float (&p)[32], unsigned long long (&l)[16], unsigned long long (&z)[16], unsigned char* row,
-                                          int r7, int chunk0, int nh, float vs, float vl, uint32_t vm) {
-  const unsigned long long vs2 = pack_f2(vs, vs), vl2 = pack_f2(vl, vl);
-#pragma unroll
-  for (int c8 = 0; c8 < 4; ++c8) {
-    if (c8 * 8 >= nh) break;
+  for (int c8 = 0; c8 < NH / 8; ++c8) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int c = c8 * 8 + 2 * e;
-      const unsigned long long p2 = pack_f2(p[c], p[c + 1]);
-      l[c / 2] = add_f2(l[c / 2], p2);
-      float w0, w1;
-      unpack_f2(mul_f2(p2, vs2), w0, w1);
+      l[c] += p[c];
+      l[c + 1] += p[c + 1];
+      float w0 = p[c] * vs, w1 = p[c + 1] * vs;
       if (kMasked) {  // (a masked row of V without a value: 0 * NaN)
         const bool v0 = (vm >> c) & 1u, v1 = (vm >> (c + 1)) & 1u;
-        z[c / 2] = fma_f2(p2, pack_f2(v0 ? vl : 0.f, v1 ? vl : 0.f), z[c / 2]);
+        z[c] = fmaf(p[c], v0 ? vl : 0.f, z[c]);
+        z[c + 1] = fmaf(p[c + 1], v1 ? vl : 0.f, z[c + 1]);
         w0 = v0 ? w0 : 0.f;
         w1 = v1 ? w1 : 0.f;
       } else {
-        z[c / 2] = fma_f2(p2, vl2, z[c / 2]);
+        z[c] = fmaf(p[c], vl, z[c]);
+        z[c + 1] = fmaf(p[c + 1], vl, z[c + 1]);
       }
       const __nv_bfloat162 h = __floats2bfloat162_rn(w0, w1);
       w[e] = *reinterpret_cast<const uint32_t*>(&h);
@@ -402,362 +285,139 @@ __device__ __forceinline__ void hand_over(const float (&p)[32], unsigned long lo
   }
 }
 
-// Merge of an item's partials by the 256 softmax threads of the CTA that finished it last: contributors in CTA order, a thread
+// Merge of an item's partials by the CTA that finished it last: contributors in CTA order, a thread
 // per 8 lanes of a row (which are 8 neighbouring dims).
 template <int HD>
-__device__ __forceinline__ void merge_item(const Q4Params& p, const Misc& s, int b, int h, int grow0, int rows, int c_lo, int c_hi,
-                                           long long first) {
-  constexpr int CPR = HD / 8, RPP = kSoftThreads / CPR;
+__device__ __forceinline__ void merge_item(const Q4Params& p, const Misc& s, int rows, int c_lo, int c_hi, long long first) {
+  constexpr int CPR = HD / 8, RPP = kThreadsQ4 / CPR;  // threads per row, rows at a time
   const int ch = threadIdx.x % CPR;
-  for (int r = threadIdx.x / CPR; r < rows; r += RPP) {
-    float M = -INFINITY;
-    for (int c = c_lo; c <= c_hi; ++c) {
-      const int slot = s.bound[c] > first ? 0 : 1;
-      if (s.bound[c + 1] > s.bound[c]) M = fmaxf(M, __ldcg(p.part_ml + ((size_t)c * 2 + slot) * kRows + r).x);
-    }
+  // The contributors' pairs, one per thread of the row, are one round trip; their rows, eight at a time, the next.
+  auto slot_of = [&](int c) { return ((uint32_t)c * 2 + (s.bound[c] > first ? 0 : 1)) * kRows; };
+  auto pair_of = [&](int c, int r) {
+    return c > c_hi || s.bound[c + 1] <= s.bound[c] || r >= rows ? make_float2(-INFINITY, 0.f) : __ldcg(p.part_ml + slot_of(c) + r);
+  };
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += RPP) {
+    const int r = r0 + threadIdx.x / CPR;
+    float2 ml = pair_of(c_lo + ch, r);
+    float M = ml.x;
+    for (int cb = c_lo + CPR; cb <= c_hi; cb += CPR) M = fmaxf(M, pair_of(cb + ch, r).x);
+#pragma unroll
+    for (int o = CPR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     float acc[8] = {}, l = 0.f;
-#pragma unroll 2
-    for (int c = c_lo; c <= c_hi; ++c) {
-      if (s.bound[c + 1] <= s.bound[c]) continue;
-      const size_t at = ((size_t)c * 2 + (s.bound[c] > first ? 0 : 1)) * kRows + r;
-      const float2 ml = __ldcg(p.part_ml + at);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + ch * 8));
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + ch * 8 + 4));
-      const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-      l += w * ml.y;
-      acc[0] += w * x.x; acc[1] += w * x.y; acc[2] += w * x.z; acc[3] += w * x.w;
-      acc[4] += w * y.x; acc[5] += w * y.y; acc[6] += w * y.z; acc[7] += w * y.w;
+    const float* const base = p.part_o + (size_t)min(r, rows - 1) * HD + ch * 8;
+#pragma unroll 1
+    for (int cb = c_lo; cb <= c_hi; cb += CPR) {
+      if (cb > c_lo) ml = pair_of(cb + ch, r);
+      const float wm = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M), lm = wm * ml.y;
+      const uint32_t off = slot_of(min(cb + ch, c_hi)) * HD;
+#pragma unroll 1
+      for (int k0 = 0; k0 < CPR && cb + k0 <= c_hi; k0 += 8) {
+        float4 x[8], y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float* at = base + __shfl_sync(0xffffffffu, off, k0 + k, CPR);
+          x[k] = __ldcg(reinterpret_cast<const float4*>(at));
+          y[k] = __ldcg(reinterpret_cast<const float4*>(at + 4));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float wk = __shfl_sync(0xffffffffu, wm, k0 + k, CPR);
+          l += __shfl_sync(0xffffffffu, lm, k0 + k, CPR);
+          if (wk != 0.f) {  // (a contributor that is none, or saw nothing: its place may hold anything)
+            acc[0] += wk * x[k].x; acc[1] += wk * x[k].y; acc[2] += wk * x[k].z; acc[3] += wk * x[k].w;
+            acc[4] += wk * y[k].x; acc[5] += wk * y[k].y; acc[6] += wk * y[k].z; acc[7] += wk * y[k].w;
+          }
+        }
+      }
     }
+    if (r >= rows) continue;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     // lanes 8 ch + j: dims base + {0, 4, 1, 5, 2, 6, 3, 7}
-    const int base = HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch;
+    const int dim = HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch;
     const __nv_bfloat162 o0 = __floats2bfloat162_rn(acc[0] * inv, acc[2] * inv), o1 = __floats2bfloat162_rn(acc[4] * inv, acc[6] * inv),
                          o2 = __floats2bfloat162_rn(acc[1] * inv, acc[3] * inv), o3 = __floats2bfloat162_rn(acc[5] * inv, acc[7] * inv);
-    const int grow = grow0 + r, t = grow / p.G;
-    *reinterpret_cast<uint4*>(p.out + (((size_t)b * p.Ncap + t) * p.Hq + h * p.G + (grow - t * p.G)) * HD + base) =
+    *reinterpret_cast<uint4*>(p.out + s.at[r] + dim) =
         make_uint4(*reinterpret_cast<const uint32_t*>(&o0), *reinterpret_cast<const uint32_t*>(&o1),
                    *reinterpret_cast<const uint32_t*>(&o2), *reinterpret_cast<const uint32_t*>(&o3));
   }
 }
 
-template <int HD>
-__device__ __forceinline__ void softmax(const Q4Params& p, Misc& s, unsigned char* smem, Walk w, uint32_t tmem) {
-  using LY = Lay<HD>;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cg = warp >> 2, wg_bar = 1 + cg;
-  const int posl = (warp & 3) * 32 + lane;                    // this thread's position in a tile, and its tensor-memory lane
-  const uint32_t tl_sel = (uint32_t)((warp & 3) * 32) << 16;
-  const float sc = p.scale_log2;
-  // pairs of the row, one tile ahead; its page, two
-  Walk wi = w, wr = w;
-  int page = -1;
-  uint32_t nkr = 0, nvr = 0;
-  bool nlive = false;
-  auto load_page = [&] {
-    if (wi.left <= 0) return;
-    page = page_of(p, wi.b, wi.t * kTile + posl, s.total[wi.b]);
-    advance(wi, s, p);
-  };
-  auto load_pair = [&] {
-    if (wr.left <= 0) return;
-    nlive = page >= 0;
-    if (nlive) {
-      const long long row = row_of(p, page, wr.hr / s.nr[wr.b], wr.t * kTile + posl);
-      nkr = __ldg(p.kr + row);
-      nvr = __ldg(p.vr + row);
-    }
-    advance(wr, s, p);
-  };
-  load_page();
-  load_pair();
-  load_page();
+// This thread's NH scores. (The wait is tied to the registers, so that no use of them can be scheduled above it.)
+template <int NH>
+__device__ __forceinline__ void read_scores(uint32_t taddr, float (&p)[NH]) {
+#pragma unroll
+  for (int c = 0; c < NH; c += 8) tmem_ld8(taddr + c, reinterpret_cast<uint32_t*>(p) + c);
+  if constexpr (NH == 8)
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(p[0]), "+f"(p[1]), "+f"(p[2]), "+f"(p[3]), "+f"(p[4]), "+f"(p[5]), "+f"(p[6]), "+f"(p[7])
+                 :
+                 : "memory");
+  else
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(p[0]), "+f"(p[1]), "+f"(p[2]), "+f"(p[3]), "+f"(p[4]), "+f"(p[5]), "+f"(p[6]), "+f"(p[7]), "+f"(p[8]), "+f"(p[9]),
+                   "+f"(p[10]), "+f"(p[11]), "+f"(p[12]), "+f"(p[13]), "+f"(p[14]), "+f"(p[15]), "+f"(p[16]), "+f"(p[17]), "+f"(p[18]),
+                   "+f"(p[19]), "+f"(p[20]), "+f"(p[21]), "+f"(p[22]), "+f"(p[23])
+                 :
+                 : "memory");
+}
 
-  int it = 0;
-  bool ok = true;
-  while (w.left > 0) {
-    const int b = w.b, nr = s.nr[b], h = w.hr / nr, rb = w.hr - h * nr, t0 = w.t, tl = s.tl[b], n = min(w.left, tl - t0);
-    const int L = s.L[b], N = s.N[b], F = s.F[b], total = s.total[b];
-    const int rows = min((N - F) * p.G - rb * kRows, kRows), nh = ((rows + 15) & -16) / 2, c0 = cg * nh, grow0 = F * p.G + rb * kRows;
-    named_sync(3, kSoftThreads);  // the item before is done with the arrays below
-    // ---- the query rows, their dims in the order of the codes in tensor memory; their sums
-    {
-      constexpr int VPR = HD / 8, W = LY::kW;
+// New references for the columns of a group of four warps (all of them call), from the tile's largest scores (`p`: the scores, as
+// they come); what the columns have gathered (first: nothing yet) follows. An item's first tile, and scores that climb by 2^60.
+template <int NH>
+__device__ __forceinline__ void move_references(Misc& s, const float (&p)[NH], int cg, int c0, int wg_bar, bool first, uint32_t t_o, float ks,
+                                                float kl, uint32_t vm, float (&l)[NH], float (&z)[NH]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mine = (int)threadIdx.x & 127;
+  {
+    float v[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) v[c] = c < NH && ((vm >> c) & 1u) ? fmaf(ks, p[c < NH ? c : 0], kl * s.sq[c0 + (c < NH ? c : 0)]) : -INFINITY;
+    const float y = reduce_columns<true>(v);
+    if (lane < NH) s.colmax[warp][lane] = y;
+  }
+  named_sync(wg_bar, 128);
+  if (mine < NH) {
+    const float nm_old = s.nm[c0 + mine];
+    const float mx = fmaxf(fmaxf(s.colmax[cg * 4][mine], s.colmax[cg * 4 + 1][mine]), fmaxf(s.colmax[cg * 4 + 2][mine], s.colmax[cg * 4 + 3][mine]));
+    const float nm_new = nm_old == INFINITY || mx + nm_old >= 59.f ? -mx : nm_old;
+    s.alpha[c0 + mine] = nm_old == INFINITY || nm_new == nm_old ? 1.f : exp2f(nm_new - nm_old);
+    s.nm[c0 + mine] = nm_new;
+  }
+  named_sync(wg_bar, 128);
+  if (first) return;
 #pragma unroll 1
-      for (int i = tid; i < 2 * nh * VPR; i += kSoftThreads) {
-        const int r = i / VPR, v = i % VPR, t = v / W, wd = v % W;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (r < rows) {
-          const int grow = grow0 + r, tok = grow / p.G;
-          x = __ldg(reinterpret_cast<const uint4*>(p.q + (((size_t)b * p.Ncap + tok) * p.Hq + h * p.G + (grow - tok * p.G)) * HD + v * 8));
-        }
-        float f[8], sum = 0.f;
-        Vec<__nv_bfloat16>::unpack(x, f);
+  for (int c8 = 0; c8 < NH; c8 += 8) {
+    uint32_t o[8];
+    tmem_ld8(t_o + c8, o);
+    tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += f[e];
+    for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * s.alpha[c0 + c8 + e]);
+    tmem_st8(t_o + c8, o);
+  }
+  tmem_wait_st();
 #pragma unroll
-        for (int o = VPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (v == 0) {
-          s.sq[r] = sum;
-          s.m[r] = r < rows ? -INFINITY : 0.f;
-        }
-        // dims 0, 4, 1, 5 and 2, 6, 3, 7 of the eight
-        const uint2 a = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
-        const uint2 c = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int g = 2 * wd + half, chunk = 2 * (g & 3) + (t >> 1);
-          *reinterpret_cast<uint2*>(smem + LY::kSmemQ + (g >> 2) * LY::kRegionQ + swz(r, chunk) + 8 * (t & 1)) = half ? c : a;
-        }
-      }
-    }
-    const bool tail = (t0 + n) * kTile > L;
-    if (tail) {  // which columns see which tree token: 32 x 32 bits a warp, turned by votes
-      const int ch = warp & 1, wd = warp >> 1, r = ch * 32 + lane;
-      uint32_t bits = 0u;
-      if (r < rows && wd < p.words) {
-        bits = __ldg(p.anc + ((size_t)b * p.Ncap + (grow0 + r) / p.G) * p.words + wd);
-        const int last = N - wd * 32;
-        bits = last >= 32 ? bits : last > 0 ? bits & ((1u << last) - 1u) : 0u;
-      }
-      uint32_t mine = 0u;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        const uint32_t v = __ballot_sync(0xffffffffu, (bits >> j) & 1u);
-        if (lane == j) mine = v;
-      }
-      s.vis[ch][wd * 32 + lane] = mine;
-    }
-    fence_proxy_async();
-    named_sync(3, kSoftThreads);
-    if (tid == 0) mbar_arrive(&s.bar_q);
-
-    unsigned long long l[16], z[16];
-#pragma unroll
-    for (int c = 0; c < 16; ++c) l[c] = z[c] = 0ull;
-    const uint32_t full = nh == 32 ? 0xffffffffu : (1u << nh) - 1u;
-#pragma unroll 1
-    for (int i = 0; i < n; ++i, ++it) {
-      // this tile's pairs; the next one's are on their way meanwhile
-      const bool live = nlive;
-      const float st_k = q4_step(nkr), lo_k = q4_low(nkr), st_v = q4_step(nvr), lo_v = q4_low(nvr);
-      const float ks = live ? sc * st_k : 0.f, kl = live ? sc * fmaf(-16.f, st_k, lo_k) : 0.f;
-      const float vs = live ? st_v : 0.f, vl = live ? fmaf(8.f, st_v, lo_v) : 0.f;
-      load_pair();
-      load_page();
-      const int pos = (t0 + i) * kTile + posl;
-      uint32_t vm = live ? full : 0u;
-      if (tail && live && pos >= L) {
-        const int j = pos - L;
-        const unsigned long long v = (unsigned long long)s.vis[0][j] | ((unsigned long long)s.vis[1][j] << 32);
-        vm = (uint32_t)(v >> c0) & full;
-      }
-      const bool plain = __all_sync(0xffffffffu, vm == full);
-      if (ok) {
-        ok = mbar_wait(&s.bar_s[it & 1], (uint32_t)(it >> 1) & 1u);
-        if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, b);
-      }
-      const uint32_t ts = tmem + kTmemS + (it & 1) * 64 + c0 + tl_sel;
-      float pr[32];
-      auto read_scores = [&] {
-        tc_fence_after();
-#pragma unroll
-        for (int c8 = 0; c8 < 4; ++c8) {
-          if (c8 * 8 >= nh) break;
-          tmem_ld8(ts + c8 * 8, reinterpret_cast<uint32_t*>(pr) + c8 * 8);
-        }
-        tmem_wait_ld_regs(reinterpret_cast<uint32_t(&)[32]>(pr));
-      };
-#pragma unroll
-      for (int c = 0; c < 32; ++c) pr[c] = 0.f;
-      if (ok) {
-        read_scores();
-        if (plain) weights<false>(pr, s, c0, nh, ks, kl, vm);
-        else weights<true>(pr, s, c0, nh, ks, kl, vm);
-      }
-      float top = pr[0];
-#pragma unroll
-      for (int c = 1; c < 31; c += 2) top = fmaxf(top, fmaxf(pr[c], pr[c + 1]));
-      top = fmaxf(top, pr[31]);
-      if (named_or(wg_bar, 128, ok && top >= kFar)) {
-        // a column without a reference yet, or a weight far above it: the tile's maxima decide (all four warps of the columns)
-        float alpha_m[1];
-        (void)alpha_m;
-        if (ok) read_scores();
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          if (c < nh) {
-            float x = ok && ((vm >> c) & 1u) ? fmaf(ks, pr[c], kl * s.sq[c0 + c]) : -INFINITY;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-            if (lane == 0) s.colmax[warp][c] = x;
-          }
-        }
-        if (ok && i > 0) {  // O^T has to be at rest
-          ok = mbar_wait(&s.bar_o[(it - 1) & 1], (uint32_t)((it - 1) >> 1) & 1u);
-          if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, b);
-        }
-        named_sync(wg_bar, 128);
-        auto moved = [&](int c, float& m_new) {  // the factor for what column c has gathered
-          const float m_old = s.m[c0 + c];
-          const float mx = fmaxf(fmaxf(s.colmax[cg * 4][c], s.colmax[cg * 4 + 1][c]), fmaxf(s.colmax[cg * 4 + 2][c], s.colmax[cg * 4 + 3][c]));
-          m_new = m_old == -INFINITY || mx >= m_old + 59.f ? mx : m_old;
-          return m_old == -INFINITY || m_new == m_old ? 1.f : exp2f(m_old - m_new);
-        };
-        if (ok) tc_fence_after();
-#pragma unroll
-        for (int c8 = 0; c8 < 4; ++c8) {
-          if (c8 * 8 >= nh) break;
-          uint32_t o[8];
-          const bool scale_o = ok && i > 0;
-          if (scale_o) {
-            tmem_ld8(tmem + kTmemO + c0 + c8 * 8 + tl_sel, o);
-            tmem_wait_ld();
-          }
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const int c = c8 * 8 + e;
-            float m0, m1;
-            const float a0 = moved(c, m0), a1 = moved(c + 1, m1);
-            const unsigned long long a2 = pack_f2(a0, a1);
-            l[c / 2] = mul_f2(l[c / 2], a2);
-            z[c / 2] = mul_f2(z[c / 2], a2);
-            if (scale_o) {
-              o[e] = __float_as_uint(__uint_as_float(o[e]) * a0);
-              o[e + 1] = __float_as_uint(__uint_as_float(o[e + 1]) * a1);
-            }
-          }
-          if (scale_o) tmem_st8(tmem + kTmemO + c0 + c8 * 8 + tl_sel, o);
-        }
-        if (ok) tmem_wait_st();
-        float m_mine = 0.f;
-        const int c_mine = tid & 127;
-        if (c_mine < nh) moved(c_mine, m_mine);
-        named_sync(wg_bar, 128);
-        if (c_mine < nh) s.m[c0 + c_mine] = m_mine;
-        named_sync(wg_bar, 128);
-        if (ok) {
-          read_scores();
-          weights<true>(pr, s, c0, nh, ks, kl, vm);
-        }
-      }
-      if (ok && it >= 2) {  // the weights of tile it - 2 have been read
-        ok = mbar_wait(&s.bar_o[it & 1], (uint32_t)((it >> 1) - 1) & 1u);
-        if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, b);
-      }
-      if (ok) {
-        unsigned char* row = smem + LY::kSmemP + (it & 1) * LY::kBufP + posl * 128;
-        if (plain) hand_over<false>(pr, l, z, row, posl & 7, c0 >> 3, nh, vs, vl, vm);
-        else hand_over<true>(pr, l, z, row, posl & 7, c0 >> 3, nh, vs, vl, vm);
-        fence_proxy_async();
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.bar_p[it & 1]);
-    }
-
-    // ---- the item's end: sums over the lanes, then over the warps of a column
-    if (ok) {
-      ok = mbar_wait(&s.bar_o[(it - 1) & 1], (uint32_t)((it - 1) >> 1) & 1u);
-      if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, b);
-    }
-    {
-      float v[32];
-#pragma unroll
-      for (int c = 0; c < 16; ++c) unpack_f2(l[c], v[2 * c], v[2 * c + 1]);
-      const float suml = reduce_columns(v);
-#pragma unroll
-      for (int c = 0; c < 16; ++c) unpack_f2(z[c], v[2 * c], v[2 * c + 1]);
-      const float sumz = reduce_columns(v);
-      if (lane < nh) {
-        s.red_l[warp & 3][c0 + lane] = suml;
-        s.red_z[warp & 3][c0 + lane] = sumz;
-      }
-    }
-    named_sync(wg_bar, 128);
-    if ((tid & 127) < nh) {
-      const int c = c0 + (tid & 127);
-      s.tot_l[c] = s.red_l[0][c] + s.red_l[1][c] + s.red_l[2][c] + s.red_l[3][c];
-      s.tot_z[c] = s.red_z[0][c] + s.red_z[1][c] + s.red_z[2][c] + s.red_z[3][c];
-    }
-    named_sync(wg_bar, 128);
-    const bool whole = n == tl;
-    // lane m of O^T: dims in the order of merge_item
-    const int ch = posl >> 3, j8 = posl & 7;
-    const int dim = (HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch) + ((j8 >> 1) | ((j8 & 1) << 2));
-    const int slot = (int)blockIdx.x * 2 + (s.bound[blockIdx.x] > s.pre[b] + (long long)w.hr * tl ? 0 : 1);
-    if (ok) {
-      tc_fence_after();
-#pragma unroll 1
-      for (int c8 = 0; c8 * 8 < nh; ++c8) {
-        uint32_t o[8];
-        tmem_ld8(tmem + kTmemO + c0 + c8 * 8 + tl_sel, o);
-        tmem_wait_ld();
-        if (HD == 64 && posl >= 64) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = c0 + c8 * 8 + e;
-          const float x = __uint_as_float(o[e]) + s.tot_z[c];
-          if (c >= rows) continue;
-          if (whole) {
-            const float lt = s.tot_l[c];
-            const int grow = grow0 + c, t = grow / p.G;
-            p.out[(((size_t)b * p.Ncap + t) * p.Hq + h * p.G + (grow - t * p.G)) * HD + dim] =
-                __float2bfloat16_rn(x * (lt == 0.f ? 0.f : 1.f / lt));
-          } else {
-            __stcg(p.part_o + ((size_t)slot * kRows + c) * HD + posl, x);
-          }
-        }
-      }
-    }
-    tc_fence_before();
-    if (!whole) {
-      if ((tid & 127) < nh) {
-        const int c = c0 + (tid & 127);
-        __stcg(p.part_ml + (size_t)slot * kRows + c, ok ? make_float2(s.m[c], s.tot_l[c]) : make_float2(-INFINITY, 0.f));
-      }
-      // the CTAs that share the item
-      const long long first = s.pre[b] + (long long)w.hr * tl, end = first + tl;
-      int c_lo = blockIdx.x, c_hi = blockIdx.x;
-      while (s.bound[c_lo] > first) --c_lo;
-      while (s.bound[c_hi + 1] < end) ++c_hi;
-      named_sync(3, kSoftThreads);
-      if (tid == 0) {
-        int parts = 0;
-        for (int c = c_lo; c <= c_hi; ++c) parts += s.bound[c + 1] > s.bound[c];
-        // releases this CTA's partial (the barrier made it this thread's to release), acquires those that came earlier
-        int32_t* cnt = p.ticket + ((size_t)b * p.Hkv + h) * p.nrb + rb;
-        int t;
-        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(t) : "l"(cnt) : "memory");
-        s.last = t == parts - 1;
-        if (t == parts - 1) *cnt = 0;  // ready for the next launch
-      }
-      named_sync(3, kSoftThreads);
-      if (s.last) merge_item<HD>(p, s, b, h, grow0, rows, c_lo, c_hi, first);
-    }
-    for (int i = 0; i < n; ++i) advance(w, s, p);
+  for (int c = 0; c < NH; ++c) {
+    l[c] *= s.alpha[c0 + c];
+    z[c] *= s.alpha[c0 + c];
   }
 }
 
-template <int HD>
-__global__ void __launch_bounds__(kThreadsQ4, 1) tree_attn_q4_kernel(const Q4Params p) {
+template <int HD, bool kPaged>
+__global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Params p) {
   extern __shared__ __align__(1024) unsigned char smem[];
   using LY = Lay<HD>;
+  constexpr int W = LY::kW;
   Misc& s = *reinterpret_cast<Misc*>(smem + LY::kSmemMisc);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // Everything, tensor memory included, behind the wait; the warp that allocates releases the dependents after it has.
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (warp == kWarpMma) {
+  if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "n"(kTmemCols));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (lane == 0) {
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&s.bar_ka[i], 4);
-        mbar_init(&s.bar_s[i], 1);
-        mbar_init(&s.bar_v[i], 4);
-        mbar_init(&s.bar_p[i], 8);
-        mbar_init(&s.bar_o[i], 1);
-      }
-      mbar_init(&s.bar_q, 1);
+      mbar_init(&s.bar_s, 1);
+      mbar_init(&s.bar_o, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       fence_proxy_async();
     }
@@ -785,14 +445,14 @@ __global__ void __launch_bounds__(kThreadsQ4, 1) tree_attn_q4_kernel(const Q4Par
       if (over && N > F && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
       const int total = (int)(over ? max_pos : (long long)L + N);
       const int nr = ((N - F) * p.G + kRows - 1) / kRows, tl = nr > 0 ? (total + kTile - 1) / kTile : 0;
-      long long mine = (long long)p.Hkv * nr * tl, upto = mine;
-      int cnt = p.Hkv * nr;
+      const long long mine = (long long)p.Hkv * nr * tl;
+      long long upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const long long x = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += x;
       }
-      items += __reduce_add_sync(0xffffffffu, cnt);
+      items += __reduce_add_sync(0xffffffffu, p.Hkv * nr);
       s.pre[b] = run + upto - mine;
       run += __shfl_sync(0xffffffffu, upto, 31);
       s.L[b] = L; s.N[b] = N; s.F[b] = F; s.tl[b] = tl; s.nr[b] = nr; s.total[b] = total;
@@ -802,56 +462,396 @@ __global__ void __launch_bounds__(kThreadsQ4, 1) tree_attn_q4_kernel(const Q4Par
       // pieces of two tiles at least, and no item over more CTAs than a merge is worth
       long long workers = (run + 1) / 2;
       workers = workers < (long long)items * kMaxJoin ? workers : (long long)items * kMaxJoin;
-      s.workers = (int)(workers < (long long)gridDim.x ? workers : (long long)gridDim.x);
+      workers = workers < (long long)gridDim.x ? workers : (long long)gridDim.x;
+      s.workers = (int)workers;
+      s.piece = workers > 0 ? run / workers : 0;
+      s.rest = workers > 0 ? (int)(run - s.piece * workers) : 0;
     }
   }
   __syncthreads();
   // where the pieces begin
-  if (tid <= (int)gridDim.x) {
-    const long long T = s.pre[CAST_MAX_BATCH];
-    long long x = tid >= s.workers ? T : T * tid / s.workers;
-    s.bound[tid] = x;
-    if (tid == (int)blockIdx.x && x < T) {
+  for (int c = tid; c <= (int)gridDim.x; c += kThreadsQ4) {
+    const long long T = s.pre[CAST_MAX_BATCH], x = c >= s.workers ? T : s.piece * c + min(c, s.rest);
+    s.bound[c] = x;
+    if (c == (int)blockIdx.x && x < T) {
       int b = 0;
       while (s.pre[b + 1] <= x) ++b;
       const long long in = x - s.pre[b];
-      s.b0 = b;
-      s.hr0 = (int)(in / s.tl[b]);
-      s.t0 = (int)(in - (long long)s.hr0 * s.tl[b]);
+      const int hr = in <= 0x7fffffffll ? (int)((uint32_t)in / (uint32_t)s.tl[b]) : (int)(in / s.tl[b]);
+      s.seg.b = b;
+      s.seg.h = hr / s.nr[b];
+      s.seg.rb = hr - s.seg.h * s.nr[b];
+      s.seg.t = (int)(in - (long long)hr * s.tl[b]);
     }
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = s.tmem;
-  Walk w;
-  w.left = (int)(s.bound[blockIdx.x + 1] - s.bound[blockIdx.x]);
-  w.b = s.b0; w.hr = s.hr0; w.t = s.t0;
+  auto look_ahead = [&](int i) {  // (thread 0) tile i into `step`
+    Walk w = s.ahead;
+    s.step[i & 7] = make_int4(w.b, w.h, w.t * kTile, s.total[w.b]);
+    advance(w, s, p);
+    s.ahead = w;
+  };
   const bool aligned = (smem_u32(smem) & 1023u) == 0u;  // the swizzled operand regions need a 1 KB aligned base
-  if (!aligned && tid == 0) report(p.st, CAST_ERR_CUDA, 1024);
-  if (w.left > 0 && aligned) {
-    if (warp < kWarpK) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
-      softmax<HD>(p, s, smem, w, tmem);
-    } else if (warp < kWarpMma) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsProduce));
-      if (warp < kWarpV) produce<HD, false>(p, s, smem, w, tmem);
-      else produce<HD, true>(p, s, smem, w, tmem);
-    } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
-      if (warp == kWarpMma) issue<HD>(p, s, smem, w, tmem);
-    }
+  __syncthreads();
+  if (tid == 0) {
+    if (!aligned) report(p.st, CAST_ERR_CUDA, 1024);
+    s.seg.left = aligned ? (int)(s.bound[blockIdx.x + 1] - s.bound[blockIdx.x]) : 0;
+    s.ahead = s.seg;
+    if (s.seg.left > 0)
+      for (int i = 0; i < 4; ++i) look_ahead(i);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == kWarpMma)
+  const uint32_t tmem = __reduce_or_sync(0xffffffffu, s.tmem);
+
+  const int part = warp & 3, cg = warp >> 2, wg_bar = 1 + cg;     // lanes of tensor memory, half of the columns
+  const int posl = part * 32 + lane;                              // this thread's position in a tile
+  const int r = lane >> 2, tq = lane & 3, row16 = part * 32 + cg * 16 + r;  // its quad's rows of the codes: row16 and row16 + 8
+  const uint32_t t_part = (uint32_t)(part * 32) << 16;
+
+  // ---- codes and pairs, a tile ahead. Every lane finds the place of its position's row; a quad of lanes loads a row of codes.
+  uint32_t kc[2][W], vc[2][W], nkr = 0, nvr = 0;
+  // Of the tile whose K codes are in kc, and of that in vc: this thread's position has a row. (The codes of one without may be
+  // anything: they are finite, and weigh nothing.)
+  bool live_k = false, live_v = false;
+  int page = 0;
+  uint32_t row = 0;                // of the tile in kc
+  auto next_page = [&](int i) {
+    const int4 e = s.step[i & 7];
+    page = request_page<kPaged>(p, e.x, e.z + posl, e.w);
+  };
+  auto next_row = [&](int i) {
+    const int4 e = s.step[i & 7];
+    row = row_of<kPaged>(p, page, e.y, e.z + posl, e.w);
+    const bool fine = page_ok<kPaged>(p, page);
+    if (kPaged && !fine && e.z + posl < e.w) report(p.st, CAST_ERR_BAD_PAGE, e.x);
+    live_k = fine && e.z + posl < e.w;
+  };
+  auto request = [&](const unsigned char* codes, uint32_t (&c)[2][W]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const unsigned char* at = codes + (size_t)__shfl_sync(0xffffffffu, row, cg * 16 + 8 * j + r) * (HD / 2) + tq * (4 * W);
+      ld_here(c[j], at);
+    }
+  };
+  // K codes of tile i (in kc) to tensor memory, the next tile's requested
+  auto store_k = [&](int i_tile, bool ok) {
+    if (ok) {
+      uint32_t out[8 * W];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < W; ++i) {  // word i's pairs 0, 1 go to the group of 16 dims 2 i, pairs 2, 3 to 2 i + 1
+          const uint32_t c = kc[j][i];
+          out[8 * i + 2 * j] = pair_plus16<0>(c);
+          out[8 * i + 2 * j + 1] = pair_plus16<1>(c);
+          out[8 * i + 4 + 2 * j] = pair_plus16<2>(c);
+          out[8 * i + 4 + 2 * j + 1] = pair_plus16<3>(c);
+        }
+      tmem_st_quads<2 * W>(tmem + kTmemK + ((uint32_t)(part * 32 + cg * 16) << 16), out);
+    }
+    next_row(i_tile + 1);
+    request(p.kc, kc);
+    next_page(i_tile + 2);
+    if (ok) tmem_wait_st();
+  };
+  unsigned char* const v_row = smem + LY::kSmemV + row16 * 128;
+  const int chunk[2] = {((2 * tq) ^ r) << 4, ((2 * tq + 1) ^ r) << 4};
+  // V codes of the tile in vc to shared memory; the tile behind it (whose row is `row`) requested
+  auto store_v = [&](int buf, bool ok) {
+    if (ok) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const uint32_t c = vc[j][i];
+          *reinterpret_cast<uint4*>(v_row + buf * LY::kBufV + (W == 4 ? i >> 1 : 0) * LY::kRegionV + j * 1024 + chunk[i & 1]) =
+              make_uint4(pair_minus8<0>(c), pair_minus8<1>(c), pair_minus8<2>(c), pair_minus8<3>(c));
+        }
+    }
+    request(p.vc, vc);
+  };
+  auto request_pair = [&] {
+    nkr = ld_here(reinterpret_cast<const int32_t*>(p.kr) + row);
+    nvr = ld_here(reinterpret_cast<const int32_t*>(p.vr) + row);
+  };
+  if (s.seg.left > 0) {
+    next_page(0);
+    next_row(0);
+    next_page(1);
+    request(p.kc, kc);
+    request(p.vc, vc);
+    request_pair();
+    live_v = live_k;
+  }
+
+  // ---- the products: one warp, converged
+  auto issue_s = [&](uint32_t shape) {
+    const uint64_t dq = umma_desc(smem_u32(smem + LY::kSmemQ), 16, 1024);
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k)
+      umma_bf16_ts(tmem + kTmemS, tmem + kTmemK + k * 8, dq + (uint64_t)((k >> 2) * (LY::kRegionQ >> 4) + (k & 3) * 2), shape, k > 0);
+    umma_commit(&s.bar_s);
+  };
+  auto issue_o = [&](uint32_t shape, int buf, bool first) {
+    // both operands are MN-major; 64 dims: both halves of M alike
+    const uint64_t dv = umma_desc(smem_u32(smem + LY::kSmemV + buf * LY::kBufV), HD == 128 ? LY::kRegionV : 0, 1024);
+    const uint64_t dp = umma_desc(smem_u32(smem + LY::kSmemP), 0, 1024);
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+      umma_bf16(tmem + kTmemO, dv + (uint64_t)(k * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), shape | (1u << 15) | (1u << 16),
+                !first || k > 0 ? 1u : 0u);
+    umma_commit(&s.bar_o);
+  };
+
+  int it = 0;
+  bool ok = true;
+  // One item, or what this CTA has of it; NH columns to a thread.
+  auto work = [&](auto nh_c) {
+    constexpr int NH = decltype(nh_c)::value;
+    const int t0 = s.seg.t, n = min(s.seg.left, s.tl[s.seg.b] - t0), L = s.L[s.seg.b];
+    const int rows_all = (s.N[s.seg.b] - s.F[s.seg.b]) * p.G - s.seg.rb * kRows, c0 = cg * NH;
+    constexpr uint32_t shape = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NH >> 2) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    // ---- the query rows, their dims in the order of the codes in tensor memory; their sums
+    if (tid < kRows) {
+      const int b = s.seg.b, grow = s.F[b] * p.G + s.seg.rb * kRows + tid, tok = grow / p.G;
+      s.at[tid] = (uint32_t)(((b * p.Ncap + tok) * p.Hq + s.seg.h * p.G + (grow - tok * p.G)) * HD);
+      s.nm[tid] = tid < rows_all ? INFINITY : 0.f;
+    }
+    __syncthreads();
+    {
+      constexpr int VPR = HD / 8, STEPS = kRows * VPR / kThreadsQ4;
+      static_assert(kRows * VPR % kThreadsQ4 == 0 || HD == 64, "whole steps");
+      uint4 x[STEPS + (HD == 64 ? 1 : 0)];
+#pragma unroll
+      for (int k = 0; k * kThreadsQ4 < kRows * VPR; ++k) {
+        const int i = tid + k * kThreadsQ4, qr = i / VPR, v = i % VPR;
+        x[k] = qr < min(rows_all, kRows) ? __ldg(reinterpret_cast<const uint4*>(p.q + s.at[qr] + v * 8)) : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k * kThreadsQ4 < kRows * VPR; ++k) {
+        const int i = tid + k * kThreadsQ4, qr = i / VPR, v = i % VPR, t = v / W, wd = v % W;
+        if (qr >= kRows) break;  // (whole warps: half of the last step at 64 dims)
+        float f[8], sum = 0.f;
+        Vec<__nv_bfloat16>::unpack(x[k], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += f[e];
+#pragma unroll
+        for (int o = VPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (v == 0) s.sq[qr] = sum;
+        // dims 0, 4, 1, 5 and 2, 6, 3, 7 of the eight
+        const uint2 lo = make_uint2(__byte_perm(x[k].x, x[k].z, 0x5410), __byte_perm(x[k].x, x[k].z, 0x7632));
+        const uint2 hi = make_uint2(__byte_perm(x[k].y, x[k].w, 0x5410), __byte_perm(x[k].y, x[k].w, 0x7632));
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int g = 2 * wd + half, ch = 2 * (g & 3) + (t >> 1);
+          *reinterpret_cast<uint2*>(smem + LY::kSmemQ + (g >> 2) * LY::kRegionQ + swz(qr, ch) + 8 * (t & 1)) = half ? hi : lo;
+        }
+      }
+    }
+    const bool tail = (t0 + n) * kTile > L;
+    if (tail) {  // which columns see which tree token: 32 x 32 bits a warp, turned by votes
+      const int b = s.seg.b, N = s.N[b], grow0 = s.F[b] * p.G + s.seg.rb * kRows, rows = min(rows_all, kRows);
+      const int ch = warp & 1, wd = warp >> 1, qr = ch * 32 + lane;
+      uint32_t bits = 0u;
+      if (qr < rows && wd < p.words) {
+        bits = __ldg(p.anc + ((size_t)b * p.Ncap + (grow0 + qr) / p.G) * p.words + wd);
+        const int last = N - wd * 32;
+        bits = last >= 32 ? bits : last > 0 ? bits & ((1u << last) - 1u) : 0u;
+      }
+      uint32_t mine = 0u;
+#pragma unroll 8
+      for (int j = 0; j < 32; ++j) {
+        const uint32_t v = __ballot_sync(0xffffffffu, (bits >> j) & 1u);
+        if (lane == j) mine = v;
+      }
+      s.vis[ch][wd * 32 + lane] = mine;
+    }
+    store_k(it, ok);
+    fence_proxy_async();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0 && ok) {
+      tc_fence_after();
+      issue_s(shape);
+    }
+
+    float l[NH], z[NH];
+#pragma unroll
+    for (int c = 0; c < NH; ++c) l[c] = z[c] = 0.f;
+    constexpr uint32_t full = (1u << NH) - 1u;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i, ++it) {
+      const uint32_t phase = (uint32_t)it & 1u;
+      // this tile's pair and rows without a place (those of `row` are the next tile's by now)
+      const float st_k = q4_step(nkr), st_v = q4_step(nvr);
+      const bool live = live_v;
+      const float ks = live ? p.scale_log2 * st_k : 0.f, kl = live ? p.scale_log2 * fmaf(-16.f, st_k, q4_low(nkr)) : 0.f;
+      const float vs = live ? st_v : 0.f, vl = live ? fmaf(8.f, st_v, q4_low(nvr)) : 0.f;
+      request_pair();
+      // ---- V codes: the buffer's last reader was O^T of tile it - 2, awaited with tile it - 1
+      store_v(it & 1, ok);
+      live_v = live_k;
+      uint32_t vm = live ? full : 0u;
+      if (tail) {
+        const int j = (t0 + i) * kTile + posl - L;
+        if (j >= 0 && live) vm = (uint32_t)(((unsigned long long)s.vis[0][j] | ((unsigned long long)s.vis[1][j] << 32)) >> c0) & full;
+      }
+      const bool plain = __all_sync(0xffffffffu, vm == full);
+      // ---- the scores, and the place of the weights (O^T of the tile before has read its own)
+      if (ok) {
+        ok = mbar_wait(&s.bar_s, phase) && (it == 0 || mbar_wait(&s.bar_o, phase ^ 1u));
+        if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, s.seg.b);
+      }
+      float pr[NH];
+      tc_fence_after();
+      const uint32_t t_s = tmem + kTmemS + c0 + t_part;
+      auto to_weights = [&] {
+        if (plain) weights<NH, false>(pr, s.sq + c0, s.nm + c0, ks, kl, vm);
+        else weights<NH, true>(pr, s.sq + c0, s.nm + c0, ks, kl, vm);
+      };
+      bool far = false;
+      if (ok) {
+        read_scores<NH>(t_s, pr);
+        if (i > 0) {
+          to_weights();
+          float top = 0.f;
+#pragma unroll
+          for (int c = 0; c < NH; c += 2) top = max3(top, pr[c], pr[c + 1]);
+          far = top >= kFar;
+        }
+      }
+      // The first tile, a column without a reference yet, or a weight far above it: the tile's maxima decide, in all four warps
+      // of the columns. (O^T is at rest.)
+      if (i == 0 || named_or(wg_bar, 128, !ok || far)) {
+        if (named_or(wg_bar, 128, !ok)) ok = false;
+        if (ok) {
+          if (i > 0) read_scores<NH>(t_s, pr);
+          move_references<NH>(s, pr, cg, c0, wg_bar, i == 0, tmem + kTmemO + c0 + t_part, ks, kl, vm, l, z);
+          to_weights();
+        }
+      }
+      if (ok) {
+        unsigned char* p_row = smem + LY::kSmemP + posl * 128;
+        if (plain) hand_over<NH, false>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl, vm);
+        else hand_over<NH, true>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl, vm);
+      }
+      if (i + 1 < n) store_k(it + 1, ok);  // (S^T of this tile has read the codes before)
+      if (tid == 0) look_ahead(it + 4);
+      fence_proxy_async();
+      tc_fence_before();
+      if (__syncthreads_or(!ok)) ok = false;
+      if (warp == __reduce_max_sync(0xffffffffu, it & 7) && ok) {  // in turn: sixteen instructions and their descriptors are a lot for one warp
+        tc_fence_after();
+        if (i + 1 < n) issue_s(shape);
+        issue_o(shape, it & 1, i == 0);
+      }
+    }
+
+    // ---- the item's end: sums over the lanes, then over the warps of a column
+    {
+      float v[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) v[c] = c < NH ? l[c < NH ? c : 0] : 0.f;
+      const float suml = reduce_columns<false>(v);
+#pragma unroll
+      for (int c = 0; c < 32; ++c) v[c] = c < NH ? z[c < NH ? c : 0] : 0.f;
+      const float sumz = reduce_columns<false>(v);
+      if (lane < NH) {
+        s.red_l[part][c0 + lane] = suml;
+        s.red_z[part][c0 + lane] = sumz;
+      }
+    }
+    if (ok) {
+      ok = mbar_wait(&s.bar_o, (uint32_t)(it - 1) & 1u);
+      if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, s.seg.b);
+    }
+    named_sync(wg_bar, 128);
+    if ((tid & 127) < NH) {
+      const int c = c0 + (tid & 127);
+      const float lt = s.red_l[0][c] + s.red_l[1][c] + s.red_l[2][c] + s.red_l[3][c];
+      s.tot_l[c] = n < s.tl[s.seg.b] ? lt : lt == 0.f ? 0.f : 1.f / lt;  // a whole item: its reciprocal
+      s.tot_z[c] = s.red_z[0][c] + s.red_z[1][c] + s.red_z[2][c] + s.red_z[3][c];
+    }
+    named_sync(wg_bar, 128);
+    const int b = s.seg.b, h = s.seg.h, rb = s.seg.rb, tl = s.tl[b], rows = min(rows_all, kRows);
+    const bool whole = n == tl;
+    const long long first = s.pre[b] + (long long)(h * s.nr[b] + rb) * tl;  // the item's first tile
+    // lane m of O^T: dims in the order of merge_item
+    const int ch = posl >> 3, j8 = posl & 7;
+    const int dim = (HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch) + ((j8 >> 1) | ((j8 & 1) << 2));
+    const int slot = (int)blockIdx.x * 2 + (s.bound[blockIdx.x] > first ? 0 : 1);
+    if (ok) {
+      tc_fence_after();
+#pragma unroll 1
+      for (int c8 = 0; c8 < NH; c8 += 8) {
+        uint32_t o[8];
+        tmem_ld8(tmem + kTmemO + c0 + c8 + t_part, o);
+        tmem_wait_ld();
+        if (HD == 64 && posl >= 64) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = c0 + c8 + e;
+          const float x = __uint_as_float(o[e]) + s.tot_z[c];
+          if (c >= rows) continue;
+          if (whole) {
+            p.out[s.at[c] + dim] = __float2bfloat16_rn(x * s.tot_l[c]);
+          } else {
+            __stcg(p.part_o + ((size_t)slot * kRows + c) * HD + posl, x);
+          }
+        }
+      }
+    }
+    tc_fence_before();
+    if (!whole) {
+      if ((tid & 127) < NH) {
+        const int c = c0 + (tid & 127);
+        __stcg(p.part_ml + (size_t)slot * kRows + c, ok ? make_float2(-s.nm[c], s.tot_l[c]) : make_float2(-INFINITY, 0.f));
+      }
+      // the CTAs that share the item
+      const long long end = first + tl;
+      int c_lo = blockIdx.x, c_hi = blockIdx.x;
+      while (s.bound[c_lo] > first) --c_lo;
+      while (s.bound[c_hi + 1] < end) ++c_hi;
+      __syncthreads();
+      if (tid == 0) {
+        int parts = 0;
+        for (int c = c_lo; c <= c_hi; ++c) parts += s.bound[c + 1] > s.bound[c];
+        // releases this CTA's partial (the barrier made it this thread's to release), acquires those that came earlier
+        int32_t* cnt = p.ticket + ((size_t)b * p.Hkv + h) * p.nrb + rb;
+        int t;
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(t) : "l"(cnt) : "memory");
+        s.last = t == parts - 1;
+        if (t == parts - 1) *cnt = 0;  // ready for the next launch
+      }
+      __syncthreads();
+      if (s.last) merge_item<HD>(p, s, rows, c_lo, c_hi, first);
+    }
+    __syncthreads();  // (all are done with the item's arrays)
+    if (tid == 0) {
+      Walk w = s.seg;
+      w.t += n - 1;
+      w.left -= n - 1;
+      advance(w, s, p);
+      s.seg = w;
+    }
+    __syncthreads();
+  };
+#pragma unroll 1
+  while (s.seg.left > 0) {  // up to 16 query rows, or up to 48: with the count known the columns' arithmetic is one straight block
+    if ((s.N[s.seg.b] - s.F[s.seg.b]) * p.G - s.seg.rb * kRows <= 16) work(Count<8>());
+    else work(Count<kHalf>());
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemCols));
 }
 
 constexpr size_t kPartBytes = (size_t)2 * kRows * (128 * sizeof(float) + sizeof(float2));  // per CTA
 
-int q4_grid(const cast_ctx* c) { return c->num_sms < kMaxGrid ? c->num_sms : kMaxGrid; }
+int q4_grid(const cast_ctx* c) { return 2 * c->num_sms < kMaxGrid ? 2 * c->num_sms : kMaxGrid; }
 int q4_row_blocks(const cast_ctx* c, int Hq, int Hkv) { return (c->cfg.total_token * (Hq / Hkv) + kRows - 1) / kRows; }
 
 }  // namespace
@@ -868,6 +868,9 @@ cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_c
                                      const uint32_t* anc, const int32_t* n_tree, const int32_t* first_row, float scale, void* out,
                                      cudaStream_t stream) {
   const int grid = q4_grid(c);
+  // rows of the cache and elements of q are counted in 32 bits: more would not fit the device's memory
+  if ((long long)B * c->cfg.max_tree * Hq * D > 0xffffffffll) return CAST_ERR_CAPACITY;
+  if ((long long)(g.page_size > 0 ? g.num_pages : B) * Hkv * (g.page_size > 0 ? g.page_size : g.seq_capacity) > 0xffffffffll) return CAST_ERR_CAPACITY;
   Q4Params p;
   p.nrb = q4_row_blocks(c, Hq, Hkv);
   // compute calls never allocate: the workspace comes from cast_reserve_attention_q4
@@ -888,9 +891,11 @@ cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_c
   p.part_ml = (float2*)(p.part_o + (size_t)grid * 2 * kRows * 128);
   p.ticket = (int32_t*)((char*)c->q4_ws + grid * kPartBytes);
   p.st = c->state;
-  auto* const kern = D == 64 ? tree_attn_q4_kernel<64> : tree_attn_q4_kernel<128>;
+  auto* const kern = D == 64 ? (g.page_size > 0 ? tree_attn_q4_kernel<64, true> : tree_attn_q4_kernel<64, false>)
+                             : (g.page_size > 0 ? tree_attn_q4_kernel<128, true> : tree_attn_q4_kernel<128, false>);
   const int smem = (D == 64 ? Lay<64>::kSmemMisc : Lay<128>::kSmemMisc) + (int)sizeof(Misc);
   CAST_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  CAST_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, 100));  // two CTAs per SM
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
   cfg.blockDim = dim3(kThreadsQ4, 1, 1);
