@@ -3,12 +3,17 @@
 //   mass[p] += sum_r e^(s_r(p) - m_r) / l_r,   s_r(p) = scale q_r . k_p,   l_r = sum_p e^(s_r(p) - m_r)
 //
 // over the rows r = (accepted token, head of the group) of a kv-head. The weights need every row's sum first, so the keys are
-// read twice: mass_kernel<.., 1> forms each row's (max, sum) over a piece of the sequence, mass_kernel<.., 2> merges the pieces'
-// pairs, forms the scores again and adds the weights of a position over the rows in their order. A position's sum belongs to one
-// thread group of one CTA: no atomics, the same bits every time.
+// read twice: pass 1 forms each row's (reference, sum) over a piece of the sequence, pass 2 merges the pieces' pairs, forms the
+// scores again and adds the weights of a position over the rows in their order. A position's sum belongs to one thread: no
+// atomics, the same bits every time.
+//
+// bf16 queries: mass_tc_kernel. As in the attention over 4-bit caches positions are the rows of the product and queries its columns,
+// S^T = K Q^T (128 positions x up to 32 queries): a thread owns a position, the sum over the rows is its own, and in pass 2 nothing
+// crosses lanes. 4-bit keys go through registers to tensor memory as exact small integers (c - 8), 16-bit ones by asynchronous copies to
+// shared memory. Four warps a CTA, three or four CTAs per SM to run under each other's waits. fp32 queries: mass_kernel on the CUDA cores.
 #include <math.h>
 
-#include "kv_q4.h"
+#include "q4_tc.h"
 
 using namespace cast;
 
@@ -26,10 +31,11 @@ struct MassParams {
   size_t q_stride, k_stride, range_stride;  // bytes per layer
   int B, Ncap, Hq, Hkv, G, max_rows, nsplit, path_stride;
   Paging g;
+  FastPaging fg;
   const int32_t* path;
   const int32_t* accept_len;
   const int32_t* kv_len;
-  float scale;
+  float scale, scale_log2;
   float* mass;
   float2* part;  // [n_layers][B][Hkv][max_rows * G][nsplit] (max, sum)
   DevState* st;
@@ -199,14 +205,314 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
   }
 }
 
+// ------------------------------------------------------------------------------------------ bf16 queries: tensor cores
+constexpr int kTile = 128;      // positions per tile (UMMA M)
+constexpr int kCols = 32;       // query columns per block (UMMA N)
+constexpr int kThreadsTc = 128;
+constexpr float kFar = 1.15292150460684698e18f;  // 2^60
+
+template <int N>
+struct Cols {
+  static constexpr int value = N;
+};
+
+template <int HD, bool kQ4>
+struct MassLay {
+  static constexpr int kRegionQ = kCols * 128;                  // [32 rows][64] bf16
+  static constexpr int kSmemK = 8 * 1024;                       // 16-bit keys: two stages of HD / 64 regions [128 positions][64]
+  static constexpr int kRegionK = kTile * 128;
+  static constexpr int kStageK = HD / 64 * kRegionK;
+  static constexpr int kSmemMisc = kSmemK + (kQ4 ? 0 : 2 * kStageK);
+  static constexpr int kTmemS = kQ4 ? 64 : 0, kTmemCols = kQ4 ? 128 : 32;
+};
+struct MassMisc {
+  uint64_t bar_s;
+  uint32_t tmem;
+  alignas(16) float sq[kCols];     // sums of the query rows (4-bit keys)
+  alignas(16) float nm[kCols];     // references, log2 units, negated; inf: none yet. Pass 2: the rows' log-sums
+  alignas(16) float alpha[kCols];
+  float colmax[4][kCols];
+};
+
+template <int HD, bool kPaged, bool kQ4, int kPass>
+__global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const MassParams p) {
+  extern __shared__ __align__(1024) unsigned char smem_tc[];
+  using LY = MassLay<HD, kQ4>;
+  constexpr int W = HD / 32, VPR = HD / 8;  // words of codes per thread and row; 16-byte pieces of a 16-bit row
+  MassMisc& s = *reinterpret_cast<MassMisc*>(smem_tc + LY::kSmemMisc);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "n"(LY::kTmemCols));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (lane == 0) {
+      mbar_init(&s.bar_s, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      fence_proxy_async();
+    }
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __reduce_or_sync(0xffffffffu, s.tmem);
+  const int split = blockIdx.x % p.nsplit, kvh = blockIdx.x / p.nsplit, b = blockIdx.y, layer = blockIdx.z;
+  const Seq sq = find_seq(p, b, kPass == 1 && tid == 0 && blockIdx.x == 0 && layer == 0);
+  const int rows_all = sq.n * p.G, ntiles = (sq.len + kTile - 1) / kTile, G = p.G;
+  const int t0 = (int)((long long)split * ntiles / p.nsplit), n = (int)((long long)(split + 1) * ntiles / p.nsplit) - t0;
+  const size_t seg = ((size_t)layer * p.B + b) * p.Hkv + kvh;
+  float2* const part = p.part + seg * (size_t)(p.max_rows * G) * p.nsplit;
+  const bool aligned = (smem_u32(smem_tc) & 1023u) == 0u;  // the swizzled operand regions need a 1 KB aligned base
+  if (!aligned && tid == 0) report(p.st, CAST_ERR_CUDA, 1024);
+  const unsigned char* const keys = p.k + p.k_stride * layer;
+  const int32_t* const range = reinterpret_cast<const int32_t*>(reinterpret_cast<const unsigned char*>(p.range) + p.range_stride * layer);
+  const __nv_bfloat16* const q = reinterpret_cast<const __nv_bfloat16*>(reinterpret_cast<const unsigned char*>(p.q) + p.q_stride * layer);
+  const int r = lane >> 2, tq = lane & 3;
+  const uint32_t t_part = (uint32_t)(warp * 32) << 16;
+  float* const mass = p.mass + seg * (size_t)p.g.max_pos();
+  uint32_t it = 0;  // tiles so far: the barrier's phase
+  bool ok = aligned;
+
+  auto block = [&](auto nh_c, int r0) {
+    constexpr int NH = decltype(nh_c)::value;
+    constexpr uint32_t shape = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NH >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const int rows = min(rows_all - r0, NH);
+    const uint32_t full = rows >= 32 ? 0xffffffffu : (1u << rows) - 1u;
+    // ---- the query rows; 4-bit keys: their dims in the order of the codes in tensor memory, and their sums
+#pragma unroll 1
+    for (int i = tid; i < NH * VPR; i += kThreadsTc) {
+      const int qr = i / VPR, v = i % VPR;
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (qr < rows) {
+        const int j = (r0 + qr) / G, t = p.path ? p.path[(size_t)b * p.path_stride + j] : j;
+        x = *reinterpret_cast<const uint4*>(q + (((size_t)b * p.Ncap + t) * p.Hq + kvh * G + (r0 + qr - j * G)) * HD + v * 8);
+      }
+      if constexpr (kQ4) {
+        float f[8], sum = 0.f;
+        Vec<__nv_bfloat16>::unpack(x, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += f[e];
+#pragma unroll
+        for (int o = VPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (v == 0) s.sq[qr] = sum;
+        // dims 0, 4, 1, 5 and 2, 6, 3, 7 of the eight
+        const uint2 lo = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
+        const uint2 hi = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+        const int t = v / W, wd = v % W;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int g = 2 * wd + half, ch = 2 * (g & 3) + (t >> 1);
+          *reinterpret_cast<uint2*>(smem_tc + (g >> 2) * LY::kRegionQ + swz(qr, ch) + 8 * (t & 1)) = half ? hi : lo;
+        }
+      } else {
+        *reinterpret_cast<uint4*>(smem_tc + (v >> 3) * LY::kRegionQ + swz(qr, v & 7)) = x;
+      }
+    }
+    if (tid < NH) {
+      if (!kQ4) s.sq[tid] = 0.f;
+      float nm = kPass == 1 ? (tid < rows ? INFINITY : 0.f) : -INFINITY;  // (pass 2: a column without a row weighs nothing)
+      if (kPass == 2 && tid < rows) {
+        const float2* row = part + (size_t)(r0 + tid) * p.nsplit;
+        float m = -INFINITY, l = 0.f;
+        for (int i = 0; i < p.nsplit; ++i) m = fmaxf(m, row[i].x);
+        for (int i = 0; i < p.nsplit; ++i) {
+          const float2 x = row[i];
+          l += x.x == -INFINITY && x.y == 0.f ? 0.f : x.y * exp2f(x.x - m);
+        }
+        nm = -(m + log2f(l));
+      }
+      s.nm[tid] = nm;
+    }
+    // ---- keys, a tile ahead: every lane finds the place of its own position's row
+    uint32_t kc[4][W], row = 0;
+    int page = 0, nkr = 0;
+    bool live_next = false;
+    auto next_page = [&](int i) { page = request_page<kPaged>(p.fg, b, (t0 + min(i, n - 1)) * kTile + tid, sq.len); };
+    auto next_row = [&](int i) {
+      const int pos = (t0 + min(i, n - 1)) * kTile + tid;
+      row = kQ4 ? row_of<kPaged>(p.fg, page, kvh, pos, sq.len) : dense_row_of<kPaged>(p.fg, page, kvh, pos, sq.len);
+      live_next = page_ok<kPaged>(p.fg, page) && pos < sq.len;
+      if (kPaged && kPass == 1 && !page_ok<kPaged>(p.fg, page) && pos < sq.len) report(p.st, CAST_ERR_BAD_PAGE, b);
+    };
+    auto request = [&](int i) {
+      if constexpr (kQ4) {
+        nkr = ld_here(range + row);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          ld_here(kc[j], keys + (size_t)__shfl_sync(0xffffffffu, row, 8 * j + r) * (HD / 2) + tq * (4 * W));
+      } else {
+        unsigned char* stage = smem_tc + LY::kSmemK + (i & 1) * LY::kStageK;
+        constexpr int RPI = 32 / VPR;  // rows per instruction
+#pragma unroll
+        for (int j = 0; j < 32 / RPI; ++j) {
+          const int rr = j * RPI + lane / VPR, v = lane % VPR;
+          const unsigned char* src = keys + (size_t)__shfl_sync(0xffffffffu, row, rr) * (HD * 2) + v * 16;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(stage + (v >> 3) * LY::kRegionK + swz(warp * 32 + rr, v & 7))),
+                       "l"(src)
+                       : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+    };
+    if (n > 0) {
+      next_page(0);
+      next_row(0);
+      next_page(1);
+      request(0);
+    }
+    float l[NH];
+#pragma unroll
+    for (int c = 0; c < NH; ++c) l[c] = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i, ++it) {
+      const bool live = live_next;
+      float ks = p.scale_log2, kl = 0.f;
+      if constexpr (kQ4) {
+        const float st = q4_step((uint32_t)nkr);
+        ks = live ? p.scale_log2 * st : 0.f;
+        kl = live ? p.scale_log2 * fmaf(8.f, st, q4_low((uint32_t)nkr)) : 0.f;
+        if (ok) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            uint32_t out[8 * W];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int w = 0; w < W; ++w) {  // word w's pairs 0, 1 go to the group of 16 dims 2 w, pairs 2, 3 to 2 w + 1
+                const uint32_t c = kc[2 * hf + j][w];
+                out[8 * w + 2 * j] = pair_minus8<0>(c);
+                out[8 * w + 2 * j + 1] = pair_minus8<1>(c);
+                out[8 * w + 4 + 2 * j] = pair_minus8<2>(c);
+                out[8 * w + 4 + 2 * j + 1] = pair_minus8<3>(c);
+              }
+            tmem_st_quads<2 * W>(tmem + t_part + ((uint32_t)(hf * 16) << 16), out);
+          }
+        }
+      }
+      // the tile behind (its 16-bit stage was last read by the product of tile i - 1, which is over)
+      next_row(i + 1);
+      next_page(i + 2);
+      request(i + 1);
+      if constexpr (kQ4) {
+        if (ok) tmem_wait_st();
+      } else {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      }
+      fence_proxy_async();
+      tc_fence_before();
+      __syncthreads();
+      if (warp == __reduce_max_sync(0xffffffffu, (int)(it & 3u)) && ok) {
+        tc_fence_after();
+        const uint64_t dq = umma_desc(smem_u32(smem_tc), 16, 1024);
+        const uint64_t dk = umma_desc(smem_u32(smem_tc + LY::kSmemK + (i & 1) * LY::kStageK), 16, 1024);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint64_t bq = dq + (uint64_t)((k >> 2) * (LY::kRegionQ >> 4) + (k & 3) * 2);
+          if constexpr (kQ4) umma_bf16_ts(tmem + LY::kTmemS, tmem + k * 8, bq, shape, k > 0);
+          else umma_bf16(tmem + LY::kTmemS, dk + (uint64_t)((k >> 2) * (LY::kRegionK >> 4) + (k & 3) * 2), bq, shape, k > 0);
+        }
+        umma_commit(&s.bar_s);
+      }
+      // row i of n sees the positions below len - n + i + 1
+      const int pos = (t0 + i) * kTile + tid, j = pos - (sq.len - sq.n);
+      uint32_t vm = live ? full : 0u;
+      if (j > 0) {
+        const int c = j * G - r0;
+        vm = c >= 32 ? 0u : c > 0 ? vm & (0xffffffffu << c) : vm;
+      }
+      const bool plain = __all_sync(0xffffffffu, vm == full);
+      if (ok) {
+        ok = mbar_wait(&s.bar_s, it & 1u);
+        if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, b);
+      }
+      tc_fence_after();
+      float pr[NH];
+      auto to_weights = [&] {
+        if (plain) weights<NH, false>(pr, s.sq, s.nm, ks, kl, vm);
+        else weights<NH, true>(pr, s.sq, s.nm, ks, kl, vm);
+      };
+      if (ok) read_scores<NH>(tmem + LY::kTmemS + t_part, pr);
+      else {
+#pragma unroll
+        for (int c = 0; c < NH; ++c) pr[c] = 0.f;
+      }
+      if (kPass == 1) {
+        bool far = false;
+        if (i > 0) {
+          to_weights();
+          float top = 0.f;
+#pragma unroll
+          for (int c = 0; c < NH; c += 2) top = max3(top, pr[c], pr[c + 1]);
+          far = top >= kFar;
+        }
+        // The first tile, a column without a reference yet, or a weight far above it: the tile's maxima decide.
+        if (i == 0 || __syncthreads_or(far)) {
+          if (i > 0 && ok) read_scores<NH>(tmem + LY::kTmemS + t_part, pr);
+          {
+            float v[32];
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              v[c] = c < NH && ((vm >> c) & 1u) ? fmaf(ks, pr[c < NH ? c : 0], kl * s.sq[c < NH ? c : 0]) : -INFINITY;
+            s.colmax[warp][lane] = reduce_columns<true>(v);
+          }
+          __syncthreads();
+          if (tid < NH) {
+            const float old = s.nm[tid], mx = fmaxf(fmaxf(s.colmax[0][tid], s.colmax[1][tid]), fmaxf(s.colmax[2][tid], s.colmax[3][tid]));
+            const float now = old == INFINITY || mx + old >= 59.f ? -mx : old;
+            s.alpha[tid] = old == INFINITY || now == old ? 1.f : exp2f(now - old);
+            s.nm[tid] = now;
+          }
+          __syncthreads();
+#pragma unroll
+          for (int c = 0; c < NH; ++c) l[c] *= s.alpha[c];
+          to_weights();
+        }
+#pragma unroll
+        for (int c = 0; c < NH; ++c) l[c] += pr[c];
+      } else {
+        to_weights();
+        float sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < NH; ++c) sum += pr[c];
+        if (vm != 0u && ok) mass[pos] += sum;
+      }
+    }
+    if constexpr (!kQ4) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (kPass == 1) {
+      float v[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) v[c] = c < NH ? l[c < NH ? c : 0] : 0.f;
+      __syncthreads();
+      s.colmax[warp][lane] = reduce_columns<false>(v);
+      __syncthreads();
+      if (tid < rows) {
+        const float sum = s.colmax[0][tid] + s.colmax[1][tid] + s.colmax[2][tid] + s.colmax[3][tid];
+        part[(size_t)(r0 + tid) * p.nsplit + split] = n > 0 ? make_float2(-s.nm[tid], sum) : make_float2(-INFINITY, 0.f);
+      }
+    }
+    __syncthreads();  // the block is done with the arrays
+  };
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows_all; r0 += kCols) {
+    if (rows_all - r0 <= 16) block(Cols<16>(), r0);
+    else block(Cols<kCols>(), r0);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(LY::kTmemCols));
+}
+
 struct MassPlan {
   int nsplit;
   size_t bytes;
 };
 MassPlan mass_plan(const cast_ctx* c, int B, int n_layers, int max_rows, int Hq, int Hkv, const Paging& g) {
   MassPlan pl;
-  const long long base = (long long)B * n_layers * Hkv, tiles = (g.max_pos() + kPT - 1) / kPT;
-  long long n = (4ll * c->num_sms + base - 1) / base;
+  const long long base = (long long)B * n_layers * Hkv, tiles = (g.max_pos() + kTile - 1) / kTile;
+  long long n = (8ll * c->num_sms + base - 1) / base;  // two rounds of resident CTAs: sequences differ in length
   if (n > kMaxSplit) n = kMaxSplit;
   if (n > tiles) n = tiles;
   pl.nsplit = (int)(n < 1 ? 1 : n);
@@ -238,6 +544,38 @@ cast_status launch_mass(cast_ctx* c, const MassParams& p, int n_layers, cudaStre
   return CAST_OK;
 }
 
+template <int HD, bool kPaged, bool kQ4>
+cast_status launch_mass_tc(const MassParams& p, int n_layers, cudaStream_t s) {
+  const int smem = MassLay<HD, kQ4>::kSmemMisc + (int)sizeof(MassMisc);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.Hkv * p.nsplit, p.B, n_layers);
+  cfg.blockDim = dim3(kThreadsTc, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // launched while its predecessor drains; waits for it
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  auto* const k1 = mass_tc_kernel<HD, kPaged, kQ4, 1>;
+  auto* const k2 = mass_tc_kernel<HD, kPaged, kQ4, 2>;
+  for (auto* k : {k1, k2}) {
+    CAST_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    CAST_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, kQ4 ? 40 : 100));
+  }
+  cudaError_t e = cudaLaunchKernelEx(&cfg, k1, p);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, k2, p);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return CAST_ERR_CUDA;
+  }
+  return CAST_OK;
+}
+template <int HD, bool kQ4>
+cast_status launch_mass_tc(const MassParams& p, int n_layers, cudaStream_t s) {
+  return p.g.page_size > 0 ? launch_mass_tc<HD, true, kQ4>(p, n_layers, s) : launch_mass_tc<HD, false, kQ4>(p, n_layers, s);
+}
+
 cast_status mass_call(cast_ctx* c, const void* q, const void* k, const void* range, bool q4, cast_dtype dtype, int B, int n_layers,
                       size_t q_stride, size_t k_stride, size_t range_stride, int Hq, int Hkv, int D, const Paging& g,
                       const int32_t* path, const int32_t* accept_len, const int32_t* kv_len, float scale, float* mass,
@@ -257,19 +595,21 @@ cast_status mass_call(cast_ctx* c, const void* q, const void* k, const void* ran
   p.max_rows = path ? p.path_stride : p.Ncap;
   p.g = g; p.path = path; p.accept_len = accept_len; p.kv_len = kv_len;
   p.scale = scale == 0.f ? 1.0f / sqrtf((float)D) : scale;
+  p.scale_log2 = p.scale * 1.4426950408889634f;
   p.mass = mass; p.st = c->state;
+  if (!fast_paging(g, B, Hkv, &p.fg)) return CAST_ERR_CAPACITY;
   const MassPlan pl = mass_plan(c, B, n_layers, p.max_rows, Hq, Hkv, g);
   // compute calls never allocate: the workspace comes from cast_reserve_attention_mass
   if (pl.bytes > c->mass_ws_bytes) return CAST_ERR_CAPACITY;
   p.nsplit = pl.nsplit;
   p.part = (float2*)c->mass_ws;
   cudaStream_t s = (cudaStream_t)stream;
-  if (q4) {
-    if (dtype == CAST_F32) return D == 64 ? launch_mass<float, 64, true>(c, p, n_layers, s) : launch_mass<float, 128, true>(c, p, n_layers, s);
-    return D == 64 ? launch_mass<__nv_bfloat16, 64, true>(c, p, n_layers, s) : launch_mass<__nv_bfloat16, 128, true>(c, p, n_layers, s);
+  if (dtype == CAST_BF16) {
+    if (q4) return D == 64 ? launch_mass_tc<64, true>(p, n_layers, s) : launch_mass_tc<128, true>(p, n_layers, s);
+    return D == 64 ? launch_mass_tc<64, false>(p, n_layers, s) : launch_mass_tc<128, false>(p, n_layers, s);
   }
-  if (dtype == CAST_F32) return D == 64 ? launch_mass<float, 64, false>(c, p, n_layers, s) : launch_mass<float, 128, false>(c, p, n_layers, s);
-  return D == 64 ? launch_mass<__nv_bfloat16, 64, false>(c, p, n_layers, s) : launch_mass<__nv_bfloat16, 128, false>(c, p, n_layers, s);
+  if (q4) return D == 64 ? launch_mass<float, 64, true>(c, p, n_layers, s) : launch_mass<float, 128, true>(c, p, n_layers, s);
+  return D == 64 ? launch_mass<float, 64, false>(c, p, n_layers, s) : launch_mass<float, 128, false>(c, p, n_layers, s);
 }
 
 }  // namespace

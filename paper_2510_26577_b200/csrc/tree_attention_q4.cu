@@ -26,8 +26,7 @@
 // CAST_ERR_TIMEOUT, stops touching the operands and runs out.
 #include <math.h>
 
-#include "kv_q4.h"
-#include "tc_ptx.h"
+#include "q4_tc.h"
 
 namespace cast {
 
@@ -47,9 +46,7 @@ struct Q4Params {
   const unsigned char *kc, *vc;
   const uint32_t *kr, *vr;
   int B, Ncap, Nmax, Hq, Hkv, G, words;
-  Paging g;
-  uint32_t page_mul;  // position / page_size = position * page_mul >> page_shift
-  int page_shift;
+  FastPaging g;
   const int32_t* kv_len;
   const int32_t* n_tree;
   const int32_t* first_row;
@@ -109,76 +106,6 @@ struct Misc {
 
 constexpr int kTmemK = 0, kTmemS = 64, kTmemO = 128, kTmemCols = 256;  // K codes 64, scores 48, output 48
 
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ bool named_or(int id, int threads, bool pred) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %3, 0;\n\t"
-      "bar.red.or.pred q, %1, %2, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(id), "r"(threads), "r"((uint32_t)pred)
-      : "memory");
-  return r != 0;
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr)
-               : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-// 16 lanes x 8 C columns: lane quad l / 4 of the warp holds columns 8 g + 2 (l % 4) and the next of row l / 4 in r[4 g], r[4 g + 1],
-// of row l / 4 + 8 in r[4 g + 2], r[4 g + 3].
-template <int C>
-__device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const uint32_t (&r)[4 * C]) {
-  if constexpr (C == 8)
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-          "r"(r[30]), "r"(r[31])
-        : "memory");
-  else
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
-// (x & mask) | base in one instruction: written with operators it became two.
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(base));
-  return r;
-}
-// Codes i and i + 4 of a word (its nibbles) as a pair of bf16. 16 + c: the code in the upper mantissa bits of 16, whose step is 1 / 8
-// there and 1 with the code three bits up. 128 + c: the code in the lowest bits.
-template <int I>
-__device__ __forceinline__ uint32_t pair_plus16(uint32_t w) {
-  return and_or(I == 0 ? w << 3 : I == 1 ? w >> 1 : I == 2 ? w >> 5 : w >> 9, 0x00780078u, 0x41804180u);
-}
-template <int I>
-__device__ __forceinline__ uint32_t pair_minus8(uint32_t w) {
-  const uint32_t x = and_or(w >> (4 * I), 0x000f000fu, 0x43004300u);
-  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), __floats2bfloat162_rn(136.f, 136.f));  // exact
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
-
 __device__ __forceinline__ void advance(Walk& w, const Misc& s, const Q4Params& p) {
   if (--w.left <= 0 || ++w.t < s.tl[w.b]) return;
   w.t = 0;
@@ -190,71 +117,6 @@ __device__ __forceinline__ void advance(Walk& w, const Misc& s, const Q4Params& 
   while (s.tl[w.b] == 0);  // (tiles are left, so a sequence with tiles follows)
 }
 
-// Loads that stay where they are written: left to itself the compiler moves a load down to its use, a tile later.
-__device__ __forceinline__ int ld_here(const int32_t* p) {
-  int r;
-  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(r) : "l"(p));
-  return r;
-}
-__device__ __forceinline__ void ld_here(uint32_t (&r)[4], const unsigned char* p) {
-  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
-}
-__device__ __forceinline__ void ld_here(uint32_t (&r)[2], const unsigned char* p) {
-  asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
-}
-
-// Pages, rows and pairs are requested tiles ahead of their use: nothing between the request and the use may look at what has
-// been requested, so places without a row request another's (position total - 1, page 0) and are told apart when they are used.
-// (Branches around the loads made every one of them a wait: 7 us a tile instead of less than one.)
-template <bool kPaged>
-__device__ __forceinline__ int request_page(const Q4Params& p, int b, int pos, int total) {
-  if (!kPaged) return b;
-  const int at = min(pos, total - 1);
-  return ld_here(p.g.table + (size_t)b * p.g.seq_capacity + (uint32_t)(((uint64_t)(uint32_t)at * p.page_mul) >> p.page_shift));
-}
-// Index of the row of a position: below 2^32, as the host has checked.
-template <bool kPaged>
-__device__ __forceinline__ uint32_t row_of(const Q4Params& p, int page, int h, int pos, int total) {
-  const uint32_t at = min(pos, total - 1);
-  if (!kPaged) return (uint32_t)(page * p.Hkv + h) * (uint32_t)p.g.seq_capacity + at;
-  const uint32_t ps = p.g.page_size, slot = at - (uint32_t)(((uint64_t)at * p.page_mul) >> p.page_shift) * ps;
-  return ((uint32_t)((uint32_t)page < (uint32_t)p.g.num_pages ? page : 0) * (uint32_t)p.Hkv + (uint32_t)h) * ps + slot;
-}
-template <bool kPaged>
-__device__ __forceinline__ bool page_ok(const Q4Params& p, int page) {
-  return !kPaged || (uint32_t)page < (uint32_t)p.g.num_pages;
-}
-
-// A value per column (32 of them, in every lane), added or maximised over the lanes: lane l returns column l's.
-template <bool kMax>
-__device__ __forceinline__ float reduce_columns(float (&v)[32]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-    for (int i = 0; i < o; ++i) {
-      const bool up = (lane & o) != 0;
-      const float mine = up ? v[i + o] : v[i], other = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + o], o);
-      v[i] = kMax ? fmaxf(mine, other) : mine + other;
-    }
-  }
-  return v[0];
-}
-
-// ---- softmax of half of the columns (kMasked: `vm` says which of them see the position). Scores become weights.
-template <int NH, bool kMasked>
-__device__ __forceinline__ void weights(float (&p)[NH], const float* sq, const float* nm, float ks, float kl, uint32_t vm) {
-#pragma unroll
-  for (int c = 0; c < NH; c += 4) {
-    const float4 q4 = *reinterpret_cast<const float4*>(sq + c), m4 = *reinterpret_cast<const float4*>(nm + c);
-    const float q[4] = {q4.x, q4.y, q4.z, q4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float y = fast_exp2(fmaf(ks, p[c + e], fmaf(kl, q[e], m[e])));
-      p[c + e] = kMasked && !((vm >> (c + e)) & 1u) ? 0.f : y;
-    }
-  }
-}
 // Sums on, weights times step to the B operand.
 template <int NH, bool kMasked>
 __device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], float (&z)[NH],
@@ -343,25 +205,6 @@ __device__ __forceinline__ void merge_item(const Q4Params& p, const Misc& s, int
   }
 }
 
-// This thread's NH scores. (The wait is tied to the registers, so that no use of them can be scheduled above it.)
-template <int NH>
-__device__ __forceinline__ void read_scores(uint32_t taddr, float (&p)[NH]) {
-#pragma unroll
-  for (int c = 0; c < NH; c += 8) tmem_ld8(taddr + c, reinterpret_cast<uint32_t*>(p) + c);
-  if constexpr (NH == 8)
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(p[0]), "+f"(p[1]), "+f"(p[2]), "+f"(p[3]), "+f"(p[4]), "+f"(p[5]), "+f"(p[6]), "+f"(p[7])
-                 :
-                 : "memory");
-  else
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(p[0]), "+f"(p[1]), "+f"(p[2]), "+f"(p[3]), "+f"(p[4]), "+f"(p[5]), "+f"(p[6]), "+f"(p[7]), "+f"(p[8]), "+f"(p[9]),
-                   "+f"(p[10]), "+f"(p[11]), "+f"(p[12]), "+f"(p[13]), "+f"(p[14]), "+f"(p[15]), "+f"(p[16]), "+f"(p[17]), "+f"(p[18]),
-                   "+f"(p[19]), "+f"(p[20]), "+f"(p[21]), "+f"(p[22]), "+f"(p[23])
-                 :
-                 : "memory");
-}
-
 // New references for the columns of a group of four warps (all of them call), from the tile's largest scores (`p`: the scores, as
 // they come); what the columns have gathered (first: nothing yet) follows. An item's first tile, and scores that climb by 2^60.
 template <int NH>
@@ -425,7 +268,7 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
   } else if (warp == 0) {
     // the line of tiles
     constexpr int KB = CAST_MAX_BATCH / 32;
-    const long long max_pos = p.g.max_pos();
+    const long long max_pos = p.g.page_size == 0 ? p.g.seq_capacity : (long long)p.g.seq_capacity * p.g.page_size;
     long long run = 0;
     int items = 0;
     int Nv[KB], Lv[KB], Fv[KB];
@@ -518,12 +361,12 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
   uint32_t row = 0;                // of the tile in kc
   auto next_page = [&](int i) {
     const int4 e = s.step[i & 7];
-    page = request_page<kPaged>(p, e.x, e.z + posl, e.w);
+    page = request_page<kPaged>(p.g, e.x, e.z + posl, e.w);
   };
   auto next_row = [&](int i) {
     const int4 e = s.step[i & 7];
-    row = row_of<kPaged>(p, page, e.y, e.z + posl, e.w);
-    const bool fine = page_ok<kPaged>(p, page);
+    row = row_of<kPaged>(p.g, page, e.y, e.z + posl, e.w);
+    const bool fine = page_ok<kPaged>(p.g, page);
     if (kPaged && !fine && e.z + posl < e.w) report(p.st, CAST_ERR_BAD_PAGE, e.x);
     live_k = fine && e.z + posl < e.w;
   };
@@ -870,8 +713,8 @@ cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_c
   const int grid = q4_grid(c);
   // rows of the cache and elements of q are counted in 32 bits: more would not fit the device's memory
   if ((long long)B * c->cfg.max_tree * Hq * D > 0xffffffffll) return CAST_ERR_CAPACITY;
-  if ((long long)(g.page_size > 0 ? g.num_pages : B) * Hkv * (g.page_size > 0 ? g.page_size : g.seq_capacity) > 0xffffffffll) return CAST_ERR_CAPACITY;
   Q4Params p;
+  if (!fast_paging(g, B, Hkv, &p.g)) return CAST_ERR_CAPACITY;
   p.nrb = q4_row_blocks(c, Hq, Hkv);
   // compute calls never allocate: the workspace comes from cast_reserve_attention_q4
   if (grid * kPartBytes + (size_t)B * Hkv * p.nrb * sizeof(int32_t) > c->q4_ws_bytes) return CAST_ERR_CAPACITY;
@@ -879,12 +722,6 @@ cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_c
   p.kc = (const unsigned char*)k_codes; p.vc = (const unsigned char*)v_codes;
   p.kr = (const uint32_t*)k_range; p.vr = (const uint32_t*)v_range;
   p.B = B; p.Ncap = c->cfg.max_tree; p.Nmax = c->cfg.total_token; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.words = c->words;
-  p.g = g;
-  // exact for positions below 2^31: the multiplier is at most page_size - 1 too large in 2^page_shift, page_shift = 31 + log2 (rounded up)
-  int lg = 0;
-  while (g.page_size > 0 && (1ll << lg) < g.page_size) ++lg;
-  p.page_shift = 31 + lg;
-  p.page_mul = g.page_size > 0 ? (uint32_t)(((1ull << p.page_shift) + g.page_size - 1) / g.page_size) : 0u;
   p.kv_len = kv_len; p.n_tree = n_tree; p.first_row = first_row; p.anc = anc;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.part_o = (float*)c->q4_ws;
