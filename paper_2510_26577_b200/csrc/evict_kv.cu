@@ -3,8 +3,8 @@
 // Two launches. evict_select_kernel, one CTA per (layer, sequence, kv-head), finds the (budget - recent)-th largest weight
 // of the positions before the recent ones by a radix selection over the order-preserving integers of the weights (11 + 11 + 10
 // bits: three histograms in shared memory), then writes the kept positions in ascending order and moves their weights to the
-// front in one pass of block-wide counting. evict_gather_kernel moves the rows: a CTA takes one (layer, sequence, kv-head), K or V,
-// and up to 128 bytes of the row, and walks the list in order, many rows in flight. A row never moves up, so all sources of a
+// front in one pass of block-wide counting. evict_gather_kernel moves the rows: a CTA takes one (layer, sequence, kv-head) of K or V
+// and walks the list in order, many rows in flight. A row never moves up, so all sources of a
 // group of rows lie at or behind the group's own destinations: its loads come before its stores, and nothing later is lost.
 // Bound by memory: the weights once, the moved rows once each way.
 #include "kv_q4.h"
@@ -73,9 +73,15 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
       const int shift = shifts[pass], n = 1 << bits[pass];
       for (int i = tid; i < n; i += kSelThreads) hist[i] = 0;
       __syncthreads();
-      for (int i = tid; i < cand; i += kSelThreads) {
-        const uint32_t k = mass_key(mass[i]);
-        if ((k & mask) == key) atomicAdd(&hist[(k >> shift) & (n - 1)], 1u);
+      for (int i0 = tid; i0 < cand; i0 += 8 * kSelThreads) {  // eight loads in flight
+        float m[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = i0 + e * kSelThreads < cand ? mass[i0 + e * kSelThreads] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t k = mass_key(m[e]);
+          if (i0 + e * kSelThreads < cand && (k & mask) == key) atomicAdd(&hist[(k >> shift) & (n - 1)], 1u);
+        }
       }
       __syncthreads();
       // from the top: thread t sums the n / kSelThreads bins below those of thread t - 1
@@ -134,17 +140,19 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
     }
     if (lane == 31) count_s[round & 1][warp] = upto;
     __syncthreads();  // (and: every weight of this round is in registers before any is overwritten)
-    uint2 before = make_uint2(above0, equal0), all = make_uint2(0u, 0u);
+    // lane w: the warps' counts up to w
+    uint2 sums = lane < kSelThreads / 32 ? count_s[round & 1][lane] : make_uint2(0u, 0u);
 #pragma unroll
-    for (int w = 0; w < kSelThreads / 32; ++w) {
-      const uint2 c = count_s[round & 1][w];
-      if (w < warp) {
-        before.x += c.x;
-        before.y += c.y;
+    for (int o = 1; o < kSelThreads / 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, sums.x, o), y = __shfl_up_sync(0xffffffffu, sums.y, o);
+      if (lane >= o) {
+        sums.x += x;
+        sums.y += y;
       }
-      all.x += c.x;
-      all.y += c.y;
     }
+    const uint2 all = make_uint2(__shfl_sync(0xffffffffu, sums.x, kSelThreads / 32 - 1), __shfl_sync(0xffffffffu, sums.y, kSelThreads / 32 - 1));
+    uint2 before = make_uint2(__shfl_sync(0xffffffffu, sums.x, (warp + 31) & 31), __shfl_sync(0xffffffffu, sums.y, (warp + 31) & 31));
+    before = warp == 0 ? make_uint2(above0, equal0) : make_uint2(above0 + before.x, equal0 + before.y);
     uint32_t nu = before.x + upto.x - n_up, ne = before.y + upto.y - n_eq;
 #pragma unroll
     for (int e = 0; e < kSelItems; ++e) {
@@ -167,26 +175,40 @@ struct MoveParams {
   EvictParams e;
   unsigned char* base[4];   // 16-bit caches: K, V; 4-bit: K codes, V codes, K pairs, V pairs
   size_t stride[4];         // bytes per layer
-  int row_bytes[4];
-  int q4;
+  FastPaging fg;
 };
 
-// Bytes [col, col + VPR * sizeof(V)) of the rows of one (layer, sequence, kv-head) of one buffer.
-template <typename V, int VPR, int U>
-__device__ __forceinline__ void move_rows(const MoveParams& p, int which, int layer, int b, int h, int col) {
-  constexpr int RPS = kMoveThreads / VPR;  // rows per step
+// The rows of one (layer, sequence, kv-head) of one buffer, VPR threads to a row, ROWS rows at a time: a thread finds the places of
+// a row, the next rows' while these rows' loads are out. (Found by every thread for itself the places were most of the work: 32
+// layers of 4 sequences cut from 6000-8192 to 4096, 1077 us.)
+constexpr int kMoveRows = 512;  // most rows at a time
+template <typename V, int VPR, int ROWS, bool kQ4>
+__device__ __forceinline__ void move_rows(const MoveParams& p, uint32_t (*src_s)[kMoveRows], uint32_t (*dst_s)[kMoveRows], int which, int layer, int b, int h) {
+  constexpr int RPS = kMoveThreads / VPR, U = ROWS / RPS;  // rows per step, steps
+  static_assert(ROWS <= kMoveRows && ROWS % RPS == 0, "whole steps");
   const EvictParams& e = p.e;
   const int tid = threadIdx.x, sub = tid % VPR, r = tid / VPR;
   const size_t seg = ((size_t)layer * e.B + b) * e.Hkv + h;
   const int32_t* const kept = e.kept + seg * (size_t)e.budget;
-  unsigned char* const base = p.base[which] + p.stride[which] * layer + col + sub * sizeof(V);
-  const size_t row_bytes = p.row_bytes[which];
-  const int slots = e.g.page_size;
-  auto place = [&](int pos) {
-    int page, slot;
-    find_place(e.g, b, pos, page, slot);  // (the selection has checked the ids)
-    if (p.q4) return (size_t)q4_row(e.g, e.Hkv, h, page, slot) * row_bytes;
-    return (((size_t)page * (slots == 0 ? e.g.seq_capacity : slots) + slot) * e.Hkv + h) * row_bytes;
+  unsigned char* const base = p.base[which] + p.stride[which] * layer + sub * sizeof(V);
+  constexpr int kRow = VPR * (int)sizeof(V);
+  auto place = [&](int pos) -> uint32_t {  // (the selection has checked the ids)
+    uint32_t page = b, slot = pos, slots = p.fg.seq_capacity;
+    if (p.fg.page_size > 0) {
+      const uint32_t at = (uint32_t)(((uint64_t)(uint32_t)pos * p.fg.mul) >> p.fg.shift);
+      page = __ldg(p.fg.table + (size_t)b * p.fg.seq_capacity + at);
+      slots = p.fg.page_size;
+      slot = pos - at * slots;
+    }
+    return kQ4 ? (page * (uint32_t)e.Hkv + h) * slots + slot : (page * slots + slot) * (uint32_t)e.Hkv + h;
+  };
+  auto find = [&](int j0, int buf) {
+#pragma unroll
+    for (int i = tid; i < ROWS; i += kMoveThreads)
+      if (j0 + i < e.budget) {
+        src_s[buf][i] = place(__ldcg(kept + j0 + i));
+        dst_s[buf][i] = place(j0 + i);
+      }
   };
   // the rows in front of the first that moves lie where they belong (kept[j] - j never falls)
   int lo = 0, hi = e.budget;
@@ -194,35 +216,28 @@ __device__ __forceinline__ void move_rows(const MoveParams& p, int which, int la
     const int mid = (lo + hi) >> 1;
     if (__ldcg(kept + mid) > mid) hi = mid; else lo = mid + 1;
   }
-  V cur[U], nxt[U];
-  auto load = [&](int j0, V (&v)[U]) {
+  find(lo, 0);
+  __syncthreads();
+  int buf = 0;
+#pragma unroll 1
+  for (int j0 = lo; j0 < e.budget; j0 += ROWS, buf ^= 1) {
+    V v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * RPS + r;
-      if (j < e.budget) v[u] = __ldcg(reinterpret_cast<const V*>(base + place(__ldcg(kept + j))));
-    }
-  };
-  int j0 = lo;
-  if (j0 < e.budget) load(j0, cur);
-  while (j0 < e.budget) {
-    const int j1 = j0 + U * RPS;
-    if (j1 < e.budget) load(j1, nxt);
-    __syncthreads();  // the sources of [j0, j1) have been read by all
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * RPS + r < e.budget) v[u] = __ldcg(reinterpret_cast<const V*>(base + (size_t)src_s[buf][u * RPS + r] * kRow));
+    find(j0 + ROWS, buf ^ 1);
+    __syncthreads();  // the sources of these rows have been read by all, the next rows' places are known
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * RPS + r;
-      if (j < e.budget) __stcg(reinterpret_cast<V*>(base + place(j)), cur[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) cur[u] = nxt[u];
-    j0 = j1;
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * RPS + r < e.budget) __stcg(reinterpret_cast<V*>(base + (size_t)dst_s[buf][u * RPS + r] * kRow), v[u]);
+    __syncthreads();  // (the places may be overwritten)
   }
 }
 
-// blockIdx.x: kv-head and piece (buffer, 128 bytes of the row) of a (sequence, layer)
+// blockIdx.x: kv-head and buffer of a (sequence, layer)
 template <int RB, bool kQ4>  // bytes of a 16-bit cache's row, or of a 4-bit row's codes
 __global__ void __launch_bounds__(kMoveThreads) evict_gather_kernel(const MoveParams p) {
-  constexpr int kCols = RB > 128 ? RB / 128 : 1, kPieces = (kQ4 ? 4 : 2 * kCols);
+  constexpr int kPieces = kQ4 ? 4 : 2;
   const int piece = blockIdx.x % kPieces, h = blockIdx.x / kPieces, b = blockIdx.y, layer = blockIdx.z;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const EvictParams& e = p.e;
@@ -239,11 +254,12 @@ __global__ void __launch_bounds__(kMoveThreads) evict_gather_kernel(const MovePa
     }
   }
   if (!cut) return;
+  __shared__ uint32_t src_s[2][kMoveRows], dst_s[2][kMoveRows];
   if constexpr (kQ4) {
-    if (piece < 2) move_rows<uint4, RB / 16, 4>(p, piece, layer, b, h, 0);
-    else move_rows<uint32_t, 1, 4>(p, piece, layer, b, h, 0);
+    if (piece < 2) move_rows<uint4, RB / 16, 512, true>(p, src_s, dst_s, piece, layer, b, h);
+    else move_rows<uint32_t, 1, 512, true>(p, src_s, dst_s, piece, layer, b, h);
   } else {
-    move_rows<uint4, 8, 4>(p, piece / kCols, layer, b, h, piece % kCols * 128);
+    move_rows<uint4, RB / 16, 32768 / RB, false>(p, src_s, dst_s, piece, layer, b, h);  // 32 KB at a time
   }
 }
 
@@ -296,10 +312,10 @@ extern "C" cast_status cast_evict_kv(cast_ctx* c, void* k_cache, void* v_cache, 
   p.e.mass = mass; p.e.kept = kept; p.e.kv_len = kv_len;
   p.base[0] = (unsigned char*)k_cache; p.base[1] = (unsigned char*)v_cache;
   p.stride[0] = p.stride[1] = layer_stride_bytes;
-  p.row_bytes[0] = p.row_bytes[1] = rb;
+  if (!fast_paging(g, B, Hkv, &p.fg)) return CAST_ERR_CAPACITY;
   void* kern = rb == 128 ? (void*)evict_gather_kernel<128, false> : rb == 256 ? (void*)evict_gather_kernel<256, false>
                                                                               : (void*)evict_gather_kernel<512, false>;
-  return launch_evict(c, p, n_layers, B, Hkv, D, 2 * (rb / 128), kern, (cudaStream_t)stream);
+  return launch_evict(c, p, n_layers, B, Hkv, D, 2, kern, (cudaStream_t)stream);
 }
 
 extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_range, void* v_codes, void* v_range,
@@ -317,9 +333,7 @@ extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_rang
   p.base[2] = (unsigned char*)k_range; p.base[3] = (unsigned char*)v_range;
   p.stride[0] = p.stride[1] = code_stride_bytes;
   p.stride[2] = p.stride[3] = range_stride_bytes;
-  p.row_bytes[0] = p.row_bytes[1] = D / 2;
-  p.row_bytes[2] = p.row_bytes[3] = 4;
-  p.q4 = 1;
+  if (!fast_paging(g, B, Hkv, &p.fg)) return CAST_ERR_CAPACITY;
   void* kern = D == 64 ? (void*)evict_gather_kernel<32, true> : (void*)evict_gather_kernel<64, true>;
   return launch_evict(c, p, n_layers, B, Hkv, D, 4, kern, (cudaStream_t)stream);
 }

@@ -22,29 +22,69 @@ struct RowsParams {
   DevState* st;
 };
 
-template <typename T>
-__device__ __forceinline__ void load16(const T* p, float (&x)[kLane]);
-template <>
-__device__ __forceinline__ void load16<float>(const float* p, float (&x)[kLane]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p) + i);
-    x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
-  }
+// Sixteen values as they come, their least and largest (NaN if one is NaN), and the values one by one in fp32.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+template <typename T>
+struct Raw;
 template <>
-__device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16* p, float (&x)[kLane]) {
+struct Raw<float> {
+  float x[kLane];
+  __device__ __forceinline__ void load(const float* p) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
-      x[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      const float4 a = __ldcs(reinterpret_cast<const float4*>(p) + i);
+      x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
     }
   }
-}
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) x[e] = 0.f;
+  }
+  __device__ __forceinline__ float get(int e) const { return x[e]; }
+  __device__ __forceinline__ void range(float& lo, float& hi) const {
+    lo = hi = x[0];
+#pragma unroll
+    for (int e = 1; e < kLane; ++e) {
+      lo = min_nan(lo, x[e]);
+      hi = max_nan(hi, x[e]);
+    }
+  }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint32_t w[kLane / 2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < kLane / 2; ++e) w[e] = 0u;
+  }
+  __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16); }
+  __device__ __forceinline__ void range(float& lo, float& hi) const {  // two at a time
+    uint32_t a = w[0], b = w[0];
+#pragma unroll
+    for (int e = 1; e < kLane / 2; ++e) {
+      asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(w[e]));
+      asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(w[e]));
+    }
+    lo = min_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    hi = max_nan(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u));
+  }
+};
 __device__ __forceinline__ void store16(float* p, const float (&x)[kLane]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) __stcs(reinterpret_cast<float4*>(p) + i, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
@@ -62,27 +102,22 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&x)[kLane
   }
 }
 
-// The row's codes and its pair, from the D / 16 threads that hold it. The quotient is that of a division, rounded to nearest even,
-// everywhere: the product with 1 / step is off by less than 4e-6 there (two roundings, quotients below 16), so it decides
-// unless it lies within 1e-4 of a half, or 1 / step is out of range.
-template <int LPR>
-__device__ __forceinline__ uint2 quantise(const float (&x)[kLane], uint32_t& range) {
-  float lo = x[0], hi = x[0], bad = 0.f;
-#pragma unroll
-  for (int e = 0; e < kLane; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-    bad = fmaf(x[e], 0.f, bad);  // NaN once a value is not finite (fminf and fmaxf pass over NaN)
-  }
+// The row's codes and its pair, from the D / 16 threads that hold it. The code is the quotient of a division, rounded to nearest
+// even, without dividing: q = d r with the rounded reciprocal r, corrected once by its exact remainder, q + (d - q step) r, is within
+// 2^-46 of the quotient before its last rounding, exact at a tie; and no quotient of a difference and a bf16 step lies nearer than
+// 2^-32 to the place where rounding to fp32 would make a tie of it. Only reciprocals out of range are divided.
+template <int LPR, typename R>
+__device__ __forceinline__ uint2 quantise(const R& x, uint32_t& range) {
+  float lo, hi;
+  x.range(lo, hi);
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    bad += __shfl_xor_sync(0xffffffffu, bad, o);
+    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
   const float span = hi - lo;
   const __nv_bfloat16 step_h = __float2bfloat16_rn(__fdiv_rn(span, 15.f)), low_h = __float2bfloat16_rn(lo);
-  if (!(bad == 0.f) || !(span < INFINITY) || !(fabsf(__bfloat162float(low_h)) < INFINITY)) {
+  if (!(span < INFINITY) || !(fabsf(__bfloat162float(low_h)) < INFINITY)) {  // (NaN among the values: span is NaN; infinities: so, or inf)
     range = 0x7fc07fc0u;
     return make_uint2(0u, 0u);
   }
@@ -90,16 +125,29 @@ __device__ __forceinline__ uint2 quantise(const float (&x)[kLane], uint32_t& ran
   const float step = __bfloat162float(step_h), low = __bfloat162float(low_h);
   if (step == 0.f) return make_uint2(0u, 0u);
   const float inv = __fdiv_rn(1.f, step);
-  const bool far = !(inv < 1e37f);
+  constexpr float kMagic = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer, ties to even, in the lowest bits
   uint32_t w[2] = {0u, 0u};
+  if (!(inv < 1e30f)) {
+#pragma unroll 1
+    for (int e = 0; e < kLane; ++e) {
+      float x0 = 0.f;
+#pragma unroll
+      for (int k = 0; k < kLane; ++k) x0 = k == e ? x.get(k) : x0;
+      const float t = rintf(__fdiv_rn(__fsub_rn(x0, low), step));
+      const uint32_t c = (uint32_t)fminf(fmaxf(t, 0.f), 15.f) << (4 * (e & 7));
+      if (e < 8) w[0] |= c;
+      else w[1] |= c;
+    }
+    return make_uint2(w[0], w[1]);
+  }
 #pragma unroll
   for (int e = 0; e < kLane; ++e) {
-    const float d = __fsub_rn(x[e], low);
-    float t = d * inv, q = rintf(t);
-    if (far || fabsf(t - q) > 0.4999f) q = rintf(__fdiv_rn(d, step));
-    w[e / 8] |= (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * (e % 8));
+    const float d = __fsub_rn(x.get(e), low), q = __fmul_rn(d, inv), t = fmaf(fmaf(-q, step, d), inv, q);
+    w[e / 8] += __float_as_uint(__fadd_rn(fminf(fmaxf(t, 0.f), 15.f), kMagic)) << (4 * (e % 8));
   }
-  return make_uint2(w[0], w[1]);
+  constexpr uint32_t kBits = 0x4b400000u;  // the magic number's own bits, eight times shifted and added
+  constexpr uint32_t kOwn = kBits + (kBits << 4) + (kBits << 8) + (kBits << 12) + (kBits << 16) + (kBits << 20) + (kBits << 24) + (kBits << 28);
+  return make_uint2(w[0] - kOwn, w[1] - kOwn);
 }
 
 // D / 16 threads per row, K and V of it side by side. kStore: into the cache, else out of it.
@@ -126,10 +174,12 @@ __global__ void __launch_bounds__(kThreads) q4_rows_kernel(const RowsParams p) {
   uint32_t* const kr = reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(p.kr) + p.range_stride * layer) + row;
   uint32_t* const vr = reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(p.vr) + p.range_stride * layer) + row;
   if (kStore) {
-    float xk[kLane] = {}, xv[kLane] = {};
+    Raw<T> xk, xv;
+    xk.clear();
+    xv.clear();
     if (live) {
-      load16(reinterpret_cast<const T*>(p.k) + at, xk);
-      load16(reinterpret_cast<const T*>(p.v) + at, xv);
+      xk.load(reinterpret_cast<const T*>(p.k) + at);
+      xv.load(reinterpret_cast<const T*>(p.v) + at);
     }
     uint32_t rk, rv;
     const uint2 ck = quantise<LPR>(xk, rk), cv = quantise<LPR>(xv, rv);
@@ -149,7 +199,11 @@ __global__ void __launch_bounds__(kThreads) q4_rows_kernel(const RowsParams p) {
       const float step = q4_step(r[w]), low = q4_low(r[w]);
       float x[kLane];
 #pragma unroll
-      for (int e = 0; e < kLane; ++e) x[e] = fmaf(step, (float)(((e < 8 ? c[w].x : c[w].y) >> (4 * (e % 8))) & 15u), low);
+      for (int e = 0; e < kLane; ++e) {
+        // 16 + code, by its bits (the conversion instruction has a quarter of the rate); the difference is exact
+        const uint32_t word = e < 8 ? c[w].x : c[w].y, sh = e % 8 < 5 ? word << (19 - 4 * (e % 8)) : word >> (4 * (e % 8) - 19);
+        x[e] = fmaf(step, __uint_as_float(and_or(sh, 0x00780000u, 0x41800000u)) - 16.f, low);
+      }
       store16(reinterpret_cast<T*>(const_cast<void*>(w ? p.v : p.k)) + at, x);
     }
   }

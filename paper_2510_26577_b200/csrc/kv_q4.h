@@ -36,6 +36,29 @@ __device__ __forceinline__ long long q4_row(const Paging& g, int Hkv, int h, int
 __device__ __forceinline__ float q4_step(uint32_t range) { return __uint_as_float(range << 16); }
 __device__ __forceinline__ float q4_low(uint32_t range) { return __uint_as_float(range & 0xffff0000u); }
 
+// (x & mask) | base in one instruction: written with operators it became two.
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(base));
+  return r;
+}
+
+// Paging with the division by the page size as a product: position / page_size = position * mul >> shift, exact for positions
+// below 2^31 (the multiplier is at most page_size - 1 too large in 2^shift, shift = 31 + log2 of the page size, rounded up).
+struct FastPaging {
+  const int32_t* table;
+  int page_size, seq_capacity, num_pages, Hkv, shift;
+  uint32_t mul;
+};
+// False where the rows are too many for 32-bit indices (more than a device's memory holds).
+inline bool fast_paging(const Paging& g, int B, int Hkv, FastPaging* f) {
+  int lg = 0;
+  while (g.page_size > 0 && (1ll << lg) < g.page_size) ++lg;
+  *f = {g.table, g.page_size, g.seq_capacity, g.num_pages, Hkv, 31 + lg,
+        g.page_size > 0 ? (uint32_t)(((1ull << (31 + lg)) + g.page_size - 1) / g.page_size) : 0u};
+  return (long long)(g.page_size > 0 ? g.num_pages : B) * Hkv * (g.page_size > 0 ? g.page_size : g.seq_capacity) <= 0xffffffffll;
+}
+
 // Arguments that every q4 call checks alike.
 inline cast_status check_q4(const cast_ctx* c, int B, int Hkv, int D, const Paging& g, const void* kc, const void* kr,
                             const void* vc, const void* vr, size_t code_stride, size_t range_stride) {

@@ -58,12 +58,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// (x & mask) | base in one instruction: written with operators it became two.
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(base));
-  return r;
-}
 // Codes i and i + 4 of a word (its nibbles) as a pair of bf16. 16 + c: the code in the upper mantissa bits of 16, whose step is 1 / 8
 // there and 1 with the code three bits up. 128 + c: the code in the lowest bits.
 template <int I>
@@ -88,22 +82,6 @@ __device__ __forceinline__ void ld_here(uint32_t (&r)[4], const unsigned char* p
 }
 __device__ __forceinline__ void ld_here(uint32_t (&r)[2], const unsigned char* p) {
   asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
-}
-
-// Paging with the division by the page size as a product: position / page_size = position * mul >> shift, exact for positions
-// below 2^31 (the multiplier is at most page_size - 1 too large in 2^shift, shift = 31 + log2 of the page size, rounded up).
-struct FastPaging {
-  const int32_t* table;
-  int page_size, seq_capacity, num_pages, Hkv, shift;
-  uint32_t mul;
-};
-// False where the rows are too many for 32-bit indices (more than a device's memory holds).
-inline bool fast_paging(const Paging& g, int B, int Hkv, FastPaging* f) {
-  int lg = 0;
-  while (g.page_size > 0 && (1ll << lg) < g.page_size) ++lg;
-  *f = {g.table, g.page_size, g.seq_capacity, g.num_pages, Hkv, 31 + lg,
-        g.page_size > 0 ? (uint32_t)(((1ull << (31 + lg)) + g.page_size - 1) / g.page_size) : 0u};
-  return (long long)(g.page_size > 0 ? g.num_pages : B) * Hkv * (g.page_size > 0 ? g.page_size : g.seq_capacity) <= 0xffffffffll;
 }
 
 // Pages, rows and pairs are requested tiles ahead of their use: nothing between the request and the use may look at what has
