@@ -17,6 +17,9 @@ struct RowsParams {
   size_t code_stride, range_stride;
   int B, rows, Hkv;
   Paging g;
+  FastPaging fg;
+  uint32_t head_mul;  // row of the call / Hkv = row * head_mul >> head_shift
+  int head_shift;
   const int32_t* start;
   const int32_t* n_rows;
   DevState* st;
@@ -155,19 +158,26 @@ template <typename T, int D, bool kStore>
 __global__ void __launch_bounds__(kThreads) q4_rows_kernel(const RowsParams p) {
   constexpr int LPR = D / kLane;
   const int b = blockIdx.y, layer = blockIdx.z;
-  const long long i = (long long)blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+  const uint32_t i = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
   const int part = threadIdx.x % LPR;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int n = min(p.n_rows[b], p.rows);
-  const int t = (int)(i / p.Hkv), h = (int)(i - (long long)t * p.Hkv);
+  const int t = (int)(((uint64_t)i * p.head_mul) >> p.head_shift), h = (int)i - t * p.Hkv;
   const unsigned here = __ballot_sync(0xffffffffu, t < n);
   if (here == 0u) return;  // (a row's threads are in one warp: whole warps leave, the others go on together)
   const bool live = t < n;
   long long pos = live ? (long long)(p.start ? p.start[b] : 0) + t : 0;
-  int page = 0, slot = 0;
-  const bool ok = live && pos >= 0 && pos < p.g.max_pos() && find_place(p.g, b, (int)pos, page, slot);
+  bool ok = live && pos >= 0 && pos < p.g.max_pos();
+  uint32_t page = b, slot = (uint32_t)pos, slots = p.fg.seq_capacity;
+  if (p.fg.page_size > 0) {
+    slots = p.fg.page_size;
+    const uint32_t e = ok ? (uint32_t)(((uint64_t)slot * p.fg.mul) >> p.fg.shift) : 0u;
+    page = (uint32_t)p.fg.table[(size_t)b * p.fg.seq_capacity + e];
+    slot -= e * slots;
+    ok = ok && page < (uint32_t)p.fg.num_pages;
+  }
   if (live && !ok && part == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
-  const long long row = ok ? q4_row(p.g, p.Hkv, h, page, slot) : 0;
+  const size_t row = ok ? (page * (uint32_t)p.Hkv + h) * slots + slot : 0u;
   const size_t at = ((((size_t)layer * p.B + b) * p.rows + (live ? t : 0)) * p.Hkv + h) * D + part * kLane;
   unsigned char* const kc = p.kc + p.code_stride * layer + row * (D / 2) + part * 8;
   unsigned char* const vc = p.vc + p.code_stride * layer + row * (D / 2) + part * 8;
@@ -212,7 +222,11 @@ __global__ void __launch_bounds__(kThreads) q4_rows_kernel(const RowsParams p) {
 template <bool kStore>
 cast_status launch_rows(cast_ctx* c, RowsParams& p, cast_dtype dtype, int n_layers, int D, cudaStream_t s) {
   const long long per = kThreads / (D / kLane), blocks = ((long long)p.rows * p.Hkv + per - 1) / per;
-  if (blocks > 0x7fffffffll || n_layers > 65535) return CAST_ERR_CAPACITY;
+  if ((long long)p.rows * p.Hkv > 0x7fffff00ll || n_layers > 65535 || !fast_paging(p.g, p.B, p.Hkv, &p.fg)) return CAST_ERR_CAPACITY;
+  int lg = 0;
+  while ((1ll << lg) < p.Hkv) ++lg;
+  p.head_shift = 31 + lg;  // (as for the pages: exact below 2^31)
+  p.head_mul = (uint32_t)(((1ull << p.head_shift) + p.Hkv - 1) / p.Hkv);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, p.B, n_layers);
   cfg.blockDim = dim3(kThreads, 1, 1);
