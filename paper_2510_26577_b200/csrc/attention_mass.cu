@@ -375,18 +375,13 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
         if (ok) {
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            uint32_t out[8 * W];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int w = 0; w < W; ++w) {  // word w's pairs 0, 1 go to the group of 16 dims 2 w, pairs 2, 3 to 2 w + 1
-                const uint32_t c = kc[2 * hf + j][w];
-                out[8 * w + 2 * j] = pair_minus8<0>(c);
-                out[8 * w + 2 * j + 1] = pair_minus8<1>(c);
-                out[8 * w + 4 + 2 * j] = pair_minus8<2>(c);
-                out[8 * w + 4 + 2 * j + 1] = pair_minus8<3>(c);
-              }
-            tmem_st_quads<2 * W>(tmem + t_part + ((uint32_t)(hf * 16) << 16), out);
+            for (int w = 0; w < W; ++w) {  // word w's pairs 0, 1 go to the group of 16 dims 2 w, pairs 2, 3 to 2 w + 1
+              const uint32_t a = kc[2 * hf][w], c = kc[2 * hf + 1][w];
+              const uint32_t out[8] = {pair_minus8<0>(a), pair_minus8<1>(a), pair_minus8<0>(c), pair_minus8<1>(c),
+                                       pair_minus8<2>(a), pair_minus8<3>(a), pair_minus8<2>(c), pair_minus8<3>(c)};
+              tmem_st_quads<2>(tmem + 16 * w + t_part + ((uint32_t)(hf * 16) << 16), out);
+            }
           }
         }
       }
@@ -429,8 +424,8 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
       tc_fence_after();
       float pr[NH];
       auto to_weights = [&] {
-        if (plain) weights<NH, false>(pr, s.sq, s.nm, ks, kl, vm);
-        else weights<NH, true>(pr, s.sq, s.nm, ks, kl, vm);
+        weights<NH>(pr, s.sq, s.nm, ks, kl);
+        if (!plain) mask_weights<NH>(pr, vm);
       };
       if (ok) read_scores<NH>(tmem + LY::kTmemS + t_part, pr);
       else {

@@ -35,22 +35,10 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
 // of row l / 4 + 8 in r[4 g + 2], r[4 g + 3].
 template <int C>
 __device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const uint32_t (&r)[4 * C]) {
-  if constexpr (C == 8)
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-          "r"(r[30]), "r"(r[31])
-        : "memory");
-  else
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
+  static_assert(C == 2, "16 columns");
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -130,19 +118,22 @@ __device__ __forceinline__ float reduce_columns(float (&v)[32]) {
   return v[0];
 }
 
-// Scores of a position become weights, 2^(ks score + kl sum(q) - reference) per column (kMasked: `vm` says which see the position).
-template <int NH, bool kMasked>
-__device__ __forceinline__ void weights(float (&p)[NH], const float* sq, const float* nm, float ks, float kl, uint32_t vm) {
+// Scores of a position become weights, 2^(ks score + kl sum(q) - reference) per column.
+template <int NH>
+__device__ __forceinline__ void weights(float (&p)[NH], const float* sq, const float* nm, float ks, float kl) {
 #pragma unroll
   for (int c = 0; c < NH; c += 4) {
     const float4 q4 = *reinterpret_cast<const float4*>(sq + c), m4 = *reinterpret_cast<const float4*>(nm + c);
     const float q[4] = {q4.x, q4.y, q4.z, q4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float y = fast_exp2(fmaf(ks, p[c + e], fmaf(kl, q[e], m[e])));
-      p[c + e] = kMasked && !((vm >> (c + e)) & 1u) ? 0.f : y;
-    }
+    for (int e = 0; e < 4; ++e) p[c + e] = fast_exp2(fmaf(ks, p[c + e], fmaf(kl, q[e], m[e])));
   }
+}
+// Nothing from the columns that do not see the position.
+template <int NH>
+__device__ __forceinline__ void mask_weights(float (&p)[NH], uint32_t vm) {
+#pragma unroll
+  for (int c = 0; c < NH; ++c) p[c] = (vm >> c) & 1u ? p[c] : 0.f;
 }
 // This thread's NH scores. (The wait is tied to the registers, so that no use of them can be scheduled above it.)
 template <int NH>

@@ -117,10 +117,11 @@ __device__ __forceinline__ void advance(Walk& w, const Misc& s, const Q4Params& 
   while (s.tl[w.b] == 0);  // (tiles are left, so a sequence with tiles follows)
 }
 
-// Sums on, weights times step to the B operand.
-template <int NH, bool kMasked>
-__device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], float (&z)[NH],
-                                          unsigned char* row, int r7, int chunk0, float vs, float vl, uint32_t vm) {
+// Sums on, weights times step to the B operand. (One copy of it: with a masked one beside it every sum was moved between two
+// registers every tile.)
+template <int NH>
+__device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], float (&z)[NH], unsigned char* row, int r7, int chunk0, float vs,
+                                          float vl) {
 #pragma unroll
   for (int c8 = 0; c8 < NH / 8; ++c8) {
     uint32_t w[4];
@@ -129,18 +130,9 @@ __device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], 
       const int c = c8 * 8 + 2 * e;
       l[c] += p[c];
       l[c + 1] += p[c + 1];
-      float w0 = p[c] * vs, w1 = p[c + 1] * vs;
-      if (kMasked) {  // (a masked row of V without a value: 0 * NaN)
-        const bool v0 = (vm >> c) & 1u, v1 = (vm >> (c + 1)) & 1u;
-        z[c] = fmaf(p[c], v0 ? vl : 0.f, z[c]);
-        z[c + 1] = fmaf(p[c + 1], v1 ? vl : 0.f, z[c + 1]);
-        w0 = v0 ? w0 : 0.f;
-        w1 = v1 ? w1 : 0.f;
-      } else {
-        z[c] = fmaf(p[c], vl, z[c]);
-        z[c + 1] = fmaf(p[c + 1], vl, z[c + 1]);
-      }
-      const __nv_bfloat162 h = __floats2bfloat162_rn(w0, w1);
+      z[c] = fmaf(p[c], vl, z[c]);
+      z[c + 1] = fmaf(p[c + 1], vl, z[c + 1]);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(p[c] * vs, p[c + 1] * vs);
       w[e] = *reinterpret_cast<const uint32_t*>(&h);
     }
     *reinterpret_cast<uint4*>(row + (((chunk0 + c8) ^ r7) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -380,18 +372,13 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
   // K codes of tile i (in kc) to tensor memory, the next tile's requested
   auto store_k = [&](int i_tile, bool ok) {
     if (ok) {
-      uint32_t out[8 * W];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < W; ++i) {  // word i's pairs 0, 1 go to the group of 16 dims 2 i, pairs 2, 3 to 2 i + 1
-          const uint32_t c = kc[j][i];
-          out[8 * i + 2 * j] = pair_plus16<0>(c);
-          out[8 * i + 2 * j + 1] = pair_plus16<1>(c);
-          out[8 * i + 4 + 2 * j] = pair_plus16<2>(c);
-          out[8 * i + 4 + 2 * j + 1] = pair_plus16<3>(c);
-        }
-      tmem_st_quads<2 * W>(tmem + kTmemK + ((uint32_t)(part * 32 + cg * 16) << 16), out);
+      for (int i = 0; i < W; ++i) {  // word i's pairs 0, 1 go to the group of 16 dims 2 i, pairs 2, 3 to 2 i + 1
+        const uint32_t a = kc[0][i], c = kc[1][i];
+        const uint32_t out[8] = {pair_plus16<0>(a), pair_plus16<1>(a), pair_plus16<0>(c), pair_plus16<1>(c),
+                                 pair_plus16<2>(a), pair_plus16<3>(a), pair_plus16<2>(c), pair_plus16<3>(c)};
+        tmem_st_quads<2>(tmem + kTmemK + 16 * i + ((uint32_t)(part * 32 + cg * 16) << 16), out);
+      }
     }
     next_row(i_tile + 1);
     request(p.kc, kc);
@@ -529,8 +516,11 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       // this tile's pair and rows without a place (those of `row` are the next tile's by now)
       const float st_k = q4_step(nkr), st_v = q4_step(nvr);
       const bool live = live_v;
-      const float ks = live ? p.scale_log2 * st_k : 0.f, kl = live ? p.scale_log2 * fmaf(-16.f, st_k, q4_low(nkr)) : 0.f;
-      const float vs = live ? st_v : 0.f, vl = live ? fmaf(8.f, st_v, q4_low(nvr)) : 0.f;
+      // (a V row without a value: the scores take the NaN over, for the columns that see them; 0 * NaN reaches no other)
+      const bool sound = st_v == st_v && q4_low(nvr) == q4_low(nvr);
+      const float ks = live ? p.scale_log2 * (sound ? st_k : st_v + q4_low(nvr)) : 0.f;
+      const float kl = live ? p.scale_log2 * fmaf(-16.f, st_k, q4_low(nkr)) : 0.f;
+      const float vs = live && sound ? st_v : 0.f, vl = live && sound ? fmaf(8.f, st_v, q4_low(nvr)) : 0.f;
       request_pair();
       // ---- V codes: the buffer's last reader was O^T of tile it - 2, awaited with tile it - 1
       store_v(it & 1, ok);
@@ -550,8 +540,8 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       tc_fence_after();
       const uint32_t t_s = tmem + kTmemS + c0 + t_part;
       auto to_weights = [&] {
-        if (plain) weights<NH, false>(pr, s.sq + c0, s.nm + c0, ks, kl, vm);
-        else weights<NH, true>(pr, s.sq + c0, s.nm + c0, ks, kl, vm);
+        weights<NH>(pr, s.sq + c0, s.nm + c0, ks, kl);
+        if (!plain) mask_weights<NH>(pr, vm);
       };
       bool far = false;
       if (ok) {
@@ -576,8 +566,7 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       }
       if (ok) {
         unsigned char* p_row = smem + LY::kSmemP + posl * 128;
-        if (plain) hand_over<NH, false>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl, vm);
-        else hand_over<NH, true>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl, vm);
+        hand_over<NH>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl);
       }
       if (i + 1 < n) store_k(it + 1, ok);  // (S^T of this tile has read the codes before)
       if (tid == 0) look_ahead(it + 4);
