@@ -385,14 +385,10 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
           }
         }
       }
-      // the tile behind (its 16-bit stage was last read by the product of tile i - 1, which is over)
-      next_row(i + 1);
-      next_page(i + 2);
-      request(i + 1);
       if constexpr (kQ4) {
         if (ok) tmem_wait_st();
       } else {
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
       }
       fence_proxy_async();
       tc_fence_before();
@@ -409,6 +405,11 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
         }
         umma_commit(&s.bar_s);
       }
+      // The tile behind: requested here because the fence waits for whatever is out. (Its 16-bit stage was last read by the product of
+      // tile i - 1, which is over.)
+      next_row(i + 1);
+      next_page(i + 2);
+      request(i + 1);
       // row i of n sees the positions below len - n + i + 1
       const int pos = (t0 + i) * kTile + tid, j = pos - (sq.len - sq.n);
       uint32_t vm = live ? full : 0u;

@@ -98,7 +98,8 @@ struct Misc {
   alignas(16) float nm[kRows];         // references, log2 units, negated; inf: none yet
   alignas(16) float alpha[kRows];      // what a moved reference scales by
   alignas(16) uint32_t at[kRows];      // a query row's first element in q and out
-  float tot_l[kRows], tot_z[kRows];
+  alignas(16) float tot_l[kRows];
+  alignas(16) float tot_z[kRows];
   float red_l[4][kRows], red_z[4][kRows];
   float colmax[8][kHalf];
   uint32_t vis[2][CAST_MAX_TREE];      // columns (32 + 16) that see a tree token
@@ -140,60 +141,81 @@ __device__ __forceinline__ void hand_over(const float (&p)[NH], float (&l)[NH], 
 }
 
 // Merge of an item's partials by the CTA that finished it last: contributors in CTA order, a thread
-// per 8 lanes of a row (which are 8 neighbouring dims).
+// per 8 lanes of a row (which are 8 neighbouring dims). (Not inlined: its registers are not to press on the tiles'.)
 template <int HD>
-__device__ __forceinline__ void merge_item(const Q4Params& p, const Misc& s, int rows, int c_lo, int c_hi, long long first) {
+__device__ __noinline__ void merge_item(const Q4Params& p, const Misc& s, int rows, int c_lo, int c_hi, long long first) {
   constexpr int CPR = HD / 8, RPP = kThreadsQ4 / CPR;  // threads per row, rows at a time
   const int ch = threadIdx.x % CPR;
-  // The contributors' pairs, one per thread of the row, are one round trip; their rows, eight at a time, the next.
+  constexpr int RP = (kRows + RPP - 1) / RPP;          // rows per thread: side by side, every round trip is paid once
+  const int r0 = threadIdx.x / CPR;
   auto slot_of = [&](int c) { return ((uint32_t)c * 2 + (s.bound[c] > first ? 0 : 1)) * kRows; };
   auto pair_of = [&](int c, int r) {
     return c > c_hi || s.bound[c + 1] <= s.bound[c] || r >= rows ? make_float2(-INFINITY, 0.f) : __ldcg(p.part_ml + slot_of(c) + r);
   };
-#pragma unroll 1
-  for (int r0 = 0; r0 < rows; r0 += RPP) {
-    const int r = r0 + threadIdx.x / CPR;
-    float2 ml = pair_of(c_lo + ch, r);
-    float M = ml.x;
-    for (int cb = c_lo + CPR; cb <= c_hi; cb += CPR) M = fmaxf(M, pair_of(cb + ch, r).x);
+  float2 ml[RP];
+  float M[RP], l[RP], acc[RP][8];
 #pragma unroll
-    for (int o = CPR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float acc[8] = {}, l = 0.f;
-    const float* const base = p.part_o + (size_t)min(r, rows - 1) * HD + ch * 8;
-#pragma unroll 1
-    for (int cb = c_lo; cb <= c_hi; cb += CPR) {
-      if (cb > c_lo) ml = pair_of(cb + ch, r);
-      const float wm = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M), lm = wm * ml.y;
-      const uint32_t off = slot_of(min(cb + ch, c_hi)) * HD;
-#pragma unroll 1
-      for (int k0 = 0; k0 < CPR && cb + k0 <= c_hi; k0 += 8) {
-        float4 x[8], y[8];
+  for (int u = 0; u < RP; ++u) ml[u] = pair_of(c_lo + ch, r0 + u * RPP);  // a contributor per thread of the row
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float* at = base + __shfl_sync(0xffffffffu, off, k0 + k, CPR);
-          x[k] = __ldcg(reinterpret_cast<const float4*>(at));
-          y[k] = __ldcg(reinterpret_cast<const float4*>(at + 4));
-        }
+  for (int u = 0; u < RP; ++u) {
+    M[u] = ml[u].x;
+    for (int cb = c_lo + CPR; cb <= c_hi; cb += CPR) M[u] = fmaxf(M[u], pair_of(cb + ch, r0 + u * RPP).x);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float wk = __shfl_sync(0xffffffffu, wm, k0 + k, CPR);
-          l += __shfl_sync(0xffffffffu, lm, k0 + k, CPR);
-          if (wk != 0.f) {  // (a contributor that is none, or saw nothing: its place may hold anything)
-            acc[0] += wk * x[k].x; acc[1] += wk * x[k].y; acc[2] += wk * x[k].z; acc[3] += wk * x[k].w;
-            acc[4] += wk * y[k].x; acc[5] += wk * y[k].y; acc[6] += wk * y[k].z; acc[7] += wk * y[k].w;
-          }
+    for (int o = CPR / 2; o > 0; o >>= 1) M[u] = fmaxf(M[u], __shfl_xor_sync(0xffffffffu, M[u], o));
+    l[u] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[u][e] = 0.f;
+  }
+#pragma unroll 1
+  for (int cb = c_lo; cb <= c_hi; cb += CPR) {
+    float wm[RP], lm[RP];
+#pragma unroll
+    for (int u = 0; u < RP; ++u) {
+      if (cb > c_lo) ml[u] = pair_of(cb + ch, r0 + u * RPP);
+      wm[u] = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - M[u]);
+      lm[u] = wm[u] * ml[u].y;
+    }
+    const uint32_t off = slot_of(min(cb + ch, c_hi)) * HD;
+#pragma unroll 1
+    for (int k0 = 0; k0 < CPR && cb + k0 <= c_hi; k0 += 4) {
+      float4 x[RP][4], y[RP][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* at = p.part_o + __shfl_sync(0xffffffffu, off, k0 + k, CPR) + ch * 8;
+#pragma unroll
+        for (int u = 0; u < RP; ++u) {
+          x[u][k] = __ldcg(reinterpret_cast<const float4*>(at + min(r0 + u * RPP, rows - 1) * HD));
+          y[u][k] = __ldcg(reinterpret_cast<const float4*>(at + min(r0 + u * RPP, rows - 1) * HD + 4));
         }
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int u = 0; u < RP; ++u) {
+          const float wk = __shfl_sync(0xffffffffu, wm[u], k0 + k, CPR);
+          l[u] += __shfl_sync(0xffffffffu, lm[u], k0 + k, CPR);
+          if (wk != 0.f) {  // (a contributor that is none, or saw nothing: its place may hold anything)
+            acc[u][0] += wk * x[u][k].x; acc[u][1] += wk * x[u][k].y; acc[u][2] += wk * x[u][k].z; acc[u][3] += wk * x[u][k].w;
+            acc[u][4] += wk * y[u][k].x; acc[u][5] += wk * y[u][k].y; acc[u][6] += wk * y[u][k].z; acc[u][7] += wk * y[u][k].w;
+          }
+        }
     }
+  }
+  // lanes 8 ch + j: dims base + {0, 4, 1, 5, 2, 6, 3, 7}
+  const int dim = HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch;
+#pragma unroll
+  for (int u = 0; u < RP; ++u) {
+    const int r = r0 + u * RPP;
     if (r >= rows) continue;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    // lanes 8 ch + j: dims base + {0, 4, 1, 5, 2, 6, 3, 7}
-    const int dim = HD == 128 ? 32 * ((ch & 7) >> 1) + 8 * (2 * (ch >> 3) + (ch & 1)) : 8 * ch;
-    const __nv_bfloat162 o0 = __floats2bfloat162_rn(acc[0] * inv, acc[2] * inv), o1 = __floats2bfloat162_rn(acc[4] * inv, acc[6] * inv),
-                         o2 = __floats2bfloat162_rn(acc[1] * inv, acc[3] * inv), o3 = __floats2bfloat162_rn(acc[5] * inv, acc[7] * inv);
-    *reinterpret_cast<uint4*>(p.out + s.at[r] + dim) =
-        make_uint4(*reinterpret_cast<const uint32_t*>(&o0), *reinterpret_cast<const uint32_t*>(&o1),
-                   *reinterpret_cast<const uint32_t*>(&o2), *reinterpret_cast<const uint32_t*>(&o3));
+    const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int a = e < 2 ? 4 * e : 4 * e - 7;  // 0, 4, 1, 5
+      const __nv_bfloat162 h = __floats2bfloat162_rn(acc[u][a] * inv, acc[u][a + 2] * inv);
+      o[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p.out + s.at[r] + dim) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -238,7 +260,7 @@ __device__ __forceinline__ void move_references(Misc& s, const float (&p)[NH], i
 }
 
 template <int HD, bool kPaged>
-__global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Params p) {
+__global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __grid_constant__ Q4Params p) {
   extern __shared__ __align__(1024) unsigned char smem[];
   using LY = Lay<HD>;
   constexpr int W = LY::kW;
@@ -294,8 +316,9 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
     }
     if (lane == 0) {
       s.pre[CAST_MAX_BATCH] = run;
-      // pieces of two tiles at least, and no item over more CTAs than a merge is worth
-      long long workers = (run + 1) / 2;
+      // pieces of three tiles at least (two, four, six: one sequence of 2048 with 60 tokens 38, 38, 38 us for 36), and no item over more
+      // CTAs than a merge is worth
+      long long workers = (run + 2) / 3;
       workers = workers < (long long)items * kMaxJoin ? workers : (long long)items * kMaxJoin;
       workers = workers < (long long)gridDim.x ? workers : (long long)gridDim.x;
       s.workers = (int)workers;
@@ -369,8 +392,8 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       ld_here(c[j], at);
     }
   };
-  // K codes of tile i (in kc) to tensor memory, the next tile's requested
-  auto store_k = [&](int i_tile, bool ok) {
+  // K codes (in kc) to tensor memory
+  auto store_k = [&](bool ok) {
     if (ok) {
 #pragma unroll
       for (int i = 0; i < W; ++i) {  // word i's pairs 0, 1 go to the group of 16 dims 2 i, pairs 2, 3 to 2 i + 1
@@ -380,9 +403,6 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
         tmem_st_quads<2>(tmem + kTmemK + 16 * i + ((uint32_t)(part * 32 + cg * 16) << 16), out);
       }
     }
-    next_row(i_tile + 1);
-    request(p.kc, kc);
-    next_page(i_tile + 2);
     if (ok) tmem_wait_st();
   };
   unsigned char* const v_row = smem + LY::kSmemV + row16 * 128;
@@ -497,7 +517,7 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       }
       s.vis[ch][wd * 32 + lane] = mine;
     }
-    store_k(it, ok);
+    store_k(ok);
     fence_proxy_async();
     tc_fence_before();
     __syncthreads();
@@ -521,9 +541,13 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
       const float ks = live ? p.scale_log2 * (sound ? st_k : st_v + q4_low(nvr)) : 0.f;
       const float kl = live ? p.scale_log2 * fmaf(-16.f, st_k, q4_low(nkr)) : 0.f;
       const float vs = live && sound ? st_v : 0.f, vl = live && sound ? fmaf(8.f, st_v, q4_low(nvr)) : 0.f;
+      // ---- V codes (the buffer's last reader was O^T of tile it - 2, awaited with the tile before), and all requests for the tile
+      // behind: the fence at this one's end waits for them, so they go out first thing (behind it, a K request cost a memory latency)
+      next_row(it + 1);
+      request(p.kc, kc);
       request_pair();
-      // ---- V codes: the buffer's last reader was O^T of tile it - 2, awaited with tile it - 1
       store_v(it & 1, ok);
+      next_page(it + 2);
       live_v = live_k;
       uint32_t vm = live ? full : 0u;
       if (tail) {
@@ -568,7 +592,7 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
         unsigned char* p_row = smem + LY::kSmemP + posl * 128;
         hand_over<NH>(pr, l, z, p_row, posl & 7, c0 >> 3, vs, vl);
       }
-      if (i + 1 < n) store_k(it + 1, ok);  // (S^T of this tile has read the codes before)
+      if (i + 1 < n) store_k(ok);  // (S^T of this tile has read the codes before)
       if (tid == 0) look_ahead(it + 4);
       fence_proxy_async();
       tc_fence_before();
@@ -615,21 +639,16 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const Q4Par
     const int slot = (int)blockIdx.x * 2 + (s.bound[blockIdx.x] > first ? 0 : 1);
     if (ok) {
       tc_fence_after();
-#pragma unroll 1
-      for (int c8 = 0; c8 < NH; c8 += 8) {
-        uint32_t o[8];
-        tmem_ld8(tmem + kTmemO + c0 + c8 + t_part, o);
-        tmem_wait_ld();
-        if (HD == 64 && posl >= 64) continue;
+      float o[NH];
+      read_scores<NH>(tmem + kTmemO + c0 + t_part, o);
+      if (HD == 128 || posl < 64) {
+        float* const part_row = p.part_o + (size_t)slot * kRows * HD + posl;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = c0 + c8 + e;
-          const float x = __uint_as_float(o[e]) + s.tot_z[c];
-          if (c >= rows) continue;
-          if (whole) {
-            p.out[s.at[c] + dim] = __float2bfloat16_rn(x * s.tot_l[c]);
-          } else {
-            __stcg(p.part_o + ((size_t)slot * kRows + c) * HD + posl, x);
+        for (int c = 0; c < NH; ++c) {
+          const float x = o[c] + s.tot_z[c0 + c];
+          if (c0 + c < rows) {
+            if (whole) p.out[s.at[c0 + c] + dim] = __float2bfloat16_rn(x * s.tot_l[c0 + c]);
+            else __stcg(part_row + (c0 + c) * HD, x);
           }
         }
       }
