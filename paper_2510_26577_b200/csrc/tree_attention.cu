@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
         if (row >= 0) {
           const uint32_t kr = p.k_range[row], vr = p.v_range[row];
           load_codes(reinterpret_cast<const unsigned char*>(p.k) + row * (D / 2) + ch * 8, q4_step(kr), q4_low(kr), f);
-          if (q4_low(vr) == q4_low(vr))
+          if (fabsf(fmaf(15.f, q4_step(vr), q4_low(vr))) < INFINITY)
             load_codes(reinterpret_cast<const unsigned char*>(p.v) + row * (D / 2) + ch * 8, q4_step(vr), q4_low(vr), g);
           else if (ch == 0) atomicOr(reinterpret_cast<unsigned long long*>(&nan_s), 1ull << pl);
         }
@@ -387,9 +387,9 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
       float sum = p0 + p1;
 #pragma unroll
       for (int of = 16; of > 0; of >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, of);
-      if constexpr (kQ4) {  // a row without a value reaches the rows that see it, and no other
+      if constexpr (kQ4) {  // a row without a value reaches the rows that see it, and no other; so does a score that is NaN
         const uint64_t nans = nan_s;
-        const bool hit = (s0 != -INFINITY && ((nans >> lane) & 1)) || (s1 != -INFINITY && ((nans >> (lane + 32)) & 1));
+        const bool hit = s0 != s0 || s1 != s1 || (s0 != -INFINITY && ((nans >> lane) & 1)) || (s1 != -INFINITY && ((nans >> (lane + 32)) & 1));
         if (__any_sync(0xffffffffu, hit)) sum = alpha = __int_as_float(0x7fffffff);
       }
       __syncwarp();

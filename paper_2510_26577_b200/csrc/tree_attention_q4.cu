@@ -536,11 +536,12 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __gri
       // this tile's pair and rows without a place (those of `row` are the next tile's by now)
       const float st_k = q4_step(nkr), st_v = q4_step(nvr);
       const bool live = live_v;
-      // (a V row without a value: the scores take the NaN over, for the columns that see them; 0 * NaN reaches no other)
-      const bool sound = st_v == st_v && q4_low(nvr) == q4_low(nvr);
-      const float ks = live ? p.scale_log2 * (sound ? st_k : st_v + q4_low(nvr)) : 0.f;
+      // (a V row without a finite value: the scores become NaN, for the columns that see them; 0 * NaN would reach the others)
+      const float mid_v = fmaf(8.f, st_v, q4_low(nvr));
+      const bool sound = fabsf(mid_v) < INFINITY;
+      const float ks = live ? p.scale_log2 * (sound ? st_k : mid_v - mid_v) : 0.f;
       const float kl = live ? p.scale_log2 * fmaf(-16.f, st_k, q4_low(nkr)) : 0.f;
-      const float vs = live && sound ? st_v : 0.f, vl = live && sound ? fmaf(8.f, st_v, q4_low(nvr)) : 0.f;
+      const float vs = live && sound ? st_v : 0.f, vl = live && sound ? mid_v : 0.f;
       // ---- V codes (the buffer's last reader was O^T of tile it - 2, awaited with the tile before), and all requests for the tile
       // behind: the fence at this one's end waits for them, so they go out first thing (behind it, a K request cost a memory latency)
       next_row(it + 1);
@@ -657,7 +658,8 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __gri
     if (!whole) {
       if ((tid & 127) < NH) {
         const int c = c0 + (tid & 127);
-        __stcg(p.part_ml + (size_t)slot * kRows + c, ok ? make_float2(-s.nm[c], s.tot_l[c]) : make_float2(-INFINITY, 0.f));
+        const float lt = s.tot_l[c];  // (NaN: its own reference may be none, and must not let the merge pass it over)
+        __stcg(p.part_ml + (size_t)slot * kRows + c, ok ? make_float2(lt == lt ? -s.nm[c] : INFINITY, lt) : make_float2(-INFINITY, 0.f));
       }
       // the CTAs that share the item
       const long long end = first + tl;

@@ -325,6 +325,38 @@ def test_attention_reports_and_masks_bad_pages(binding, dtype):
     assert ctx.cast_poll_status() == (6, 1)
 
 
+@pytest.mark.parametrize("dtype,D,lens", [("bf16", 128, [2100, 3]), ("bf16", 64, [1500, 0]), ("f32", 64, [700, 3]), ("f32", 128, [2100, 0])])
+def test_attention_nan_and_infinity(binding, dtype, D, lens):
+    """A query row of NaN gives NaN, however its sequence is divided, and so do keys without a value that fill whole tiles; a
+    masked row whose pair holds infinities reaches nothing."""
+    rng = np.random.default_rng(15)
+    tokens, Hq, Hkv = 6, 8, 2
+    cache = Cache(rng, o4.Paged(rng, 2, max(lens) + tokens, 16), 1, Hkv, D)
+    pg, sl = cache.paged.at(0, np.arange(400))
+    cache.pair["k"][0, pg, 1, sl] = np.nan
+    anc, vis = (list(z) for z in zip(*(random_masks(rng, tokens, tokens) for b in range(2))))
+    for b in range(2):  # token 4 is seen by itself alone
+        vis[b][5, 4] = False
+        anc[b][5, 0] &= ~np.uint32(1 << 4)
+        pg, sl = cache.paged.at(b, np.array([lens[b] + 4]))
+        cache.pair["v"][0, pg, 0, sl] = [np.inf, 1.0] if b else [0.25, -np.inf]
+    cache.upload()
+    q = torch.randn((2, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(4), device="cuda").to(DT[dtype])
+    q[0, 2, 1], q[1, 3, 5] = float("nan"), float("nan")
+    q[0, 3, 2, 7] = float("nan")
+    ctx = context(binding, 2, tokens)
+    n_tree = np.full(2, tokens, np.int32)
+    out = run_attention(ctx, cache, q, np.array(lens, np.int32), np.stack(anc), n_tree)
+    assert ctx.cast_poll_status()[0] == 0
+    got = torch.isnan(out).cpu().numpy()
+    want = np.zeros_like(got)
+    want[0, :, 4:] = True                        # kv-head 1 of the first sequence
+    want[0, 2, 1] = want[0, 3, 2] = want[1, 3, 5] = True
+    want[:, 4, :4] = True                        # token 4 sees its own infinity
+    out = torch.where(torch.isinf(out), torch.full_like(out, float("nan")), out)
+    np.testing.assert_array_equal(got | torch.isnan(out).cpu().numpy(), want)
+
+
 def test_attention_needs_its_workspace_and_shapes(binding):
     rng = np.random.default_rng(14)
     cache = Cache(rng, o4.Paged(rng, 1, 4096, 16), 1, 2, 128)
