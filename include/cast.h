@@ -221,7 +221,7 @@ CAST_API cast_status cast_reserve_attention(cast_ctx* ctx, cast_dtype dtype, int
  * It also reuses, from one attention call to the next, the work list it decoded from kv_len, n_tree and the call's
  * shape: so the promise includes that kv_len, n_tree (and their pointers) keep their values between two attention
  * calls unless a call of this library changed them. Calls of this library that write those inputs
- * (cast_select_nodes, cast_compact_kv) or start a step (cast_step_begin) are accounted for by the library: the
+ * (cast_select_nodes, cast_compact_kv[_q4], cast_evict_kv[_q4], cast_load_kv_q4) or start a step (cast_step_begin) are accounted for by the library: the
  * attention call that follows one of them decodes afresh and takes no early reads. A caller that changes the lengths
  * or tree sizes by other means calls this function again (it discards the list); so does one that captures attention
  * calls in a graph apart from the calls that change them, before the capture, so that every replay decodes.
@@ -390,6 +390,9 @@ CAST_API cast_status cast_accept_static(const void* target_logits, cast_dtype dt
  * other heads would be read in pieces.) The codes of layer l start code_stride_bytes * l after the base pointers, the
  * pairs range_stride_bytes * l; calls that take one layer take the layer's pointers.
  * Codes 16-byte aligned (code_stride_bytes a multiple of 16), pairs 4-byte aligned; D in {64, 128}.
+ * These calls and those of the eviction want the context's device to be the current one (else INVALID_ARG), are launched with
+ * programmatic dependent launch, read nothing before their predecessor on the stream has completed, and count rows of the cache in
+ * 32 bits: a layer of 2^32 rows (positions times kv-heads) or more, and B * Ncap * Hq * D past 2^31, are CAPACITY.
  *
  * cast_store_kv_q4: rows t < n_rows[b] of k, v [n_layers, B, rows, Hkv, D] (dtype `dtype`) to positions
  * start[b] + t (start NULL: 0). Per row, in fp32: lo, hi its least and largest value, low = bf16(lo),
@@ -424,8 +427,9 @@ CAST_API cast_status cast_reserve_attention_q4(cast_ctx* ctx, cast_dtype dtype, 
  * cast_tree_attention_rows over a 4-bit cache (first_row NULL: all rows). q, out [B, Ncap, Hq, D] of type `dtype`; the rows
  * of the tree tokens are already stored at positions kv_len[b] + j. Sums and softmax in fp32; with bf16 queries the codes
  * enter the matrix products as exact small integers, step and low are applied in fp32 outside them, and the weights
- * (times the row's step) are rounded to bf16 once. A masked row of the cache reaches no output, NaN included; a query row
- * that sees nothing gives zeros. Needs Hq % Hkv == 0 and a workspace reserved for this shape; never reads early (see
+ * (times the row's step) are rounded to bf16 once. A masked row of the cache reaches no output, NaN and infinities
+ * included; a query row that sees nothing gives zeros. (bf16 queries: weights run up to 2^60 above the item's reference before
+ * they are scaled back, so values past 2^64 may overflow the sums.) scale 0 selects 1/sqrt(D), here and below. Needs Hq % Hkv == 0 and a workspace reserved for this shape; never reads early (see
  * cast_set_attention_early_reads). Device errors: BAD_TREE, BAD_PAGE (the position counts as masked).
  */
 CAST_API cast_status cast_tree_attention_q4(cast_ctx* ctx, const void* q, const void* k_codes, const void* k_range,
@@ -482,7 +486,8 @@ CAST_API cast_status cast_attention_mass_q4(cast_ctx* ctx, const void* q, const 
  * kv_len[b] = min(kv_len[b], budget). Sequences of at most `budget` positions are left alone.
  *   kept   [n_layers, B, Hkv, budget] int32 out: the old positions of the rows, ascending, -1 beyond them
  *   mass   as for cast_attention_mass, in/out
- * The cache rows behind the new length keep what they hold. Positions of a sequence must not share a page slot.
+ * The cache rows behind the new length keep what they hold. Positions of a sequence must not share a page slot, nor
+ * a sequence that is cut its pages with another.
  * Errors: INVALID_ARG (budget < 1, recent outside [0, budget]); device: BAD_PAGE (a page id of the sequence out of range, or
  * kv_len[b] outside [0, capacity]: the sequence is left alone, its kept is -1).
  */

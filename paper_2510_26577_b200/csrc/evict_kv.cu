@@ -20,7 +20,7 @@ constexpr int kMoveThreads = 256;
 
 struct EvictParams {
   Paging g;
-  int B, n_layers, Hkv, budget, recent;
+  int B, Hkv, budget, recent;
   float* mass;   // [n_layers][B][Hkv][max_pos]
   int32_t* kept; // [n_layers][B][Hkv][budget]
   int32_t* kv_len;
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_gather_kernel(const MovePa
   }
 }
 
-cast_status launch_evict(cast_ctx* c, MoveParams& p, int n_layers, int B, int Hkv, int D, int pieces, void* kern, cudaStream_t s) {
+cast_status launch_evict(cast_ctx* c, MoveParams& p, int n_layers, int B, int Hkv, int pieces, void* kern, cudaStream_t s) {
   if (n_layers > 65535 || (long long)Hkv * pieces > 0x7fffffffll) return CAST_ERR_CAPACITY;
   c->tree_inputs_fresh = 1;  // kv_len and cache rows: an attention call that follows reads them after its dependency wait
   p.e.ticket = c->compact_ticket;
@@ -308,14 +308,14 @@ extern "C" cast_status cast_evict_kv(cast_ctx* c, void* k_cache, void* v_cache, 
   if (((uintptr_t)k_cache | (uintptr_t)v_cache | layer_stride_bytes) & 15) return CAST_ERR_SHAPE;
   const int rb = D * (dtype == CAST_F32 ? 4 : 2);
   MoveParams p = {};
-  p.e.g = g; p.e.B = B; p.e.n_layers = n_layers; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
+  p.e.g = g; p.e.B = B; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
   p.e.mass = mass; p.e.kept = kept; p.e.kv_len = kv_len;
   p.base[0] = (unsigned char*)k_cache; p.base[1] = (unsigned char*)v_cache;
   p.stride[0] = p.stride[1] = layer_stride_bytes;
   if (!fast_paging(g, B, Hkv, &p.fg)) return CAST_ERR_CAPACITY;
   void* kern = rb == 128 ? (void*)evict_gather_kernel<128, false> : rb == 256 ? (void*)evict_gather_kernel<256, false>
                                                                               : (void*)evict_gather_kernel<512, false>;
-  return launch_evict(c, p, n_layers, B, Hkv, D, 2, kern, (cudaStream_t)stream);
+  return launch_evict(c, p, n_layers, B, Hkv, 2, kern, (cudaStream_t)stream);
 }
 
 extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_range, void* v_codes, void* v_range,
@@ -327,7 +327,7 @@ extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_rang
   const cast_status st = check_q4(c, B, Hkv, D, g, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes);
   if (st != CAST_OK) return st;
   MoveParams p = {};
-  p.e.g = g; p.e.B = B; p.e.n_layers = n_layers; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
+  p.e.g = g; p.e.B = B; p.e.Hkv = Hkv; p.e.budget = budget; p.e.recent = recent;
   p.e.mass = mass; p.e.kept = kept; p.e.kv_len = kv_len;
   p.base[0] = (unsigned char*)k_codes; p.base[1] = (unsigned char*)v_codes;
   p.base[2] = (unsigned char*)k_range; p.base[3] = (unsigned char*)v_range;
@@ -335,5 +335,5 @@ extern "C" cast_status cast_evict_kv_q4(cast_ctx* c, void* k_codes, void* k_rang
   p.stride[2] = p.stride[3] = range_stride_bytes;
   if (!fast_paging(g, B, Hkv, &p.fg)) return CAST_ERR_CAPACITY;
   void* kern = D == 64 ? (void*)evict_gather_kernel<32, true> : (void*)evict_gather_kernel<64, true>;
-  return launch_evict(c, p, n_layers, B, Hkv, D, 4, kern, (cudaStream_t)stream);
+  return launch_evict(c, p, n_layers, B, Hkv, 4, kern, (cudaStream_t)stream);
 }

@@ -259,6 +259,7 @@ cast_status rows_call(cast_ctx* c, const void* k, const void* v, cast_dtype dtyp
   p.kc = (unsigned char*)kc; p.vc = (unsigned char*)vc; p.kr = (uint32_t*)kr; p.vr = (uint32_t*)vr;
   p.code_stride = code_stride; p.range_stride = range_stride;
   p.B = B; p.rows = rows; p.Hkv = Hkv; p.g = g; p.start = start; p.n_rows = n_rows; p.st = c->state;
+  if (!kStore) c->tree_inputs_fresh = 1;  // (k and v may be a 16-bit cache: an attention call that follows reads no row early)
   return launch_rows<kStore>(c, p, dtype, n_layers, D, (cudaStream_t)stream);
 }
 

@@ -721,8 +721,8 @@ cast_status tree_attention_q4_launch(cast_ctx* c, const void* q, const void* k_c
                                      const uint32_t* anc, const int32_t* n_tree, const int32_t* first_row, float scale, void* out,
                                      cudaStream_t stream) {
   const int grid = q4_grid(c);
-  // rows of the cache and elements of q are counted in 32 bits: more would not fit the device's memory
-  if ((long long)B * c->cfg.max_tree * Hq * D > 0xffffffffll) return CAST_ERR_CAPACITY;
+  // elements of q are counted in 31 bits, rows of the cache in 32: more would not fit the device's memory
+  if ((long long)B * c->cfg.max_tree * Hq * D > 0x7fffffffll) return CAST_ERR_CAPACITY;
   Q4Params p;
   if (!fast_paging(g, B, Hkv, &p.g)) return CAST_ERR_CAPACITY;
   p.nrb = q4_row_blocks(c, Hq, Hkv);

@@ -75,3 +75,20 @@ def test_kernel_attributes_are_remembered_per_context():
     """They hold for one device: a process that drives two has a context on each."""
     launch = _body(_source(), "bool tree_attention_tc_launch(")
     assert "cudaFuncSetAttribute" in launch and not re.search(r"\bstatic\b", launch)
+
+
+def test_the_kernels_over_4_bit_caches_allocate_behind_the_wait():
+    """One allocation each, behind the wait, and the warp that allocates releases the dependents behind it; every kernel of
+    these files waits before it does anything else, so a block that leaves early has waited too."""
+    for name, head in (("tree_attention_q4.cu", "tree_attn_q4_kernel(const __grid_constant__ Q4Params p)"), ("attention_mass.cu", "mass_tc_kernel(const MassParams p)")):
+        kernel = _body(_source(name), head)
+        steps = ("griddepcontrol.wait", "if (warp == 1) {", "tcgen05.alloc", "tcgen05.relinquish_alloc_permit", "griddepcontrol.launch_dependents")
+        at = [kernel.index(x) for x in steps]
+        assert at == sorted(at) and all(kernel.count(x) == 1 for x in (steps[0], *steps[2:]))
+        assert at[-1] < at[1] + len(_body(kernel[at[1]:], "if (warp == 1)"))
+    for name in ("tree_attention_q4.cu", "attention_mass.cu", "kv_q4.cu", "evict_kv.cu"):
+        text = _source(name)
+        for m in re.finditer(r"__global__ void __launch_bounds__\([^)]*\) (\w+)\(", text):
+            body = _body(text[m.start():], m.group(1))
+            wait = body.index("griddepcontrol.wait")
+            assert "return" not in body[:wait] and "p.kv_len[" not in body[:wait], m.group(1)

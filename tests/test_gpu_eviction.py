@@ -135,6 +135,36 @@ def test_mass_of_a_window_of_rows(binding, kind):
     check_mass(mass, torch.zeros_like(mass), cache, q, None, alen, kv_len, scale=0.2)
 
 
+@pytest.mark.parametrize("kind,dtype", [("16", "bf16"), ("4", "bf16"), ("16", "f32"), ("4", "f32")])
+def test_mass_nan(binding, kind, dtype):
+    """A query of NaN makes what its row sees NaN, in its layer and kv-head alone; a key without a value likewise, and one
+    that no row sees reaches nothing."""
+    rng = np.random.default_rng(10)
+    B, nl, T, Hq, Hkv, D, L = 3, 2, 8, 4, 2, 128, 1500
+    paged = o4.Paged(rng, B, L + 20, 16)
+    cache = Cache(rng, paged, nl, Hkv, D) if kind == "4" else Dense(rng, paged, nl, Hkv, D, dtype)
+    pos = np.concatenate([np.arange(1498, 1510)])
+    for b in (1, 2):  # the last row alone sees position 1499; 1500 and on lie behind the sequence
+        pg, sl = paged.at(b, pos if b == 1 else pos[2:])
+        if kind == "4":
+            cache.pair["k"][1, pg, 1, sl] = np.nan
+        else:
+            cache.k[1, torch.from_numpy(pg), torch.from_numpy(sl), 1] = float("nan")
+    if kind == "4":
+        cache.upload()
+    q = torch.randn((nl, B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(6), device="cuda").to(DT[dtype])
+    q[0, 0, 3, 1] = float("nan")
+    path = np.tile(np.array([[1, 3, 6, 0, 0]], np.int32), (B, 1))
+    mass = torch.zeros((nl, B, Hkv, paged.positions), device="cuda")
+    ctx = context(binding, B, T, 4)
+    run_mass(ctx, cache, q, path, np.full(B, 2, np.int32), np.full(B, L, np.int32), mass)
+    assert ctx.cast_poll_status()[0] == 0
+    want = np.zeros(mass.shape, bool)
+    want[0, 0, 0, :L - 1] = True   # row 1 of 3 sees all positions but the last
+    want[1, 1, 1, :L] = True       # rows 1 and 2 see 1498; what row 2 gives reaches all
+    np.testing.assert_array_equal(np.isnan(mass.cpu().numpy()), want)
+
+
 def test_mass_refuses(binding):
     rng = np.random.default_rng(9)
     B, T, Hq, Hkv, D, H = 5, 16, 4, 2, 128, 4

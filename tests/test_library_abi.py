@@ -44,3 +44,20 @@ def test_config_struct_matches_header_layout():
     # 3 doubles + 14 int32 = 80 bytes, no padding (doubles first)
     assert ctypes.sizeof(CastConfig) == 80
     assert CastConfig.max_batch.offset == 24 and CastConfig.rerank_per_row.offset == 76
+
+
+def test_calls_of_the_4_bit_cache_and_of_eviction_refuse_a_missing_context():
+    """INVALID_ARG from every entry point, before anything is asked of a device."""
+    from paper_2510_26577_b200 import binding
+    lib = binding.load_library()
+    names = [n for n in _declared() if n.endswith("_q4") or "mass" in n or "evict" in n]
+    assert len(names) == 10
+    some = ctypes.create_string_buffer(64)
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "cast.h")).read(), flags=re.S)
+    for n in names:
+        kinds = [ctypes.c_void_p if "*" in a else ctypes.c_float if "float" in a else ctypes.c_size_t if "size_t" in a else ctypes.c_int
+                 for a in re.search(r"\b%s\(([^)]*)\)" % n, text).group(1).split(",")]
+        f = ctypes.CDLL(lib._name)[n]
+        f.argtypes, f.restype = kinds, ctypes.c_int
+        assert f(*[0 if t is not ctypes.c_void_p else None for t in kinds]) == 1, n
+        assert f(None, *[ctypes.cast(some, t) if t is ctypes.c_void_p else t(1) for t in kinds[1:]]) == 1, n
