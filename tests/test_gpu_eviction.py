@@ -165,6 +165,32 @@ def test_mass_nan(binding, kind, dtype):
     np.testing.assert_array_equal(np.isnan(mass.cpu().numpy()), want)
 
 
+def test_16_bit_rows_past_four_gigabytes(binding):
+    """As for the 4-bit cache: weights and eviction at the far end of a large cache."""
+    rng = np.random.default_rng(11)
+    B, Hq, Hkv, D, page, cap, T, H = 2, 4, 2, 128, 16, 12, 9, 4
+    few, far = B * cap, (1 << 32) // (Hkv * page * D * 2) + 100
+    table = rng.permutation(few).reshape(B, cap).astype(np.int32)
+    rows = torch.randn((2, few, page, Hkv, D), generator=torch.Generator("cuda").manual_seed(7), device="cuda").to(torch.bfloat16)
+    q = torch.randn((1, B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(8), device="cuda").to(torch.bfloat16)
+    ctx = context(binding, B, T, H)
+    ctx.cast_reserve_attention_mass(q.dtype, B, 1, T, Hq, Hkv, D, page, cap)
+    results = []
+    for pages, first in ((few, 0), (far, far - few)):
+        k, v = (torch.empty((pages, page, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        k[first:], v[first:] = rows[0], rows[1]
+        where, kv_len = (page, dev(table + first), cap, pages), dev(np.array([190, 61], np.int32))
+        mass, kept = torch.zeros((1, B, Hkv, cap * page), device="cuda"), torch.zeros((1, B, Hkv, 60), dtype=torch.int32, device="cuda")
+        ctx.cast_attention_mass(q, k, B, 1, 0, 0, Hq, Hkv, D, *where, None, dev(np.array([8, 3], np.int32)), kv_len, 0.0, mass)
+        ctx.cast_evict_kv(k, v, B, 1, 0, Hkv, D, *where, 60, 10, mass, kept, kv_len)
+        assert ctx.cast_poll_status()[0] == 0
+        results.append((k[first:].clone(), v[first:].clone(), mass, kept, kv_len))
+        del k, v
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert not torch.equal(results[1][0], rows[0])
+
+
 def test_mass_refuses(binding):
     rng = np.random.default_rng(9)
     B, T, Hq, Hkv, D, H = 5, 16, 4, 2, 128, 4

@@ -357,6 +357,58 @@ def test_attention_nan_and_infinity(binding, dtype, D, lens):
     np.testing.assert_array_equal(got | torch.isnan(out).cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+def test_rows_past_four_gigabytes(binding, dtype, D):
+    """Pages at the far end of a cache of more than 2^32 bytes: the same bits as from a small one, through every call."""
+    rng = np.random.default_rng(22)
+    B, Hq, Hkv, page, cap, T, H = 2, 4, 2, 16, 12, 9, 4
+    few = B * cap
+    far = (1 << 32) // (Hkv * page * D // 2) + 100
+    table = rng.permutation(few).reshape(B, cap).astype(np.int32)
+    x = torch.randn((2, 1, B, 180, Hkv, D), generator=torch.Generator("cuda").manual_seed(7), device="cuda").to(DT[dtype])
+    q = torch.randn((B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(8), device="cuda").to(DT[dtype])
+    anc = np.stack([random_masks(rng, T, T)[0] for b in range(B)])
+    n_tree, path = dev(np.full(B, T, np.int32)), dev(np.tile(np.array([0, 3, 5, 6, 8], np.int32), (B, 1)))
+    ctx = context(binding, B, T, H)
+    ctx.cast_reserve_attention_q4(q.dtype, B, Hq, Hkv, D, page, cap)
+    ctx.cast_reserve_attention_mass(q.dtype, B, 1, H + 1, Hq, Hkv, D, page, cap)
+    results = []
+    for pages, first in ((few, 0), (far, far - few)):
+        codes = [torch.empty((1, pages, Hkv, page, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        pairs = [torch.empty((1, pages, Hkv, page, 2), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        cache, strides = (codes[0], pairs[0], codes[1], pairs[1]), (codes[0][0].numel(), pairs[0][0].numel() * 2)
+        where, kv_len = (page, dev(table + first), cap, pages), dev(np.array([171, 100], np.int32))
+        out, back, mass = torch.zeros_like(q), torch.zeros_like(x), torch.zeros((1, B, Hkv, cap * page), device="cuda")
+        kept = torch.zeros((1, B, Hkv, 60), dtype=torch.int32, device="cuda")
+        ctx.cast_store_kv_q4(x[0], x[1], B, 1, 180, Hkv, D, *where, None, dev(np.array([180, 109], np.int32)), *cache, *strides)
+        ctx.cast_tree_attention_q4(q, *(t[0] for t in cache), B, Hq, Hkv, D, *where, kv_len, dev(anc.view(np.int32)), n_tree, None, 0.0, out)
+        ctx.cast_compact_kv_q4(*cache, *strides, B, 1, Hkv, D, *where, path, dev(np.array([4, 2], np.int32)), kv_len)
+        ctx.cast_attention_mass_q4(q, codes[0], pairs[0], B, 1, 0, *strides, Hq, Hkv, D, *where, path, dev(np.array([4, 2], np.int32)), kv_len, 0.0, mass)
+        ctx.cast_evict_kv_q4(*cache, *strides, B, 1, Hkv, D, *where, 60, 10, mass, kept, kv_len)
+        ctx.cast_load_kv_q4(*cache, *strides, B, 1, 180, Hkv, D, *where, None, kv_len, back[0], back[1])
+        assert ctx.cast_poll_status()[0] == 0
+        results.append((out, back, mass, kept, kv_len))
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and bool(a.any())
+
+
+def test_attention_without_work_and_with_a_larger_workspace(binding):
+    """No token in any sequence: nothing is written; a call after the workspace has grown for a larger one."""
+    rng = np.random.default_rng(23)
+    small, large = (Cache(rng, o4.Paged(rng, B, n, 16), 1, 2, 128) for B, n in ((2, 300), (9, 700)))
+    ctx = context(binding, 9, 12)
+    for cache, kv in ((small, [280, 3]), (large, [680] * 9), (small, [280, 3])):
+        B = len(kv)
+        q = torch.randn((B, 12, 14, 128), generator=torch.Generator("cuda").manual_seed(B), device="cuda").to(torch.bfloat16)
+        anc, vis = zip(*(random_masks(rng, 12, 12) for b in range(B)))
+        kv, n_tree = np.array(kv, np.int32), np.full(B, 12, np.int32)
+        out = run_attention(ctx, cache, q, kv, np.stack(anc), n_tree)
+        check_attention(out, cache, q, kv, vis, n_tree, "bf16")
+        none = run_attention(ctx, cache, q, kv, np.stack(anc), np.zeros(B, np.int32))
+        assert bool(torch.isnan(none).all())
+    assert ctx.cast_poll_status()[0] == 0
+
+
 def test_attention_needs_its_workspace_and_shapes(binding):
     rng = np.random.default_rng(14)
     cache = Cache(rng, o4.Paged(rng, 1, 4096, 16), 1, 2, 128)
