@@ -20,13 +20,14 @@
 // and under the other CTA. Codes and pairs are requested a tile ahead, into registers. (Warps of their own for K, V, pairs, the MMAs and
 // the softmax, 18 in one CTA per SM, took six times as long: five streams of unrolled code on one SM's instruction cache, every
 // instruction about ten cycles apart.)
-// Work is one line of tiles, item after item (sequence, kv-head, block of 48 rows), cut into equal pieces, one per CTA: ragged
-// batches load the machine evenly. An item that lies across CTAs leaves partials in the workspace; the last CTA to finish it
+// Work is one line of tiles, item after item (sequence, kv-head, block of 48 rows), cut into pieces, one per CTA: item by item while
+// there are few items, else evenly, so that ragged batches load the machine evenly. An item that lies across CTAs leaves partials in the workspace; the last CTA to finish it
 // (an atomic ticket, nothing spins) merges them in CTA order. All mbarrier waits are bounded: on expiry the CTA records
 // CAST_ERR_TIMEOUT, stops touching the operands and runs out.
 //
 // Measured, heads of 128 dims, per layer: 64 sequences of 512 to 4096, 12 tokens, 32 / 8 heads 162 us (26 to read the cache); 4 of
-// 32768, 96 tokens, 28 / 4 heads 672 us (109 for the products at the matrix units' measured rate); one of 2048, 60 tokens 35 us.
+// 32768, 96 tokens, 28 / 4 heads 672 us (109 for the products at the matrix units' measured rate); one of 2048, 60 tokens 31 us
+// (25 with 12).
 // Neither memory (12 %) nor the matrix units (8 %) bound it but the instructions that turn codes into operands and scores into
 // weights, with their waits: issue slots are 44 % busy with 16 warps per SM, which is what the registers allow. A single short
 // sequence is bound by the chain launch - queries - first scores - partials - merge. Tried and slower: warps of their own per task (above);
@@ -97,11 +98,13 @@ struct Misc {
   int last, workers;
   long long piece;                     // tiles of a CTA, rounded down; the first `rest` CTAs take one more
   int rest;
+  int whole;                           // pieces end with their items: the line is cut item by item
   Walk seg;                            // the item in work, from its first tile here on
   Walk ahead;                          // the furthest tile in `step`
   alignas(16) int4 step[8];            // tile i of the CTA at i % 8: sequence, kv-head, first position, positions of the sequence
   long long pre[CAST_MAX_BATCH + 1];   // tiles of the sequences before
   long long bound[kMaxGrid + 1];       // first tile of every CTA
+  int cta[CAST_MAX_BATCH], per[CAST_MAX_BATCH];  // cut item by item: CTAs of the sequences before, CTAs of an item
   int L[CAST_MAX_BATCH], N[CAST_MAX_BATCH], F[CAST_MAX_BATCH], tl[CAST_MAX_BATCH], nr[CAST_MAX_BATCH], total[CAST_MAX_BATCH];
   alignas(16) float sq[kRows];         // sums of the query rows
   alignas(16) float nm[kRows];         // references, log2 units, negated; inf: none yet
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __gri
     const long long max_pos = p.g.page_size == 0 ? p.g.seq_capacity : (long long)p.g.seq_capacity * p.g.page_size;
     long long run = 0;
     int items = 0;
-    int Nv[KB], Lv[KB], Fv[KB];
+    int Nv[KB], Lv[KB], Fv[KB], hn[KB], tn[KB], longest = 0;
 #pragma unroll
     for (int k = 0; k < KB; ++k) {  // all loads first: one memory round trip
       const int b = k * 32 + lane;
@@ -321,16 +324,53 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __gri
       items += __reduce_add_sync(0xffffffffu, p.Hkv * nr);
       s.pre[b] = run + upto - mine;
       run += __shfl_sync(0xffffffffu, upto, 31);
+      hn[k] = p.Hkv * nr;
+      tn[k] = tl;
+      longest = max(longest, __reduce_max_sync(0xffffffffu, tl));
       s.L[b] = L; s.N[b] = N; s.F[b] = F; s.tl[b] = tl; s.nr[b] = nr; s.total[b] = total;
+    }
+    // Cut item by item where that makes no piece more than three tiles longer than an even cut would: a CTA that works on two items
+    // pays the queries, the first references and the handing over twice, as much as three tiles (one sequence of 2048 with 60
+    // tokens, cut evenly, had its last partial at 31 us, at 21 cut like this). Pieces of three tiles at least (one, two, four for a
+    // sequence of 2048 with 12 tokens: 30, 26, 27 us for 25), no item over more CTAs than a merge is worth.
+    const long long even = (run + gridDim.x - 1) / gridDim.x;
+    const int q0 = (int)max(max(3ll, even), (long long)((longest + kMaxJoin - 1) / kMaxJoin));
+    int q = q0 + 3, ctas = 0;
+    auto cut = [&] {
+      int sum = 0;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) sum += hn[k] * ((tn[k] + q - 1) / q);
+      ctas = __reduce_add_sync(0xffffffffu, sum);
+      return ctas <= (int)gridDim.x;
+    };
+    const bool fits = cut();
+    if (fits) {
+#pragma unroll 1
+      for (q = q0; q < q0 + 3 && !cut(); ++q) {}
+      if (q == q0 + 3) cut();
+      int before = 0;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const int per = (tn[k] + q - 1) / q, mine = hn[k] * per;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += x;
+        }
+        s.cta[k * 32 + lane] = before + upto - mine;
+        s.per[k * 32 + lane] = per;
+        before += __shfl_sync(0xffffffffu, upto, 31);
+      }
     }
     if (lane == 0) {
       s.pre[CAST_MAX_BATCH] = run;
-      // pieces of three tiles at least (two, four, six: one sequence of 2048 with 60 tokens 38, 38, 38 us for 36), and no item over more
-      // CTAs than a merge is worth
+      s.whole = fits;
+      // (else:) the same for an even cut
       long long workers = (run + 2) / 3;
       workers = workers < (long long)items * kMaxJoin ? workers : (long long)items * kMaxJoin;
       workers = workers < (long long)gridDim.x ? workers : (long long)gridDim.x;
-      s.workers = (int)workers;
+      s.workers = fits ? ctas : (int)workers;
       s.piece = workers > 0 ? run / workers : 0;
       s.rest = workers > 0 ? (int)(run - s.piece * workers) : 0;
     }
@@ -338,7 +378,18 @@ __global__ void __launch_bounds__(kThreadsQ4, 2) tree_attn_q4_kernel(const __gri
   __syncthreads();
   // where the pieces begin
   for (int c = tid; c <= (int)gridDim.x; c += kThreadsQ4) {
-    const long long T = s.pre[CAST_MAX_BATCH], x = c >= s.workers ? T : s.piece * c + min(c, s.rest);
+    const long long T = s.pre[CAST_MAX_BATCH];
+    long long x = T;
+    if (c < s.workers) {
+      x = s.piece * c + min(c, s.rest);
+      if (s.whole) {
+        int b = 0;  // the last sequence that starts at or before c (one without tiles starts where the next does)
+#pragma unroll
+        for (int o = CAST_MAX_BATCH / 2; o > 0; o >>= 1) b += s.cta[b + o] <= c ? o : 0;
+        const int in = c - s.cta[b], item = in / s.per[b], k = in - item * s.per[b];
+        x = s.pre[b] + (long long)item * s.tl[b] + (int)((long long)k * s.tl[b] / s.per[b]);
+      }
+    }
     s.bound[c] = x;
     if (c == (int)blockIdx.x && x < T) {
       int b = 0;
