@@ -315,20 +315,25 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
         *reinterpret_cast<uint4*>(smem_tc + (v >> 3) * LY::kRegionQ + swz(qr, v & 7)) = x;
       }
     }
-    if (tid < NH) {
-      if (!kQ4) s.sq[tid] = 0.f;
-      float nm = kPass == 1 ? (tid < rows ? INFINITY : 0.f) : -INFINITY;  // (pass 2: a column without a row weighs nothing)
-      if (kPass == 2 && tid < rows) {
-        const float2* row = part + (size_t)(r0 + tid) * p.nsplit;
-        float m = -INFINITY, l = 0.f;
-        for (int i = 0; i < p.nsplit; ++i) m = fmaxf(m, row[i].x);
-        for (int i = 0; i < p.nsplit; ++i) {
-          const float2 x = row[i];
-          l += x.x == -INFINITY && x.y == 0.f ? 0.f : x.y * exp2f(x.x - m);
-        }
-        nm = -(m + log2f(l));
+    if (!kQ4 && tid < NH) s.sq[tid] = 0.f;
+    if (kPass == 1) {
+      if (tid < NH) s.nm[tid] = tid < rows ? INFINITY : 0.f;
+    } else if (tid < 4 * NH) {  // the row's sum from the pieces' pairs: four threads to a row
+      const int row = tid >> 2, sub = tid & 3;
+      const float2* pairs = part + (size_t)(r0 + min(row, rows - 1)) * p.nsplit;
+      float m = -INFINITY, l = 0.f;
+#pragma unroll 8
+      for (int i = sub; i < p.nsplit; i += 4) m = fmaxf(m, pairs[i].x);
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+#pragma unroll 4
+      for (int i = sub; i < p.nsplit; i += 4) {
+        const float2 x = pairs[i];
+        l += x.x == -INFINITY && x.y == 0.f ? 0.f : x.y * exp2f(x.x - m);
       }
-      s.nm[tid] = nm;
+      l += __shfl_xor_sync(0xffffffffu, l, 1);
+      l += __shfl_xor_sync(0xffffffffu, l, 2);
+      if (sub == 0) s.nm[row] = row < rows ? -(m + log2f(l)) : -INFINITY;  // (a column without a row weighs nothing)
     }
     // ---- keys, a tile ahead: every lane finds the place of its own position's row
     uint32_t kc[4][W], row = 0;
