@@ -215,6 +215,7 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
 constexpr int kTile = 128;      // positions per tile (UMMA M)
 constexpr int kCols = 32;       // query columns per block (UMMA N)
 constexpr int kThreadsTc = 128;
+constexpr int kMinTiles = 2;    // of a piece (one sequence of 8192, 2 layers: 34 us, pieces of one 44, of three 37)
 constexpr float kFar = 1.15292150460684698e18f;  // 2^60
 
 template <int N>
@@ -265,8 +266,10 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
   const uint32_t tmem = __reduce_or_sync(0xffffffffu, s.tmem);
   const int split = blockIdx.x % p.nsplit, kvh = blockIdx.x / p.nsplit, b = blockIdx.y, layer = blockIdx.z;
   const Seq sq = find_seq(p, b, kPass == 1 && tid == 0 && blockIdx.x == 0 && layer == 0);
-  const int rows_all = sq.n * p.G, ntiles = (sq.len + kTile - 1) / kTile, G = p.G;
-  const int t0 = (int)((long long)split * ntiles / p.nsplit), n = (int)((long long)(split + 1) * ntiles / p.nsplit) - t0;
+  // pieces of kMinTiles tiles at least, whatever the capacity that the launch was sized for
+  const int ntiles = (sq.len + kTile - 1) / kTile, G = p.G, pieces = min(p.nsplit, (ntiles + kMinTiles - 1) / kMinTiles);
+  const int rows_all = split < pieces ? sq.n * G : 0;
+  const int t0 = (int)((long long)split * ntiles / max(pieces, 1)), n = (int)((long long)(split + 1) * ntiles / max(pieces, 1)) - t0;
   const size_t seg = ((size_t)layer * p.B + b) * p.Hkv + kvh;
   float2* const part = p.part + seg * (size_t)(p.max_rows * G) * p.nsplit;
   const bool aligned = (smem_u32(smem_tc) & 1023u) == 0u;  // the swizzled operand regions need a 1 KB aligned base
@@ -323,11 +326,11 @@ __global__ void __launch_bounds__(kThreadsTc, kQ4 ? 4 : 3) mass_tc_kernel(const 
       const float2* pairs = part + (size_t)(r0 + min(row, rows - 1)) * p.nsplit;
       float m = -INFINITY, l = 0.f;
 #pragma unroll 8
-      for (int i = sub; i < p.nsplit; i += 4) m = fmaxf(m, pairs[i].x);
+      for (int i = sub; i < pieces; i += 4) m = fmaxf(m, pairs[i].x);
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
 #pragma unroll 4
-      for (int i = sub; i < p.nsplit; i += 4) {
+      for (int i = sub; i < pieces; i += 4) {
         const float2 x = pairs[i];
         l += x.x == -INFINITY && x.y == 0.f ? 0.f : x.y * exp2f(x.x - m);
       }
