@@ -152,22 +152,31 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
         float f[16] = {};
         if (slot_s[pl] >= 0) load_key_piece<T, D, kQ4>(p, layer, slot_s[pl], ch, f);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) Ks[pl * KS + ch * 16 + e] = f[e];
+        for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(Ks + pl * KS + ch * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       }
       __syncthreads();
+      float acc[2][4] = {};
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {  // (by 16 bytes: the rows lie 16 apart modulo 128, eight threads of them meet no bank twice)
+        float4 a[2], k[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) a[i] = *reinterpret_cast<const float4*>(Qs + (2 * ty + i) * KS + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * j) * KS + d);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = fmaf(a[i].w, k[j].w, fmaf(a[i].z, k[j].z, fmaf(a[i].y, k[j].y, fmaf(a[i].x, k[j].x, acc[i][j]))));
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = 2 * ty + i, row = r0 + r;
-        float acc[4] = {};
-#pragma unroll 8
-        for (int d = 0; d < D; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = fmaf(Qs[r * KS + d], Ks[(tx + 16 * j) * KS + d], acc[j]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int pl = tx + 16 * j, pos = tile * kPT + pl;
           const bool vis = row < rows && slot_s[pl] >= 0 && pos < sq.len - sq.n + row / p.G + 1;
-          Ss[r * SS + pl] = vis ? acc[j] : -INFINITY;
+          Ss[r * SS + pl] = vis ? acc[i][j] : -INFINITY;
         }
       }
       __syncthreads();
