@@ -17,6 +17,8 @@
 // rows: 140 us (12 to read the keys once): bound by the instructions of the codes and the exponentials, issue slots half busy. Slower:
 // three CTAs per SM for the 4-bit pass 1, which then spills nothing (151 us); the next product sent off ahead of this one's scores, with two
 // tiles' scores in tensor memory (153, and 155 for 148 with bf16 keys: the other CTAs hide a product's time already); columns by 24 (159).
+// fp32, 4 layers of 4 sequences of 1000 to 2111: 32 / 8 heads of 128 226 us, 4-bit keys 196 (a warp without rows leaves the products to the
+// others: 291 and 253 before); 8 / 8 heads of 64, 300 to 2111: 81 and 72.
 #include <math.h>
 
 #include "q4_tc.h"
@@ -155,9 +157,10 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
         for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(Ks + pl * KS + ch * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       }
       __syncthreads();
+      const bool any_row = r0 + 4 * warp < rows;  // a warp's four rows, here and below
       float acc[2][4] = {};
 #pragma unroll 4
-      for (int d = 0; d < D; d += 4) {  // (by 16 bytes: the rows lie 16 apart modulo 128, eight threads of them meet no bank twice)
+      for (int d = 0; d < D && any_row; d += 4) {  // (by 16 bytes: the rows lie 16 apart modulo 128, eight threads of them meet no bank twice)
         float4 a[2], k[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) a[i] = *reinterpret_cast<const float4*>(Qs + (2 * ty + i) * KS + d);
@@ -182,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
       __syncthreads();
       if (kPass == 1) {
 #pragma unroll
-        for (int rr = 0; rr < 4; ++rr) {
+        for (int rr = 0; rr < 4 && any_row; ++rr) {
           const int r = 4 * warp + rr;
           const float s0 = Ss[r * SS + lane], s1 = Ss[r * SS + lane + 32];
           float mx = fmaxf(s0, s1);
