@@ -111,7 +111,8 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&x)[kLane
 // The row's codes and its pair, from the D / 16 threads that hold it. The code is the quotient of a division, rounded to nearest
 // even, without dividing: q = d r with the rounded reciprocal r, corrected once by its exact remainder, q + (d - q step) r, is within
 // 2^-46 of the quotient before its last rounding, exact at a tie; and no quotient of a difference and a bf16 step lies nearer than
-// 2^-32 to the place where rounding to fp32 would make a tie of it. Only reciprocals out of range are divided.
+// 2^-32 to the place where rounding to fp32 would make a tie of it. Reciprocals out of range are divided, and rows whose largest
+// value is further from the rounded low than fp32 reaches (hi - lo in range, low below lo): a difference of inf has no remainder.
 template <int LPR, typename R>
 __device__ __forceinline__ uint2 quantise(const R& x, uint32_t& range) {
   float lo, hi;
@@ -133,7 +134,7 @@ __device__ __forceinline__ uint2 quantise(const R& x, uint32_t& range) {
   const float inv = __fdiv_rn(1.f, step);
   constexpr float kMagic = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer, ties to even, in the lowest bits
   uint32_t w[2] = {0u, 0u};
-  if (!(inv < 1e30f)) {
+  if (!(inv < 1e30f) || !(__fsub_rn(hi, low) < INFINITY)) {
 #pragma unroll 1
     for (int e = 0; e < kLane; ++e) {
       float x0 = 0.f;

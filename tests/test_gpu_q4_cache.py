@@ -153,6 +153,32 @@ def test_store_refuses_places_outside(binding):
     assert ctx.cast_poll_status()[0] == 7
 
 
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 0)])
+def test_store_at_the_end_of_the_fp32_range(binding, D, page):
+    """Rows whose span is finite while a value's distance from the rounded low is not: the definition's quotient is infinite
+    there, and its code 15. Bit by bit, with rows just inside of the range beside them."""
+    ends = [(-1.7e38, 1.7026e38), (-3.0e38, 0.4e38), (-1.7e38, 1.70e38), (-2.51e38, 0.89e38), (-0.1e38, 3.3e38), (1e38, 3.3e38)]
+    rng = np.random.default_rng(D)
+    x = np.stack([np.linspace(lo, hi, D).astype(np.float32)[rng.permutation(D)] for lo, hi in ends])
+    with np.errstate(over="ignore"):
+        low = o4.bf16(x.min(-1))
+        assert np.isfinite(x.max(-1) - x.min(-1)).all() and (np.isinf(x.max(-1) - low) == [True, True, False, False, False, False]).all()
+    paged = o4.Paged(rng, 1, len(ends) + 3, page)
+    cache = Cache(rng, paged, 1, 1, D)
+    code, pair = o4.quantise(x)
+    assert (code.max(-1) == 15).all()
+    pg, sl = paged.at(0, np.arange(len(ends)))
+    for w, rows in (("k", slice(None)), ("v", slice(None, None, -1))):
+        cache.code[w][0, pg, 0, sl], cache.pair[w][0, pg, 0, sl] = code[rows], pair[rows]
+    ctx = context(binding, 1)
+    xd = dev(x.reshape(1, 1, len(ends), 1, D))
+    ctx.cast_store_kv_q4(xd, xd.flip(2).contiguous(), 1, 1, len(ends), 1, D, *cache.where(), None, dev(np.array([len(ends)], np.int32)),
+                         cache.kc, cache.kr, cache.vc, cache.vr, *cache.strides)
+    assert ctx.cast_poll_status()[0] == 0
+    for got, want in zip(cache.bits(), cache.host_bits()):
+        np.testing.assert_array_equal(got, want)
+
+
 # ------------------------------------------------------------------------------------------------ attention
 def random_masks(rng, N, cap):
     anc = np.zeros((cap, (cap + 31) // 32), np.uint32)
