@@ -148,7 +148,9 @@ inline bool on_device(const cast_ctx* c) {
   return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
 }
 
-// Grows a workspace (set-up time only: synchronises and allocates); its first `zeroed` bytes start at zero.
+// Grows a workspace (set-up time only: synchronises and allocates); its first `zeroed` bytes are zero when it returns. (The host
+// does not wait for cudaMemset, and streams that do not block on the default one are not ordered behind it: a call enqueued on such a stream would
+// race with the clearing.)
 inline cast_status grow_workspace(void** ws, size_t* have, size_t need, size_t zeroed) {
   if (need <= *have) return CAST_OK;
   CAST_CUDA_OK(cudaDeviceSynchronize());
@@ -156,7 +158,10 @@ inline cast_status grow_workspace(void** ws, size_t* have, size_t need, size_t z
   *ws = nullptr;
   *have = 0;
   CAST_CUDA_OK(cudaMalloc(ws, need));
-  if (zeroed) CAST_CUDA_OK(cudaMemset(*ws, 0, zeroed));
+  if (zeroed) {
+    CAST_CUDA_OK(cudaMemset(*ws, 0, zeroed));
+    CAST_CUDA_OK(cudaDeviceSynchronize());
+  }
   *have = need;
   return CAST_OK;
 }

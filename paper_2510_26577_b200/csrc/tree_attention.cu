@@ -626,18 +626,9 @@ extern "C" cast_status cast_reserve_attention(cast_ctx* c, cast_dtype dtype, int
     const cast_status st = tree_attention_tc_reserve(c, tree_attention_tc_workspace(c, B, Hq, Hkv, D, page_size, seq_capacity));
     if (st != CAST_OK) return st;
   }
-  const size_t need = cc_plan(c, own ? kOwn : kFallback, B, Hq, Hkv, D, page_size, seq_capacity).bytes;
-  if (need > c->attn_ws_bytes) {
-    CAST_CUDA_OK(cudaDeviceSynchronize());
-    if (c->attn_ws) cudaFree(c->attn_ws);
-    c->attn_ws = nullptr;
-    c->attn_ws_bytes = 0;
-    CAST_CUDA_OK(cudaMalloc(&c->attn_ws, need));
-    // tickets start at zero; every merge leaves its ticket at zero again
-    CAST_CUDA_OK(cudaMemset(c->attn_ws, 0, kCcTicketBytes));
-    c->attn_ws_bytes = need;
-  }
-  return CAST_OK;
+  // tickets start at zero; every merge leaves its ticket at zero again
+  return grow_workspace(&c->attn_ws, &c->attn_ws_bytes, cc_plan(c, own ? kOwn : kFallback, B, Hq, Hkv, D, page_size, seq_capacity).bytes,
+                        kCcTicketBytes);
 }
 
 extern "C" cast_status cast_tree_attention_rows(cast_ctx* c, const void* q, const void* k_cache, const void* v_cache,

@@ -1388,16 +1388,8 @@ size_t tree_attention_tc_workspace(const cast_ctx* c, int B, int Hq, int Hkv, in
 }
 // Grows the tensor path's workspace to `bytes` (set-up time only: synchronises and allocates).
 cast_status tree_attention_tc_reserve(cast_ctx* c, size_t bytes) {
-  if (bytes <= c->attn_tc_ws_bytes) return CAST_OK;
-  CAST_CUDA_OK(cudaDeviceSynchronize());
-  if (c->attn_tc_ws) cudaFree(c->attn_tc_ws);
-  c->attn_tc_ws = nullptr;
-  c->attn_tc_ws_bytes = 0;
-  CAST_CUDA_OK(cudaMalloc(&c->attn_tc_ws, bytes));
   // tickets start at zero; every merge leaves its ticket at zero again
-  CAST_CUDA_OK(cudaMemset(c->attn_tc_ws, 0, kTicketBytes));
-  c->attn_tc_ws_bytes = bytes;
-  return CAST_OK;
+  return grow_workspace(&c->attn_tc_ws, &c->attn_tc_ws_bytes, bytes, kTicketBytes);
 }
 
 bool tree_attention_tc_launch(cast_ctx* c, const void* q, const void* k, const void* v, int B, int Hq, int Hkv, int D,

@@ -92,3 +92,14 @@ def test_the_kernels_over_4_bit_caches_allocate_behind_the_wait():
             body = _body(text[m.start():], m.group(1))
             wait = body.index("griddepcontrol.wait")
             assert "return" not in body[:wait] and "p.kv_len[" not in body[:wait], m.group(1)
+
+
+def test_a_workspace_is_cleared_when_the_call_that_reserves_it_returns():
+    """cudaMemset returns ahead of the device, and a stream that does not block on the default one is not ordered behind it: every
+    clearing is followed by a wait, in the one function that grows workspaces and in the one that creates a context."""
+    grow = _body(_source("cast_internal.h"), "cast_status grow_workspace(")
+    assert grow.count("cudaMemset(") == 1 and 0 < grow.index("cudaMemset(") < grow.rindex("cudaDeviceSynchronize()") < grow.index("*have = need")
+    create = _body(_source("cast_api.cu"), "cast_create(")
+    assert create.rindex("dev_alloc(") < create.rindex("cudaDeviceSynchronize()")
+    uses = {n: _source(n).count("cudaMemset(") for n in sorted(os.listdir(CSRC)) if n.endswith((".cu", ".h"))}
+    assert {n: k for n, k in uses.items() if k} == {"cast_internal.h": 1, "cast_api.cu": 1}  # (the latter: dev_alloc's)
