@@ -461,7 +461,8 @@ CAST_API cast_status cast_compact_kv_q4(cast_ctx* ctx, void* k_codes, void* k_ra
  *   mass         [n_layers, B, Hkv, P] fp32, in/out, P = the sequence's capacity in positions (seq_capacity times page_size,
  *                or seq_capacity); positions that no row sees are left untouched
  * Rows are added in a fixed order: the same inputs give the same bits. Needs a workspace (cast_reserve_attention_mass,
- * max_rows >= H+1, or Ncap where accept_path is NULL). bf16 products on the tensor cores, sums in fp32.
+ * max_rows >= H+1, or Ncap where accept_path is NULL), which also serves calls with fewer sequences, layers, rows or kv-heads of the
+ * same Hq / Hkv, and with a smaller capacity. bf16 products on the tensor cores, sums in fp32.
  * Device errors: BAD_TREE (more rows than the path or Ncap holds, a path entry outside [0, Ncap), kv_len[b] < n), BAD_PAGE
  * (kv_len[b] past the capacity): nothing is added for the sequence; a page id out of range: its positions count as masked.
  */

@@ -541,6 +541,15 @@ MassPlan mass_plan(const cast_ctx* c, int B, int n_layers, int max_rows, int Hq,
   pl.bytes = (size_t)base * max_rows * (Hq / Hkv) * pl.nsplit * sizeof(float2);
   return pl;
 }
+// What every call needs at most that has no more sequences, layers, rows and positions than these: base * n of mass_plan goes up and
+// down with base, but stays below 8 SMs + base, and below base times the tiles or kMaxSplit. (By the plan alone a workspace for 5
+// sequences of 32 layers of 8 kv-heads, one piece each, did not hold 4 of them, two pieces each.)
+size_t mass_workspace(const cast_ctx* c, int B, int n_layers, int max_rows, int Hq, int Hkv, const Paging& g) {
+  const long long base = (long long)B * n_layers * Hkv, tiles = (g.max_pos() + kTile - 1) / kTile;
+  long long pieces = base * (tiles < kMaxSplit ? tiles : kMaxSplit);
+  if (pieces > 8ll * c->num_sms + base - 1) pieces = 8ll * c->num_sms + base - 1;
+  return (size_t)pieces * max_rows * (Hq / Hkv) * sizeof(float2);
+}
 
 template <typename T, int D, bool kQ4>
 cast_status launch_mass(cast_ctx* c, const MassParams& p, int n_layers, cudaStream_t s) {
@@ -644,7 +653,7 @@ extern "C" cast_status cast_reserve_attention_mass(cast_ctx* c, cast_dtype dtype
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
   if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll || max_rows > CAST_MAX_TREE) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
-  return grow_workspace(&c->mass_ws, &c->mass_ws_bytes, mass_plan(c, B, n_layers, max_rows, Hq, Hkv, g).bytes, 0);
+  return grow_workspace(&c->mass_ws, &c->mass_ws_bytes, mass_workspace(c, B, n_layers, max_rows, Hq, Hkv, g), 0);
 }
 
 extern "C" cast_status cast_attention_mass(cast_ctx* c, const void* q, const void* k_cache, cast_dtype dtype, int B, int n_layers,

@@ -191,6 +191,37 @@ def test_16_bit_rows_past_four_gigabytes(binding):
     assert not torch.equal(results[1][0], rows[0])
 
 
+@pytest.mark.parametrize("kind,dtype", [("16", "bf16"), ("4", "bf16"), ("4", "f32")])
+def test_mass_workspace_serves_smaller_calls(binding, kind, dtype):
+    """Reserved once for the most sequences, layers and rows, as a server does: calls with fewer of each (among them those
+    that divide a sequence into more pieces), shorter caches and fewer kv-heads run, and give the bits they give after a
+    reservation of their own."""
+    rng = np.random.default_rng(14)
+    Bmax, nlmax, T, Hq, Hkv, D, H = 10, 16, 9, 8, 8, 64, 6
+    ctx = context(binding, Bmax, T, H)
+    ctx.cast_reserve_attention_mass(DT[dtype], Bmax, nlmax, H + 1, Hq, Hkv, D, 16, 20)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    pieces = {b: b * nlmax * Hkv * min(3, -(-8 * sms // (b * nlmax * Hkv))) for b in range(1, Bmax + 1)}
+    assert max(pieces.values()) > pieces[Bmax]  # the case at hand: a smaller call that needs more
+    for B, nl, heads, cap in [(b, nlmax, Hkv, 20) for b in range(Bmax, 0, -1)] + [(Bmax, 9, Hkv, 20), (Bmax, 1, Hkv, 20), (7, 11, 5, 20), (1, 1, 1, 20), (9, nlmax, Hkv, 17)]:
+        paged = o4.Paged(rng, B, cap * 16, 16)
+        cache = Cache(rng, paged, nl, heads, D) if kind == "4" else Dense(rng, paged, nl, heads, D, dtype)
+        q = torch.randn((nl, B, T, heads, D), generator=torch.Generator("cuda").manual_seed(B), device="cuda").to(DT[dtype])
+        path, alen = np.tile(np.arange(H + 1, dtype=np.int32), (B, 1)), rng.integers(0, H + 1, B).astype(np.int32)
+        kv_len = rng.integers(H + 1, cap * 16 + 1, B).astype(np.int32)
+        mass, want = (torch.zeros((nl, B, heads, paged.positions), device="cuda") for _ in range(2))
+        qs, rest = q[0].numel() * q.element_size(), (dev(path), dev(alen), dev(kv_len), 0.0, mass)
+        if kind == "4":
+            ctx.cast_attention_mass_q4(q, cache.kc, cache.kr, B, nl, qs, *cache.strides, heads, heads, D, *cache.where(), *rest)
+        else:
+            ctx.cast_attention_mass(q, cache.k, B, nl, qs, cache.stride, heads, heads, D, *cache.where(), *rest)
+        assert ctx.cast_poll_status()[0] == 0
+        own = context(binding, B, T, H)
+        run_mass(own, cache, q, path, alen, kv_len, want)
+        assert own.cast_poll_status()[0] == 0
+        assert torch.equal(mass, want) and bool((mass.sum((0, 2, 3)) > 0).all())
+
+
 def test_mass_refuses(binding):
     rng = np.random.default_rng(9)
     B, T, Hq, Hkv, D, H = 5, 16, 4, 2, 128, 4
