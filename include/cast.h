@@ -419,7 +419,7 @@ CAST_API cast_status cast_load_kv_q4(cast_ctx* ctx, const void* k_codes, const v
                                      const int32_t* page_table, int seq_capacity, int num_pages, const int32_t* start,
                                      const int32_t* n_rows, void* k, void* v, void* stream);
 
-/* Set-up call, as cast_reserve_attention, for calls of cast_tree_attention_q4 with these arguments. */
+/* Set-up call, as cast_reserve_attention, for calls of cast_tree_attention_q4 with these arguments, and with fewer sequences. */
 CAST_API cast_status cast_reserve_attention_q4(cast_ctx* ctx, cast_dtype dtype, int B, int Hq, int Hkv, int D,
                                                int page_size, int seq_capacity);
 

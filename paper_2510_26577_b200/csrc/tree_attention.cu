@@ -575,8 +575,13 @@ extern "C" cast_status cast_reserve_attention_q4(cast_ctx* c, cast_dtype dtype, 
   if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
   if (dtype == CAST_BF16) return tree_attention_q4_reserve(c, B, Hq, Hkv);
+  size_t need = 0;  // the number of splits, and with it the bytes, may rise as the batch falls
+  for (int b = 1; b <= B; ++b) {
+    const size_t bytes = cc_plan(c, kOwn, b, Hq, Hkv, D, page_size, seq_capacity).bytes;
+    if (bytes > need) need = bytes;
+  }
   // tickets start at zero; every merge leaves its ticket at zero again
-  return grow_workspace(&c->attn_ws, &c->attn_ws_bytes, cc_plan(c, kOwn, B, Hq, Hkv, D, page_size, seq_capacity).bytes, kCcTicketBytes);
+  return grow_workspace(&c->attn_ws, &c->attn_ws_bytes, need, kCcTicketBytes);
 }
 
 extern "C" cast_status cast_tree_attention_q4(cast_ctx* c, const void* q, const void* k_codes, const void* k_range,

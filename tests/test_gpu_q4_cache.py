@@ -435,6 +435,30 @@ def test_attention_without_work_and_with_a_larger_workspace(binding):
     assert ctx.cast_poll_status()[0] == 0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_workspace_serves_fewer_sequences(binding, dtype):
+    """Reserved once for the most sequences: every smaller batch runs, those among them that divide a sequence further, with the
+    bits that it has after a reservation of its own."""
+    rng = np.random.default_rng(24)
+    Bmax, tokens, Hq, Hkv, D = 5, 12, 32, 8, 64
+    ctx = context(binding, Bmax, tokens)
+    ctx.cast_reserve_attention_q4(DT[dtype], Bmax, Hq, Hkv, D, 16, 64)
+    anc, vis = zip(*(random_masks(rng, tokens, tokens) for b in range(Bmax)))
+    for B in range(Bmax, 0, -1):
+        cache = Cache(rng, o4.Paged(rng, B, 1024, 16), 1, Hkv, D)
+        q = torch.randn((B, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(B), device="cuda").to(DT[dtype])
+        kv, n_tree = rng.integers(0, 1024 - tokens, B).astype(np.int32), np.full(B, tokens, np.int32)
+        out = torch.full_like(q, float("nan"))
+        ctx.cast_tree_attention_q4(q, cache.kc[0], cache.kr[0], cache.vc[0], cache.vr[0], B, Hq, Hkv, D, *cache.where(), dev(kv),
+                                   dev(np.stack(anc[:B]).view(np.int32)), dev(n_tree), None, 0.0, out)
+        assert ctx.cast_poll_status()[0] == 0
+        own = context(binding, B, tokens)
+        want = run_attention(own, cache, q, kv, np.stack(anc[:B]), n_tree)
+        assert torch.equal(out, want)
+        if B in (1, 3):
+            check_attention(out, cache, q, kv, vis, n_tree, dtype)
+
+
 def test_attention_needs_its_workspace_and_shapes(binding):
     rng = np.random.default_rng(14)
     cache = Cache(rng, o4.Paged(rng, 1, 4096, 16), 1, 2, 128)
