@@ -224,11 +224,9 @@ __global__ void __launch_bounds__(kThreads) tree_attn_cc_kernel(const AttnParams
   const int row0 = rb * kRB;
   if (row0 >= rows_total) return;
   const int max_pos = p.page_size == 0 ? p.seq_capacity : p.seq_capacity * p.page_size;
-  int total = L + N;
-  if (total > max_pos) {
-    if (tid == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
-    total = max_pos;
-  }
+  int total = max_pos;
+  if ((long long)L + N <= max_pos) total = L + N;
+  else if (tid == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
   const int ntiles = (total + kPT - 1) / kPT;
   const int t0 = (int)((long long)split * ntiles / p.nsplit), t1 = (int)((long long)(split + 1) * ntiles / p.nsplit);
 

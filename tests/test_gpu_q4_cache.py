@@ -351,6 +351,23 @@ def test_attention_reports_and_masks_bad_pages(binding, dtype):
     assert ctx.cast_poll_status() == (6, 1)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_reports_lengths_past_32_bits(binding, dtype):
+    """A length whose sum with the tree leaves the 32-bit integers is past the capacity like any other; the batch's other
+    sequence is what it is."""
+    rng = np.random.default_rng(25)
+    cache = Cache(rng, o4.Paged(rng, 2, 100, 16), 1, 2, 64)
+    q = torch.randn((2, 5, 4, 64), generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(DT[dtype])
+    anc, vis = zip(*(random_masks(rng, 5, 5) for b in range(2)))
+    ctx, n_tree = context(binding, 2, 5), np.array([5, 5], np.int32)
+    want = run_attention(ctx, cache, q, np.array([60, 90], np.int32), np.stack(anc), n_tree)
+    assert ctx.cast_poll_status()[0] == 0
+    for far in (2 ** 31 - 1, 2 ** 31 - 5, 2 ** 31 - 6):
+        out = run_attention(ctx, cache, q, np.array([far, 90], np.int32), np.stack(anc), n_tree)
+        assert ctx.cast_poll_status() == (7, 0)
+        assert torch.equal(out[1], want[1])
+
+
 @pytest.mark.parametrize("dtype,D,lens", [("bf16", 128, [2100, 3]), ("bf16", 64, [1500, 0]), ("f32", 64, [700, 3]), ("f32", 128, [2100, 0])])
 def test_attention_nan_and_infinity(binding, dtype, D, lens):
     """A query row of NaN gives NaN, however its sequence is divided, and so do keys without a value that fill whole tiles; a
