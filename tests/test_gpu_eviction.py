@@ -119,6 +119,98 @@ def test_mass(binding, kind, dtype, Hq, Hkv, D, page, depth, accepted, lens):
     check_mass(again, mass, cache, q, path, alen, kv_len)
 
 
+@pytest.mark.parametrize("kind,dtype,Hq,Hkv,D,page,depth,accepted,lens", [
+    ("4", "bf16", 7, 1, 64, 0, 13, [13, 5], [1100, 517]),
+    ("4", "bf16", 8, 2, 128, 0, 6, [3, 0, 6, -1], [200, 1, 65, 40]),
+    ("16", "bf16", 28, 4, 128, 0, 6, [2, 6], [2200, 127]),
+    ("16", "bf16", 8, 2, 64, 24, 6, [3, 0, 6, -1], [200, 1, 65, 40]),
+    ("16", "bf16", 7, 1, 64, 1, 13, [13, 5], [1100, 517]),
+    ("4", "f32", 8, 8, 64, 0, 4, [4, 2], [300, 129]),
+])
+def test_mass_in_other_layouts(binding, kind, dtype, Hq, Hkv, D, page, depth, accepted, lens):
+    test_mass(binding, kind, dtype, Hq, Hkv, D, page, depth, accepted, lens)
+
+
+class Kept(Dense):
+    """A cache whose rows are brought to the host once."""
+
+    def rows(self, which, layer, b, h, n):
+        if not hasattr(self, "host"):
+            self.host = self.k.float().cpu().numpy()
+        page, slot = self.paged.at(b, np.arange(n))
+        return self.host[layer][page, slot, h].astype(np.float64), None
+
+
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 0)])
+@pytest.mark.parametrize("kind,dtype", [("16", "bf16"), ("4", "bf16"), ("16", "f32"), ("4", "f32")])
+def test_mass_far_scores(binding, kind, dtype, D, page):
+    """Scores that climb by hundreds from tile to tile and fall again, several tiles to a piece and two pieces to a sequence: a
+    row's reference has to follow within a piece, and pieces with references far apart have to meet."""
+    rng = np.random.default_rng(16)
+    nl, T, Hq, Hkv, H = 16, 6, 16, 8, 2
+    lens = np.array([1000, 517, 130, 900, 1003], np.int32)
+    B = len(lens)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert 2 <= -(-8 * sms // (B * nl * Hkv)) <= 2  # pieces, of 4 tiles of 128 in the longest
+    paged = o4.Paged(rng, B, 1010, page)
+    cache = Cache(rng, paged, nl, Hkv, D) if kind == "4" else Kept(rng, paged, nl, Hkv, D, dtype)
+    pos = np.arange(1010)
+    lift = (np.where(pos % 700 < 350, pos % 350, 0) * 0.25).astype(np.float32)
+    for b in range(B):
+        pg, sl = paged.at(b, pos)
+        if kind == "4":
+            cache.pair["k"][:, pg, :, sl, 1] += lift[:, None, None]
+        else:
+            cache.k[:, torch.from_numpy(pg).cuda(), torch.from_numpy(sl).cuda()] += torch.from_numpy(lift).cuda().to(DT[dtype])[:, None, None]
+    if kind == "4":
+        cache.pair["k"] = o4.bf16(cache.pair["k"])
+        cache.upload()
+    q = torch.rand((nl, B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(2), device="cuda").to(DT[dtype])
+    path, alen = np.tile(np.array([[0, 2, 5]], np.int32), (B, 1)), np.array([2, 0, 2, 1, 2], np.int32)
+    mass = torch.zeros((nl, B, Hkv, paged.positions), device="cuda")
+    ctx = context(binding, B, T, H)
+    run_mass(ctx, cache, q, path, alen, lens, mass)
+    assert ctx.cast_poll_status()[0] == 0
+    check_mass(mass, torch.zeros_like(mass), cache, q, path, alen, lens)
+
+
+@pytest.mark.parametrize("kind,dtype", [("16", "bf16"), ("4", "bf16"), ("16", "f32"), ("4", "f32")])
+def test_mass_beside_bad_pages(binding, kind, dtype):
+    """Pages that are none: the first tile of a piece, a whole piece and the beginning of the next, a tile in the middle, all of
+    a sequence. Their positions count as masked, draw nothing, and the others share what the rows give."""
+    rng = np.random.default_rng(17)
+    nl, T, Hq, Hkv, D, H, L = 2, 8, 8, 2, 128, 4, 1000
+    bad = [np.arange(128), np.arange(304), np.arange(512, 640), np.arange(L + 16), np.zeros(0, int)]
+    B = len(bad)
+    paged = o4.Paged(rng, B, L + 20, 16)
+    cache = Cache(rng, paged, nl, Hkv, D) if kind == "4" else Kept(rng, paged, nl, Hkv, D, dtype)
+    good = paged.table.copy()
+    q = torch.randn((nl, B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(5), device="cuda").to(DT[dtype])
+    path, alen, kv_len = np.tile(np.array([[0, 2, 5, 6, 7]], np.int32), (B, 1)), np.array([4, 2, 0, 3, 1], np.int32), np.full(B, L, np.int32)
+    for b, pos in enumerate(bad):
+        paged.table[b, pos // 16] = rng.choice([-1, paged.pages, 2 ** 31 - 1], len(pos))
+    mass = torch.zeros((nl, B, Hkv, paged.positions), device="cuda")
+    ctx = context(binding, B, T, H)
+    run_mass(ctx, cache, q, path, alen, kv_len, mass)
+    assert ctx.cast_poll_status()[0] == 7
+    paged.table = good
+    got, x = mass.double().cpu().numpy(), q.double().cpu().numpy()
+    for l in range(nl):
+        for b in range(B):
+            n = int(alen[b]) + 1
+            for h in range(Hkv):
+                k = cache.rows("k", l, b, h, L)[0]
+                keep = np.setdiff1d(np.arange(L), bad[b])
+                qh = x[l, b, path[b, :n], h * 4:h * 4 + 4]
+                want = np.zeros(L)
+                # a row sees the kept positions below its own bound: as many of them as lie there
+                if len(keep):
+                    want[keep] = o4.mass_of(qh, k[keep], [(keep < L - n + i + 1).sum() for i in range(n)], D ** -0.5)
+                s_err = D * 2.0 ** -24 * np.einsum("tgd,pd->tgp", np.abs(qh), np.abs(k)).max() * D ** -0.5
+                tol = want * (2 * s_err + 2.0 ** -19 + (n * 4 + 2) * 2.0 ** -24) + 1e-30
+                assert (np.abs(got[l, b, h, :L] - want) <= tol).all() and not got[l, b, h, L:].any()
+
+
 @pytest.mark.parametrize("kind", ["16", "4"])
 def test_mass_of_a_window_of_rows(binding, kind):
     """Without a path: the last rows of a prompt chunk, more of them than one block of the kernels."""

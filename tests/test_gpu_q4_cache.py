@@ -267,6 +267,59 @@ def test_attention(binding, dtype, Hq, Hkv, D, page, tokens, lens):
     assert torch.equal(out.view(torch.uint8), again.view(torch.uint8))  # the same bits every time
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,tokens,lens", [(32, 8, 128, 60, [2048]), (14, 2, 128, 20, [5, 300, 129]), (8, 8, 128, 1, [400, 0, 7])])
+def test_attention_of_unpaged_heads_of_128(binding, Hq, Hkv, D, tokens, lens):
+    test_attention(binding, "bf16", Hq, Hkv, D, 0, tokens, lens)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,page,tokens,lens", [
+    (32, 8, 128, 16, 12, None),
+    (32, 8, 64, 0, 12, None),
+    (28, 4, 128, 0, 96, [1100, 1150, 1180]),
+    (28, 4, 64, 24, 96, [1180, 1110, 1150]),
+])
+def test_attention_cut_evenly(binding, Hq, Hkv, D, page, tokens, lens):
+    """More work than thread blocks: the line of tiles is cut without regard to where items end, so a block holds the end of one
+    item and the beginning of another, wide and narrow ones, and hands over two partials. Without lengths: many ragged sequences,
+    some with nothing to do; else few items, long enough for several blocks each."""
+    rng = np.random.default_rng(D + tokens)
+    if lens is None:
+        lens = rng.integers(0, 700, 64)
+        n_tree = rng.integers(0, tokens + 1, 64).astype(np.int32)
+        n_tree[:8] = [12, 4, 0, 1, 5, 0, 0, 12]   # 16 query rows and fewer beside more
+        lens[:3] = [0, 1, 650]
+    else:
+        n_tree = np.full(len(lens), tokens, np.int32)
+    B, kv_len = len(lens), np.array(lens, np.int32)
+    items = Hkv * (-(-n_tree * (Hq // Hkv) // 48))      # (48 query rows to an item, 128 positions to a tile)
+    tiles = np.where(n_tree > 0, -(-(kv_len + n_tree) // 128), 0)
+    grid = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    longest = max(3, -(-int((items * tiles).sum()) // grid), -(-int(tiles.max()) // 32)) + 3
+    assert (items * -(-tiles // longest)).sum() > grid  # or items would be cut one by one
+    cache = Cache(rng, o4.Paged(rng, B, max(lens) + tokens, page), 1, Hkv, D)
+    anc, vis = zip(*(random_masks(rng, n_tree[b], tokens) for b in range(B)))
+    q = torch.randn((B, tokens, Hq, D), generator=torch.Generator("cuda").manual_seed(tokens), device="cuda").to(torch.bfloat16)
+    ctx = context(binding, B, tokens)
+    out = run_attention(ctx, cache, q, kv_len, np.stack(anc), n_tree)
+    assert ctx.cast_poll_status()[0] == 0
+    check_attention(out, cache, q, kv_len, vis, n_tree, "bf16")
+    # the same bits again, but for query rows of NaN, in every sequence and so in items that several blocks share
+    q2, spoilt = q.clone(), torch.zeros((B, tokens, Hq), dtype=torch.bool)
+    for b in range(B):
+        if n_tree[b]:
+            spoilt[b, int(rng.integers(n_tree[b])), torch.from_numpy(rng.integers(0, Hq, 3))] = True
+    q2[spoilt.cuda()] = float("nan")
+    again = run_attention(ctx, cache, q2, kv_len, np.stack(anc), n_tree)
+    assert ctx.cast_poll_status()[0] == 0
+    assert bool(torch.isnan(again[spoilt.cuda()]).all())
+    left = ~spoilt.cuda()
+    assert torch.equal(again[left].view(torch.int16), out[left].view(torch.int16))
+    # and a window of the rows, whose first tokens are context alone
+    first = np.minimum(n_tree, rng.integers(0, tokens, B)).astype(np.int32)
+    check_attention(run_attention(ctx, cache, q, kv_len, np.stack(anc), n_tree, first, 0.2), cache, q, kv_len, vis, n_tree, "bf16", first, 0.2)
+    assert ctx.cast_poll_status()[0] == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [0.3, 4.0, -0.5])
 def test_attention_window_scale_and_odd_masks(binding, dtype, scale):
