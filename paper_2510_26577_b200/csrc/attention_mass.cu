@@ -34,7 +34,7 @@ constexpr int kMaxSplit = 64;
 
 struct MassParams {
   const void* q;
-  const unsigned char* k;    // 16-bit or fp32 rows, or codes
+  const unsigned char* k;    // bf16 or fp32 rows (as the queries are), or codes
   const uint32_t* range;     // 4-bit caches: the pairs
   size_t q_stride, k_stride, range_stride;  // bytes per layer
   int B, Ncap, Hq, Hkv, G, max_rows, nsplit, path_stride;
@@ -70,7 +70,8 @@ __device__ __forceinline__ Seq find_seq(const MassParams& p, int b, bool say) {
   return s;
 }
 
-template <typename T, int D, bool kQ4>
+// Sixteen dims of a key row of a fp32 or 4-bit cache.
+template <int D, bool kQ4>
 __device__ __forceinline__ void load_key_piece(const MassParams& p, int layer, long long row, int ch, float (&f)[16]) {
   if constexpr (kQ4) {
     const uint32_t r = *(reinterpret_cast<const uint32_t*>(reinterpret_cast<const unsigned char*>(p.range) + p.range_stride * layer) + row);
@@ -79,19 +80,16 @@ __device__ __forceinline__ void load_key_piece(const MassParams& p, int layer, l
 #pragma unroll
     for (int e = 0; e < 16; ++e) f[e] = fmaf(step, (float)(((e < 8 ? w.x : w.y) >> (4 * (e % 8))) & 15u), low);
   } else {
-    const T* src = reinterpret_cast<const T*>(p.k + p.k_stride * layer) + row * D + ch * 16;
+    const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.k + p.k_stride * layer) + row * D + ch * 16);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) {
-      const uint4 a = reinterpret_cast<const uint4*>(src)[i];
-      float x[Vec<T>::N];
-      Vec<T>::unpack(a, x);
-#pragma unroll
-      for (int e = 0; e < Vec<T>::N; ++e) f[i * Vec<T>::N + e] = x[e];
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = src[i];
+      f[4 * i] = x.x; f[4 * i + 1] = x.y; f[4 * i + 2] = x.z; f[4 * i + 3] = x.w;
     }
   }
 }
 
-template <typename T, int D, bool kQ4, int kPass>
+template <int D, bool kQ4, int kPass>
 __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
   constexpr int KS = D + 4, SS = kPT + 4;
   extern __shared__ __align__(16) float smem[];
@@ -113,13 +111,13 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
   const int ty = tid / 16, tx = tid % 16;
   for (int r0 = 0; r0 < rows; r0 += kRB) {
     __syncthreads();
-    const T* q = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(p.q) + p.q_stride * layer);
+    const float* q = reinterpret_cast<const float*>(reinterpret_cast<const unsigned char*>(p.q) + p.q_stride * layer);
     for (int i = tid; i < kRB * D; i += kThreads) {
       const int r = i / D, d = i % D, row = r0 + r;
       float x = 0.f;
       if (row < rows) {
         const int j = row / p.G, t = p.path ? p.path[(size_t)b * p.path_stride + j] : j;
-        x = to_float(q[(((size_t)b * p.Ncap + t) * p.Hq + kvh * p.G + row % p.G) * D + d]) * p.scale;
+        x = q[(((size_t)b * p.Ncap + t) * p.Hq + kvh * p.G + row % p.G) * D + d] * p.scale;
       }
       Qs[r * KS + d] = x;
     }
@@ -152,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) mass_kernel(const MassParams p) {
       for (int i = tid; i < kPT * (D / 16); i += kThreads) {
         const int pl = i / (D / 16), ch = i % (D / 16);
         float f[16] = {};
-        if (slot_s[pl] >= 0) load_key_piece<T, D, kQ4>(p, layer, slot_s[pl], ch, f);
+        if (slot_s[pl] >= 0) load_key_piece<D, kQ4>(p, layer, slot_s[pl], ch, f);
 #pragma unroll
         for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(Ks + pl * KS + ch * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       }
@@ -551,8 +549,8 @@ size_t mass_workspace(const cast_ctx* c, int B, int n_layers, int max_rows, int 
   return (size_t)pieces * max_rows * (Hq / Hkv) * sizeof(float2);
 }
 
-template <typename T, int D, bool kQ4>
-cast_status launch_mass(cast_ctx* c, const MassParams& p, int n_layers, cudaStream_t s) {
+template <int D, bool kQ4>
+cast_status launch_mass(const MassParams& p, int n_layers, cudaStream_t s) {
   const size_t smem = (size_t)(kRB * (D + 4) + kPT * (D + 4) + kRB * (kPT + 4)) * sizeof(float);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.Hkv * p.nsplit, p.B, n_layers);
@@ -564,10 +562,10 @@ cast_status launch_mass(cast_ctx* c, const MassParams& p, int n_layers, cudaStre
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  CAST_CUDA_OK(cudaFuncSetAttribute(mass_kernel<T, D, kQ4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  CAST_CUDA_OK(cudaFuncSetAttribute(mass_kernel<T, D, kQ4, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  cudaError_t e = cudaLaunchKernelEx(&cfg, mass_kernel<T, D, kQ4, 1>, p);
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, mass_kernel<T, D, kQ4, 2>, p);
+  CAST_CUDA_OK(cudaFuncSetAttribute(mass_kernel<D, kQ4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CAST_CUDA_OK(cudaFuncSetAttribute(mass_kernel<D, kQ4, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  cudaError_t e = cudaLaunchKernelEx(&cfg, mass_kernel<D, kQ4, 1>, p);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, mass_kernel<D, kQ4, 2>, p);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return CAST_ERR_CUDA;
@@ -639,8 +637,8 @@ cast_status mass_call(cast_ctx* c, const void* q, const void* k, const void* ran
     if (q4) return D == 64 ? launch_mass_tc<64, true>(p, n_layers, s) : launch_mass_tc<128, true>(p, n_layers, s);
     return D == 64 ? launch_mass_tc<64, false>(p, n_layers, s) : launch_mass_tc<128, false>(p, n_layers, s);
   }
-  if (q4) return D == 64 ? launch_mass<float, 64, true>(c, p, n_layers, s) : launch_mass<float, 128, true>(c, p, n_layers, s);
-  return D == 64 ? launch_mass<float, 64, false>(c, p, n_layers, s) : launch_mass<float, 128, false>(c, p, n_layers, s);
+  if (q4) return D == 64 ? launch_mass<64, true>(p, n_layers, s) : launch_mass<128, true>(p, n_layers, s);
+  return D == 64 ? launch_mass<64, false>(p, n_layers, s) : launch_mass<128, false>(p, n_layers, s);
 }
 
 }  // namespace
