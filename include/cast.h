@@ -33,7 +33,8 @@
  *    work: they never synchronise the host. Tree sizes (n_i, go/no-go, N) are
  *    decided on the device and stay there.
  *  - Compute calls allocate nothing. The split workspace of the attention is
- *    sized at set-up time by cast_reserve_attention; an attention call whose
+ *    sized at set-up time by cast_reserve_attention (of the attention over 4-bit
+ *    caches and of the attention mass by calls of their own); a call whose
  *    shape needs more than was reserved returns CAST_ERR_CAPACITY.
  *  - The return value reports errors the host can see (bad arguments, caps).
  *    Errors only the device can see (non-finite logits, a malformed tree, a
@@ -391,8 +392,9 @@ CAST_API cast_status cast_accept_static(const void* target_logits, cast_dtype dt
  * pairs range_stride_bytes * l; calls that take one layer take the layer's pointers.
  * Codes 16-byte aligned (code_stride_bytes a multiple of 16), pairs 4-byte aligned; D in {64, 128}.
  * These calls and those of the eviction want the context's device to be the current one (else INVALID_ARG), are launched with
- * programmatic dependent launch, read nothing before their predecessor on the stream has completed, and count rows of the cache in
- * 32 bits: a layer of 2^32 rows (positions times kv-heads) or more, and B * Ncap * Hq * D past 2^31, are CAPACITY.
+ * programmatic dependent launch and read nothing before their predecessor on the stream has completed. CAPACITY: B beyond max_batch;
+ * a sequence of more than 2^31 - 2^16 positions; a layer of 2^32 rows (positions times kv-heads) or more, which all but the compaction and the
+ * attention with fp32 queries count in 32 bits; and, for the attention with bf16 queries, B * Ncap * Hq * D past 2^31.
  *
  * cast_store_kv_q4: rows t < n_rows[b] of k, v [n_layers, B, rows, Hkv, D] (dtype `dtype`) to positions
  * start[b] + t (start NULL: 0). Per row, in fp32: lo, hi its least and largest value, low = bf16(lo),

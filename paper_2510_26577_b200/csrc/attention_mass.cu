@@ -613,7 +613,7 @@ cast_status mass_call(cast_ctx* c, const void* q, const void* k, const void* ran
       g.page_size < 0 || g.seq_capacity < 1 || (g.page_size > 0 && (!g.table || g.num_pages < 1)) || !on_device(c))
     return CAST_ERR_INVALID_ARG;
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
-  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll || n_layers > 65535) return CAST_ERR_CAPACITY;
+  if (B > c->cfg.max_batch || g.max_pos() > kMaxPositions || n_layers > 65535) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
   if (((uintptr_t)q | (uintptr_t)k | q_stride | k_stride) & 15 || ((uintptr_t)range | range_stride) & 3) return CAST_ERR_SHAPE;
   MassParams p;
@@ -649,7 +649,7 @@ extern "C" cast_status cast_reserve_attention_mass(cast_ctx* c, cast_dtype dtype
   if (!c || B < 1 || n_layers < 1 || max_rows < 1 || Hq < 1 || Hkv < 1 || page_size < 0 || seq_capacity < 1 || !on_device(c))
     return CAST_ERR_INVALID_ARG;
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
-  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll || max_rows > CAST_MAX_TREE) return CAST_ERR_CAPACITY;
+  if (B > c->cfg.max_batch || g.max_pos() > kMaxPositions || max_rows > CAST_MAX_TREE) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
   return grow_workspace(&c->mass_ws, &c->mass_ws_bytes, mass_workspace(c, B, n_layers, max_rows, Hq, Hkv, g), 0);
 }

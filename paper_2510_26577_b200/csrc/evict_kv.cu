@@ -305,7 +305,7 @@ extern "C" cast_status cast_evict_kv(cast_ctx* c, void* k_cache, void* v_cache, 
       !on_device(c))
     return CAST_ERR_INVALID_ARG;
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
-  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  if (B > c->cfg.max_batch || g.max_pos() > kMaxPositions) return CAST_ERR_CAPACITY;
   if (D != 64 && D != 128) return CAST_ERR_SHAPE;
   if (((uintptr_t)k_cache | (uintptr_t)v_cache | layer_stride_bytes) & 15) return CAST_ERR_SHAPE;
   const int rb = D * (dtype == CAST_F32 ? 4 : 2);

@@ -14,6 +14,9 @@ struct Paging {
   }
 };
 
+// Positions of a sequence at most: below 2^31 by more than a tile or a round of a kernel, whose last indices may lie past the end.
+constexpr long long kMaxPositions = (1ll << 31) - (1ll << 16);
+
 // Page and slot of position `pos` of sequence b (0 <= pos < max_pos); false for a page id out of range.
 __device__ __forceinline__ bool find_place(const Paging& g, int b, int pos, int& page, int& slot) {
   if (g.page_size == 0) {
@@ -65,7 +68,7 @@ inline cast_status check_q4(const cast_ctx* c, int B, int Hkv, int D, const Pagi
   if (!c || !kc || !kr || !vc || !vr || B < 1 || Hkv < 1 || g.page_size < 0 || g.seq_capacity < 1 ||
       (g.page_size > 0 && (!g.table || g.num_pages < 1)) || !on_device(c))
     return CAST_ERR_INVALID_ARG;
-  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  if (B > c->cfg.max_batch || g.max_pos() > kMaxPositions) return CAST_ERR_CAPACITY;
   if (D != 64 && D != 128) return CAST_ERR_SHAPE;
   if (((uintptr_t)kc | (uintptr_t)vc | code_stride) & 15 || ((uintptr_t)kr | (uintptr_t)vr | range_stride) & 3)
     return CAST_ERR_SHAPE;

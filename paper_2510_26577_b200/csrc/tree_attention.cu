@@ -570,7 +570,7 @@ extern "C" cast_status cast_reserve_attention_q4(cast_ctx* c, cast_dtype dtype, 
   if (!c || B < 1 || Hq < 1 || Hkv < 1 || page_size < 0 || seq_capacity < 1 || !on_device(c)) return CAST_ERR_INVALID_ARG;
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
   const Paging g = {nullptr, page_size, seq_capacity, 0};
-  if (B > c->cfg.max_batch || g.max_pos() > 0x7fffffffll) return CAST_ERR_CAPACITY;
+  if (B > c->cfg.max_batch || g.max_pos() > kMaxPositions) return CAST_ERR_CAPACITY;
   if (Hq % Hkv != 0 || (D != 64 && D != 128)) return CAST_ERR_SHAPE;
   if (dtype == CAST_BF16) return tree_attention_q4_reserve(c, B, Hq, Hkv);
   size_t need = 0;  // the number of splits, and with it the bytes, may rise as the batch falls

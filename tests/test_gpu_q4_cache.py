@@ -563,6 +563,42 @@ def test_attention_needs_its_workspace_and_shapes(binding):
     assert ctx.cast_poll_status()[0] == 0
 
 
+def test_sequences_too_long_for_32_bit_positions(binding):
+    """The most positions that a sequence may have, and one more, by pages and without: refused by every call, before anything
+    runs, since the kernels' indices run past a sequence's end by a tile."""
+    B, T, H, D, most = 1, 4, 4, 64, 2 ** 31 - 2 ** 16
+    ctx = context(binding, B, T, H)
+    x, q = (torch.ones((1, B, T, n, D), device="cuda", dtype=torch.bfloat16) for n in (1, 2))
+    kc, vc = (torch.zeros((1, B, 1, 16, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2))
+    kr, vr = (torch.zeros((1, B, 1, 16, 2), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dense = torch.ones((1, B, 16, 1, D), device="cuda", dtype=torch.bfloat16)
+    cache, strides = (kc, kr, vc, vr), (kc.numel(), kr.numel() * 2)
+    n, one, path = dev(np.array([T], np.int32)), dev(np.array([0], np.int32)), torch.zeros((B, H + 1), dtype=torch.int32, device="cuda")
+    anc, table = torch.ones((B, T, 1), dtype=torch.int32, device="cuda"), torch.zeros((B, 16), dtype=torch.int32, device="cuda")
+    out, mass, kept = torch.zeros_like(q[0]), torch.zeros(16, device="cuda"), torch.zeros(16, dtype=torch.int32, device="cuda")
+    calls = [
+        lambda w: ctx.cast_reserve_attention_q4(torch.bfloat16, B, 2, 1, D, w[0], w[2]),
+        lambda w: ctx.cast_reserve_attention_q4(torch.float32, B, 2, 1, D, w[0], w[2]),
+        lambda w: ctx.cast_reserve_attention_mass(torch.bfloat16, B, 1, H + 1, 2, 1, D, w[0], w[2]),
+        lambda w: ctx.cast_store_kv_q4(x, x, B, 1, T, 1, D, *w, None, n, *cache, *strides),
+        lambda w: ctx.cast_load_kv_q4(*cache, *strides, B, 1, T, 1, D, *w, None, n, x.clone(), x.clone()),
+        lambda w: ctx.cast_tree_attention_q4(q[0], kc, kr, vc, vr, B, 2, 1, D, *w, one, anc, n, None, 0.0, out),
+        lambda w: ctx.cast_compact_kv_q4(*cache, *strides, B, 1, 1, D, *w, path, one, n.clone()),
+        lambda w: ctx.cast_attention_mass_q4(q, kc, kr, B, 1, 0, *strides, 2, 1, D, *w, path, one, n, 0.0, mass),
+        lambda w: ctx.cast_attention_mass(q, dense, B, 1, 0, 0, 2, 1, D, *w, path, one, n, 0.0, mass),
+        lambda w: ctx.cast_evict_kv_q4(*cache, *strides, B, 1, 1, D, *w, 8, 2, mass, kept, n),
+        lambda w: ctx.cast_evict_kv(dense, dense.clone(), B, 1, 0, 1, D, *w, 8, 2, mass, kept, n),
+    ]
+    for where in ((0, None, most + 1, 0), (1 << 15, table, (1 << 16) - 1, 1)):
+        for i, call in enumerate(calls):
+            with pytest.raises(binding.CastError) as e:
+                call(where)
+            assert e.value.code == 3, i
+    for call in calls:  # (a few positions of it are there)
+        call((0, None, most, 0))
+    assert ctx.cast_poll_status()[0] == 0
+
+
 # ------------------------------------------------------------------------------------------------ compaction
 @pytest.mark.parametrize("D,page,Hkv", [(128, 16, 8), (64, 0, 2), (128, 5, 1)])
 def test_compaction(binding, D, page, Hkv):
