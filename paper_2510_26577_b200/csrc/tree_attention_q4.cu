@@ -6,8 +6,8 @@
 // so a score carries no rounding but the accumulation's, and a weight (times its row's step) one to bf16; the last sum stays in fp32.
 //
 // Positions are the rows of both products, queries the columns: S^T = C_k Q^T (128 positions x N queries) and
-// O^T = C_v^T P^T (dims x N). A query column is a (tree token, head of the GQA group) pair, up to 48 per work item, N rounded up to
-// 16: a small tree costs what it has, not a block of 128 rows, and its exponentials spread over all lanes. A thread of the softmax
+// O^T = C_v^T P^T (dims x N). A query column is a (tree token, head of the GQA group) pair, up to 48 per work item; N is 16 for items of
+// up to 16 of them and 48 otherwise: a small tree costs that, not a block of 128 rows, and its exponentials spread over all lanes. A thread of the softmax
 // owns one position: step and low are scalars of its own, masks are one word per position, and sums run in registers over
 // all its tiles, reduced across lanes once per item. What is paid for that: the maximum of a column lies across lanes, so the
 // running reference of a column is not its maximum but the first visible tile's, moved when a weight reaches 2^60 (bf16 and fp32 have
