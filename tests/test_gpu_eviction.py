@@ -518,3 +518,52 @@ def test_mass_then_eviction_then_attention(binding, kind, captured):
                     k, v = rows["k"][l][b][h][mine], rows["v"][l][b][h][mine]
                     want, _ = o4.attend(x[1, b, :, h * 4:h * 4 + 4], k, v, v, len(mine), np.zeros((T, 0), bool), D ** -0.5)
                     assert np.abs(got[b, :, h * 4:h * 4 + 4] - want).max() < 2e-2
+
+
+def test_early_reads_beside_the_new_calls(binding):
+    """With early reads promised: attention over the 16-bit cache right behind rows that came out of a 4-bit cache, behind the
+    weights of the accepted rows, and behind an eviction - with the bits of a context without the promise that waits for
+    every call."""
+    rng = np.random.default_rng(40)
+    B, cap, T, Hq, Hkv, D, H, budget = 4, 2048, 12, 32, 8, 128, 4, 700
+    paged = o4.Paged(rng, B, cap, 0)
+    stores = [Cache(rng, paged, 1, Hkv, D) for _ in range(2)]
+    q = torch.randn((1, B, T, Hq, D), generator=torch.Generator("cuda").manual_seed(9), device="cuda").to(torch.bfloat16)
+    lens = np.array([2030, 1500, 701, 12], np.int32)
+    anc = torch.ones((B, T, 1), dtype=torch.int32, device="cuda")
+    n_tree, all_rows, path, alen = dev(np.full(B, T, np.int32)), dev(np.full(B, cap, np.int32)), dev(np.tile(np.arange(H + 1, dtype=np.int32), (B, 1))), dev(np.array([4, 2, 0, 1], np.int32))
+
+    def run(promise):
+        ctx = context(binding, B, T, H)
+        ctx.cast_reserve_attention(torch.bfloat16, B, Hq, Hkv, D, 0, cap)
+        ctx.cast_reserve_attention_mass(torch.bfloat16, B, 1, H + 1, Hq, Hkv, D, 0, cap)
+        ctx.cast_set_attention_early_reads(promise)
+        k, v = (torch.zeros((1, B, cap, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        where, kv_len = (0, None, cap, 0), dev(lens)
+        mass, kept = torch.zeros((1, B, Hkv, cap), device="cuda"), torch.zeros((1, B, Hkv, budget), dtype=torch.int32, device="cuda")
+        outs = torch.zeros((12, *q.shape), dtype=torch.bfloat16, device="cuda")
+        at = iter(outs)
+        torch.cuda.synchronize()
+
+        def between():
+            if not promise:
+                torch.cuda.synchronize()
+
+        def attend():
+            between()
+            ctx.cast_tree_attention(q[0], k[0], v[0], B, Hq, Hkv, D, *where, kv_len, anc, n_tree, 0.0, next(at)[0])
+            between()
+
+        for c in stores + stores:
+            ctx.cast_load_kv_q4(c.kc, c.kr, c.vc, c.vr, *c.strides, B, 1, cap, Hkv, D, *where, None, all_rows, k, v)
+            attend()
+            ctx.cast_attention_mass(q, k, B, 1, q.numel() * 2, k.numel() * 2, Hq, Hkv, D, *where, path, alen, kv_len, 0.0, mass)
+            attend()
+            ctx.cast_evict_kv(k, v, B, 1, k.numel() * 2, Hkv, D, *where, budget, 100, mass, kept, kv_len)
+            attend()
+        assert ctx.cast_poll_status()[0] == 0
+        np.testing.assert_array_equal(kv_len.cpu().numpy(), np.minimum(lens, budget))
+        return outs, mass, kept
+
+    for a, b in zip(run(True), run(False)):
+        assert torch.equal(a, b) and bool(a.any())
