@@ -14,7 +14,7 @@
 //
 // Measured: 8 layers of 8 sequences of 1024 to 4096, 28 rows of bf16 per kv-head at most, 32 / 8 heads of 128: 140 us (54 to read the
 // keys once; the two passes read 350 MB each at 58 % of the memory's rate). 2 layers of 4 sequences of 32768 in 4 bits, 28 / 4 heads, up to 49
-// rows: 140 us (12 to read the keys once): bound by the instructions of the codes and the exponentials, issue slots half busy. Slower:
+// rows: 107 to 155 us by the rows accepted (12 to read the keys once): bound by the instructions of the codes and the exponentials, issue slots half busy. Slower:
 // three CTAs per SM for the 4-bit pass 1, which then spills nothing (151 us); the next product sent off ahead of this one's scores, with two
 // tiles' scores in tensor memory (153, and 155 for 148 with bf16 keys: the other CTAs hide a product's time already); columns by 24 (159).
 // fp32, 4 layers of 4 sequences of 1000 to 2111: 32 / 8 heads of 128 226 us, 4-bit keys 196 (a warp without rows leaves the products to the
