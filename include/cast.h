@@ -25,6 +25,13 @@
  *                        the attention weight that every cached position has drawn, and the eviction of the
  *                        positions that drew least
  *
+ * And what stands around the step in a serving loop (not in the paper):
+ *   cast_append_kv       new queries, keys and values from a projection's output to where the attention reads them, with the norm
+ *                        per head and the rotation by position on the way
+ *   cast_chunk_attention causal attention of new tokens over the cache: prompts, chunk by chunk, and decoding without a tree,
+ *                        with an optional sliding window
+ *   cast_tree_attention_window  the verification attention under a sliding window
+ *
  * Conventions
  *  - Plain C. Every tensor pointer is a DEVICE pointer owned by the caller
  *    unless its comment says "host". The library owns only what cast_create
@@ -503,6 +510,80 @@ CAST_API cast_status cast_evict_kv_q4(cast_ctx* ctx, void* k_codes, void* k_rang
                                       int D, int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
                                       int budget, int recent, float* mass, int32_t* kept, int32_t* kv_len /* in/out */,
                                       void* stream);
+
+/*
+ * ---- New rows, chunks of new tokens, and sliding windows ---------------------------------------
+ * cast_append_kv takes the rows t, first_row[b] <= t < n_rows[b], of every sequence from a projection's output to where the
+ * attention reads them: queries to q_out, keys and values to the cache positions start[b] + t.
+ *   q [.., Hq, D], k, v [.., Hkv, D]  of type `dtype`; the heads of a row lie one behind the other, rows q_stride_bytes (k_, v_) apart,
+ *                so the three may be views of one fused projection. Row t of sequence b is row b * rows + t, or, where row_start
+ *                [B] is given, row row_start[b] + t of `rows` rows in all (packed batches; sequences must not share rows).
+ *                q NULL: keys and values alone; k and v NULL: queries alone.
+ *   q_out        [.., Hq, D], dense, the same rows; may be q itself where q is dense
+ *   first_row    NULL: 0 (as for cast_tree_attention_rows: the rows before it are where they belong already)
+ *   depth        [B, rows] (packed: [rows]) int32 or NULL: a row's distance from `position`; NULL: t. (For a tree: depth as
+ *                cast_select_nodes writes it, so that a node's row keeps its rotation when the compaction moves it to kv_len + depth.)
+ *   position     [B] or NULL (start): the position of a sequence's row at distance 0; other than start where positions have left
+ *                the cache (cast_evict_kv)
+ *   start        [B] or NULL (0): cache position of row 0, the kv_len of the attention that follows
+ *   q_weight, k_weight  [D] fp32 or NULL: queries (keys) become x / sqrt(mean(x^2) + eps) * weight, per head
+ *   inv_freq     [rot_dim / 2] fp64: pair i is rotated by (position + distance) * inv_freq[i] radians and multiplied by `magnitude` (0: 1).
+ *                rot_dim, even, 0..D: the first rot_dim dims of a head rotate; interleaved 0: pair i is dims (i, i + rot_dim / 2),
+ *                else (2i, 2i + 1). Stretched contexts are other frequencies and magnitudes (rotary.py has the common ones).
+ *   cache        as for cast_tree_attention. A dense [B, rows, Hkv, D] buffer is a cache with page_size 0, seq_capacity rows and start NULL
+ *                (rotated keys on their way to cast_store_kv_q4; position then says where the sequences stand).
+ * Norm and rotation in fp32, angles in fp64, one rounding on the way out; what is neither normalised nor rotated keeps its bits. Rows outside
+ * [first_row, n_rows) of q_out and the cache are left untouched; n_rows[b] is clamped to [0, rows].
+ * Under cast_set_attention_early_reads the call is one of the caller's own: it writes q and the rows at start + t, which the promise
+ * allows right before an attention call whose kv_len is start, and nothing else.
+ * Needs D in {64, 128}, pointers and strides that are multiples of 16 bytes. CAPACITY: B beyond max_batch, B * rows or a sequence's positions past
+ * 2^31 - 2^16. Device errors: BAD_PAGE (a position below 0 or past the capacity, a page id out of range: keys and values of that row are not stored),
+ * BAD_TREE (packed: rows of the sequence outside [0, rows): it is left out).
+ */
+CAST_API cast_status cast_append_kv(cast_ctx* ctx, const void* q, size_t q_stride_bytes, const void* k, size_t k_stride_bytes,
+                                    const void* v, size_t v_stride_bytes, cast_dtype dtype, int B, int rows, int Hq, int Hkv, int D,
+                                    const int32_t* row_start, const int32_t* first_row, const int32_t* n_rows,
+                                    const int32_t* depth, const int32_t* position, const double* inv_freq, int rot_dim,
+                                    int interleaved, float magnitude, const float* q_weight, const float* k_weight, float eps,
+                                    int page_size, const int32_t* page_table, int seq_capacity, int num_pages,
+                                    const int32_t* start, void* q_out, void* k_cache, void* v_cache, void* stream);
+
+/* Set-up call, as cast_reserve_attention, for cast_chunk_attention and cast_tree_attention_window with heads of D dims: the workspace
+ * depends on nothing else. */
+CAST_API cast_status cast_reserve_chunk_attention(cast_ctx* ctx, cast_dtype dtype, int D);
+
+/*
+ * Causal attention of the new tokens t < n_new[b] of every sequence, whose cache rows are already stored at positions kv_len[b] + t:
+ * out[b,t,h] = softmax over the positions p <= kv_len[b] + t (window > 0: those of them with p > kv_len[b] + t - window or
+ * p < sinks) of (q . k) * scale, times v. One token per sequence (decoding), a prompt's chunk, or both in one batch.
+ *   q, out       [B, rows, Hq, D], or packed, as for cast_append_kv: row_start [B], `rows` rows in all; rows behind n_new[b] are left
+ *                untouched, n_new[b] is clamped to [0, rows]; the tokens' number is not bound to the context's trees
+ *   window       0: none; sinks: with a window, the first positions that stay visible. Page-table entries all of whose positions no
+ *                row of the sequence sees are not read (but for those of a tree's own tokens).
+ * Sums and softmax in fp32, a weight of a bf16 call is rounded to bf16 once on its way into the product. What a row does not see reaches no output of it, NaN
+ * and infinities included; a row that sees nothing gives zeros. The same inputs give the same bits. Never reads early.
+ * Other arguments and errors as for cast_tree_attention; needs cast_reserve_chunk_attention, the context's device as the current one (INVALID_ARG)
+ * and q, out, caches aligned to 16 bytes. INVALID_ARG: window or sinks below 0. CAPACITY: B beyond max_batch; positions of a sequence, B * rows or rows * Hq / Hkv past
+ * 2^31 - 2^16. Device errors: BAD_TREE (packed: rows outside [0, rows), the sequence is left out), BAD_PAGE (kv_len + n_new past the capacity: the
+ * positions behind it are not seen; a page id out of range: which row of the cache stands in for it is not defined).
+ */
+CAST_API cast_status cast_chunk_attention(cast_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, cast_dtype dtype,
+                                          int B, int rows, const int32_t* row_start, int Hq, int Hkv, int D, int page_size,
+                                          const int32_t* page_table, int seq_capacity, int num_pages, const int32_t* kv_len,
+                                          const int32_t* n_new, int window, int sinks, float scale, void* out, void* stream);
+
+/*
+ * cast_tree_attention_rows under a sliding window: tree token t stands at position kv_len[b] + depth[b,t], and of the positions that the tree's mask shows
+ * it, it sees those less than `window` below its own, and the first `sinks` (a tree token j counts as position kv_len[b] + depth[b,j]). depth [B, Ncap]
+ * as cast_select_nodes writes it (read as 0..CAST_MAX_TREE). window 0: none. Precision, the pages that are read, workspace, capacities and page errors as for cast_chunk_attention,
+ * all else as for cast_tree_attention_rows. Never reads early.
+ */
+CAST_API cast_status cast_tree_attention_window(cast_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,
+                                                cast_dtype dtype, int B, int Hq, int Hkv, int D, int page_size,
+                                                const int32_t* page_table, int seq_capacity, int num_pages,
+                                                const int32_t* kv_len, const uint32_t* anc_mask, const int32_t* depth,
+                                                const int32_t* n_tree, const int32_t* first_row, int window, int sinks,
+                                                float scale, void* out, void* stream);
 
 /* Synchronises `stream`, returns the device status word and clears it.
  * detail: an index that identifies the offending row/entry (meaning per status). */

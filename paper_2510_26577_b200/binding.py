@@ -36,7 +36,8 @@ EXPORTS = [
     "cast_accept_stochastic", "cast_accept_stochastic_plan", "cast_tree_attention_rows", "cast_reserve_attention",
     "cast_set_attention_early_reads", "cast_store_kv_q4", "cast_load_kv_q4", "cast_reserve_attention_q4",
     "cast_tree_attention_q4", "cast_compact_kv_q4", "cast_reserve_attention_mass", "cast_attention_mass",
-    "cast_attention_mass_q4", "cast_evict_kv", "cast_evict_kv_q4",
+    "cast_attention_mass_q4", "cast_evict_kv", "cast_evict_kv_q4", "cast_append_kv", "cast_reserve_chunk_attention",
+    "cast_chunk_attention", "cast_tree_attention_window",
 ]
 
 
@@ -87,6 +88,7 @@ def load_library() -> C.CDLL:
         "cast_set_attention_early_reads": [vp, i32],
         "cast_reserve_attention_q4": [vp, i32, i32, i32, i32, i32, i32, i32],
         "cast_reserve_attention_mass": [vp, i32, i32, i32, i32, i32, i32, i32, i32, i32],
+        "cast_reserve_chunk_attention": [vp, i32, i32],
         "cast_accept_stochastic_plan": [vp, i32, C.POINTER(C.c_int), C.POINTER(C.c_int)],
         "cast_poll_status": [vp, vp, C.POINTER(C.c_int), C.POINTER(C.c_int32)],
         "cast_step_info": [vp, vp, C.POINTER(C.c_int32)],
@@ -184,6 +186,11 @@ class CastContext:
         _check(self.lib.cast_reserve_attention_mass(self.handle, code, B, n_layers, max_rows, Hq, Hkv, D, page_size,
                                                     seq_capacity), "cast_reserve_attention_mass")
 
+    def cast_reserve_chunk_attention(self, dtype, D):
+        """The same for cast_chunk_attention and cast_tree_attention_window, whatever their shapes."""
+        code = CAST_F32 if dtype == torch.float32 else CAST_BF16
+        _check(self.lib.cast_reserve_chunk_attention(self.handle, code, D), "cast_reserve_chunk_attention")
+
     def cast_set_attention_early_reads(self, promise: bool):
         """The caller's promise that only q and the tree tokens' cache rows come from the operation right before an
         attention call (see include/cast.h)."""
@@ -279,6 +286,28 @@ class CastContext:
         _check(_calls.evict_kv_q4(self._ctx, k_codes, k_range, v_codes, v_range, code_stride_bytes, range_stride_bytes, B,
                                   n_layers, Hkv, D, page_size, page_table, seq_capacity, num_pages, budget, recent, mass, kept,
                                   kv_len, stream), "cast_evict_kv_q4")
+
+    # --- new rows, chunks of new tokens, sliding windows ----------------------
+    def cast_append_kv(self, q, q_stride_bytes, k, k_stride_bytes, v, v_stride_bytes, B, rows, Hq, Hkv, D, row_start, first_row, n_rows,
+                       depth, position, inv_freq, rot_dim, interleaved, magnitude, q_weight, k_weight, eps, page_size, page_table,
+                       seq_capacity, num_pages, start, q_out, k_cache, v_cache, stream=None):
+        """q, k and v may be views: [.., heads, D] with dense heads and one distance between rows (a fused projection's output)."""
+        _check(_calls.append_kv(self._ctx, q, q_stride_bytes, k, k_stride_bytes, v, v_stride_bytes, B, rows, Hq, Hkv, D, row_start,
+                                first_row, n_rows, depth, position, inv_freq, rot_dim, interleaved, magnitude, q_weight, k_weight, eps,
+                                page_size, page_table, seq_capacity, num_pages, start, q_out, k_cache, v_cache, stream),
+               "cast_append_kv")
+
+    def cast_chunk_attention(self, q, k_cache, v_cache, B, rows, row_start, Hq, Hkv, D, page_size, page_table, seq_capacity, num_pages,
+                             kv_len, n_new, window, sinks, scale, out, stream=None):
+        _check(_calls.chunk_attention(self._ctx, q, k_cache, v_cache, B, rows, row_start, Hq, Hkv, D, page_size, page_table,
+                                      seq_capacity, num_pages, kv_len, n_new, window, sinks, scale, out, stream),
+               "cast_chunk_attention")
+
+    def cast_tree_attention_window(self, q, k_cache, v_cache, B, Hq, Hkv, D, page_size, page_table, seq_capacity, num_pages, kv_len,
+                                   anc_mask, depth, n_tree, first_row, window, sinks, scale, out, stream=None):
+        _check(_calls.tree_attention_window(self._ctx, q, k_cache, v_cache, B, Hq, Hkv, D, page_size, page_table, seq_capacity,
+                                            num_pages, kv_len, anc_mask, depth, n_tree, first_row, window, sinks, scale, out, stream),
+               "cast_tree_attention_window")
 
     def cast_accept_stochastic_plan(self, dtype):
         """(cluster size, slices cached in shared memory?) for logits of torch dtype `dtype`."""

@@ -92,6 +92,41 @@ struct Args {
     }
     return tensor();
   }
+  // rows [.., heads, D] that may lie apart (a view of a fused projection's output): dense heads, `stride` bytes from row to row,
+  // which is the next argument; null for None
+  void* strided(cast_dtype* dtype, bool* given, size_t* stride) {
+    PyObject* o = next();
+    *given = o != nullptr && o != Py_None;
+    if (!o) return nullptr;
+    if (o == Py_None) {
+      *stride = size();
+      return nullptr;
+    }
+    if (!THPVariable_Check(o)) {
+      PyErr_SetString(PyExc_TypeError, "torch tensor expected");
+      ok = false;
+      return nullptr;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    *stride = size();
+    if (!ok) return nullptr;
+    const int64_t nd = t.dim();
+    bool fits = t.is_cuda() && nd >= 2 && t.stride(nd - 1) == 1 && (t.size(nd - 2) == 1 || t.stride(nd - 2) == t.size(nd - 1));
+    int64_t step = (int64_t)(*stride / t.element_size());
+    for (int64_t d = nd - 3; fits && d >= 0; --d) {
+      fits = t.size(d) == 1 || t.stride(d) == step;
+      step *= t.size(d);
+    }
+    if (!fits || *stride % t.element_size() != 0) {
+      PyErr_SetString(PyExc_AssertionError, "device-resident tensor of dense heads, rows one given stride apart, expected");
+      ok = false;
+      return nullptr;
+    }
+    if (t.scalar_type() == at::kFloat) *dtype = CAST_F32;
+    else if (t.scalar_type() == at::kBFloat16) *dtype = CAST_BF16;
+    else known_dtype = false;
+    return t.data_ptr();
+  }
   // codes and pairs of a 4-bit cache
   void* codes() { return tensor_of(at::kByte); }
   void* range() { return tensor_of(at::kBFloat16); }
@@ -417,6 +452,112 @@ PyObject* evict_kv_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
                         s));
 }
 
+PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_ctx* c = g.context();
+  // every tensor of rows that is given has one type
+  cast_dtype dt = CAST_F32, one = CAST_F32;
+  bool any = false, given = false;
+  auto same = [&] {
+    if (g.ok && given && any && one != dt) g.known_dtype = false;
+    if (given && !any) dt = one;
+    any = any || given;
+  };
+  size_t qs = 0, ks = 0, vs = 0;
+  void* q = g.strided(&one, &given, &qs);
+  same();
+  void* k = g.strided(&one, &given, &ks);
+  same();
+  void* v = g.strided(&one, &given, &vs);
+  same();
+  const int B = g.integer(), rows = g.integer(), Hq = g.integer(), Hkv = g.integer(), D = g.integer();
+  auto* row_start = g.ints();
+  auto* first = g.ints();
+  auto* n_rows = g.ints();
+  auto* depth = g.ints();
+  auto* position = g.ints();
+  auto* inv_freq = static_cast<double*>(g.tensor_of(at::kDouble));
+  const int rot_dim = g.integer(), interleaved = g.integer();
+  const float magnitude = (float)g.real();
+  auto* q_weight = static_cast<float*>(g.tensor_of(at::kFloat));
+  auto* k_weight = static_cast<float*>(g.tensor_of(at::kFloat));
+  const float eps = (float)g.real();
+  const int page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* start = g.ints();
+  auto dense = [&]() -> void* {
+    PyObject* o = g.ok && g.at < g.n ? g.a[g.at] : nullptr;
+    given = o != nullptr && o != Py_None;
+    void* t = given ? g.tensor(&one) : g.tensor();
+    same();
+    return t;
+  };
+  void* q_out = dense();
+  void* kc = dense();
+  void* vc = dense();
+  void* s = g.stream();
+  CALL(cast_append_kv(c, q, qs, k, ks, v, vs, dt, B, rows, Hq, Hkv, D, row_start, first, n_rows, depth, position, inv_freq, rot_dim,
+                      interleaved, magnitude, q_weight, k_weight, eps, page, table, cap, pages, start, q_out, kc, vc, s));
+}
+
+// Queries and the two caches of an attention, of one type; the same of its output.
+void attended(Args& g, cast_dtype* dt, void** q, void** k, void** v) {
+  cast_dtype other = CAST_F32;
+  *q = g.tensor(dt);
+  both(g, &other, k, v);
+  if (g.ok && other != *dt) g.known_dtype = false;
+}
+void* output(Args& g, cast_dtype dt) {
+  cast_dtype other = CAST_F32;
+  void* out = g.tensor(&other);
+  if (g.ok && other != dt) g.known_dtype = false;
+  return out;
+}
+
+PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32;
+  cast_ctx* c = g.context();
+  void *q, *k, *v;
+  attended(g, &dt, &q, &k, &v);
+  const int B = g.integer(), rows = g.integer();
+  auto* row_start = g.ints();
+  const int Hq = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* kv_len = g.ints();
+  auto* n_new = g.ints();
+  const int window = g.integer(), sinks = g.integer();
+  const float scale = (float)g.real();
+  void* out = output(g, dt);
+  void* s = g.stream();
+  CALL(cast_chunk_attention(c, q, k, v, dt, B, rows, row_start, Hq, Hkv, D, page, table, cap, pages, kv_len, n_new, window, sinks,
+                            scale, out, s));
+}
+
+PyObject* tree_attention_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g{a, n};
+  cast_dtype dt = CAST_F32;
+  cast_ctx* c = g.context();
+  void *q, *k, *v;
+  attended(g, &dt, &q, &k, &v);
+  const int B = g.integer(), Hq = g.integer(), Hkv = g.integer(), D = g.integer(), page = g.integer();
+  auto* table = g.ints();
+  const int cap = g.integer(), pages = g.integer();
+  auto* kv_len = g.ints();
+  auto* anc = g.tensor<uint32_t>();
+  auto* depth = g.ints();
+  auto* n_tree = g.ints();
+  auto* first = g.ints();
+  const int window = g.integer(), sinks = g.integer();
+  const float scale = (float)g.real();
+  void* out = output(g, dt);
+  void* s = g.stream();
+  CALL(cast_tree_attention_window(c, q, k, v, dt, B, Hq, Hkv, D, page, table, cap, pages, kv_len, anc, depth, n_tree, first, window,
+                                  sinks, scale, out, s));
+}
+
 #define METHOD(name, fn) {name, (PyCFunction)(void (*)())(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     METHOD("step_begin", step_begin),
@@ -436,6 +577,9 @@ PyMethodDef methods[] = {
     METHOD("attention_mass_q4", attention_mass<true>),
     METHOD("evict_kv", evict_kv),
     METHOD("evict_kv_q4", evict_kv_q4),
+    METHOD("append_kv", append_kv),
+    METHOD("chunk_attention", chunk_attention),
+    METHOD("tree_attention_window", tree_attention_window),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

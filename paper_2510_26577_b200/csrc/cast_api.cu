@@ -38,7 +38,7 @@ void free_all(cast_ctx* c) {
   cudaFree(c->layer_ticket); cudaFree(c->seq_ticket); cudaFree(c->tail_vs); cudaFree(c->tail_sorted); cudaFree(c->tail_tok);
   cudaFree(c->fifo_vals); cudaFree(c->fifo_cnt); cudaFree(c->sel_score); cudaFree(c->sel_value);
   cudaFree(c->sel_idx); cudaFree(c->acc_part); cudaFree(c->compact_ticket); cudaFree(c->attn_ws); cudaFree(c->attn_tc_ws);
-  cudaFree(c->q4_ws); cudaFree(c->mass_ws);
+  cudaFree(c->q4_ws); cudaFree(c->mass_ws); cudaFree(c->chunk_ws);
   if (c->tables) {
     for (auto& kv : *c->tables) cudaFree(kv.second.storage);
     delete c->tables;

@@ -110,6 +110,9 @@ struct cast_ctx {
   size_t q4_ws_bytes;
   void* mass_ws;
   size_t mass_ws_bytes;
+  // workspace of the chunk and window attention (cast_reserve_chunk_attention)
+  void* chunk_ws;
+  size_t chunk_ws_bytes;
 
   // stochastic acceptance, per logits dtype (0 fp32, 1 bf16): cluster size found to be launchable
   // (0: not looked up yet), whether a CTA's vocabulary slice is cached on chip, and how many such clusters run at once
