@@ -1,5 +1,6 @@
 // cast_chunk_attention and cast_tree_attention_window: attention of new tokens over the cache, causal or under a tree's mask, with an
-// optional sliding window and its sinks.
+// optional sliding window and its sinks. Here the entry points and the CUDA-core kernel: fp32 inputs, and the bf16 shapes that the tensor-core
+// kernel does not take (chunk_attention_tc.cu).
 //
 // One CTA works its stretch of the line of tiles (chunk_attn.h) item by item: 32 query rows of one kv-head against tiles of 64 positions,
 // both in fp32 in shared memory; S = Q K^T by packed multiply-adds, an online softmax, O += P V in registers. Positions that no row of the
@@ -11,12 +12,18 @@
 
 using namespace cast;
 
+namespace cast {
+// implemented in chunk_attention_tc.cu
+size_t chunk_attention_tc_workspace(const cast_ctx* c, int D);
+bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspace, cudaStream_t s, cast_status* status);
+}
+
 namespace {
 
 constexpr int kRB = 32;
 constexpr int kPT = 64;
 constexpr int kThreads = 256;
-constexpr size_t kTicketBytes = kChunkGrid * sizeof(int32_t);
+constexpr size_t kTicketBytes = 2 * kChunkGrid * sizeof(int32_t);
 
 typedef unsigned long long f32x2;
 __device__ __forceinline__ float sum2(f32x2 v) {
@@ -301,7 +308,6 @@ cast_status launch_cc(cast_ctx* c, ChunkParams& p, cudaStream_t s) {
   p.block_rows = kRB;
   p.min_units = kItemCost + 2;
   const int grid = 2 * c->num_sms < kChunkGrid ? 2 * c->num_sms : kChunkGrid;
-  p.ticket = reinterpret_cast<int32_t*>(c->chunk_ws);
   p.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(c->chunk_ws) + kTicketBytes);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)kChunkGrid * 2 * kRB * D);
   const size_t smem = (size_t)(kRB * (D + 4) + kPT * (D + 4) + kPT * D + kRB * (kPT + 4)) * sizeof(float);
@@ -324,7 +330,12 @@ cast_status launch_cc(cast_ctx* c, ChunkParams& p, cudaStream_t s) {
   return launch_status();
 }
 
-size_t cc_workspace(int D) { return kTicketBytes + (size_t)kChunkGrid * 2 * kRB * (D + 2) * sizeof(float); }
+// A bf16 call goes either way by its shape: both workspaces fit.
+size_t workspace(const cast_ctx* c, cast_dtype dtype, int D) {
+  const size_t cc = (size_t)kChunkGrid * 2 * kRB * (D + 2) * sizeof(float);
+  const size_t tc = dtype == CAST_BF16 ? chunk_attention_tc_workspace(c, D) : 0;
+  return kTicketBytes + (cc > tc ? cc : tc);
+}
 
 template <bool kTree>
 cast_status attend(cast_ctx* c, ChunkParams& p, cast_dtype dtype, int D, float scale, void* stream) {
@@ -336,12 +347,15 @@ cast_status attend(cast_ctx* c, ChunkParams& p, cast_dtype dtype, int D, float s
   if (((uintptr_t)p.q | (uintptr_t)p.k | (uintptr_t)p.v | (uintptr_t)p.out) & 15) return CAST_ERR_SHAPE;
   // (rows of a sequence and positions are counted in 32 bits)
   if (p.B > c->cfg.max_batch || p.g.max_pos() > kMaxPositions || (long long)p.B * p.rows > kMaxPositions ||
-      (long long)p.rows * (p.Hq / p.Hkv) > kMaxPositions || cc_workspace(D) > c->chunk_ws_bytes)
+      (long long)p.rows * (p.Hq / p.Hkv) > kMaxPositions || workspace(c, dtype, D) > c->chunk_ws_bytes)
     return CAST_ERR_CAPACITY;
   p.G = p.Hq / p.Hkv;
   p.scale = scale == 0.f ? 1.0f / sqrtf((float)D) : scale;
   p.st = c->state;
   cudaStream_t s = (cudaStream_t)stream;
+  p.ticket = reinterpret_cast<int32_t*>(c->chunk_ws);
+  cast_status st;
+  if (dtype == CAST_BF16 && chunk_attention_tc_launch(c, p, D, reinterpret_cast<char*>(c->chunk_ws) + kTicketBytes, s, &st)) return st;
   if (dtype == CAST_BF16) return D == 64 ? launch_cc<__nv_bfloat16, 64, kTree>(c, p, s) : launch_cc<__nv_bfloat16, 128, kTree>(c, p, s);
   return D == 64 ? launch_cc<float, 64, kTree>(c, p, s) : launch_cc<float, 128, kTree>(c, p, s);
 }
@@ -353,7 +367,7 @@ extern "C" cast_status cast_reserve_chunk_attention(cast_ctx* c, cast_dtype dtyp
   if (dtype != CAST_F32 && dtype != CAST_BF16) return CAST_ERR_DTYPE;
   if (D != 64 && D != 128) return CAST_ERR_SHAPE;
   // tickets start at zero; every merge leaves its ticket at zero again
-  return grow_workspace(&c->chunk_ws, &c->chunk_ws_bytes, cc_workspace(D), kTicketBytes);
+  return grow_workspace(&c->chunk_ws, &c->chunk_ws_bytes, workspace(c, dtype, D), kTicketBytes);
 }
 
 extern "C" cast_status cast_chunk_attention(cast_ctx* c, const void* q, const void* k_cache, const void* v_cache, cast_dtype dtype, int B,

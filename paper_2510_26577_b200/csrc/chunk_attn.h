@@ -40,8 +40,8 @@ struct ChunkParams {
 
 // A sequence's live rows and what its items walk.
 struct ChunkSeq {
-  int L, n, F, off;  // prefix, tokens, first output token, row of token 0
-  int d0;            // tree: least depth of an output token
+  int L, n, off;          // prefix, tokens, row of token 0
+  unsigned short F, d0;   // tree: first output token, least depth of an output token
 };
 
 // The tiles of an item.
@@ -88,7 +88,7 @@ template <int PT, bool kTree>
 __device__ __forceinline__ Span block_span(const ChunkParams& p, const ChunkSeq& s, int rb) {
   const int r0 = rb * p.block_rows, rows = (s.n - s.F) * p.G;
   const int r1 = min(r0 + p.block_rows, rows);
-  return span_of<PT, kTree>(p, s, s.F + r0 / p.G, s.F + (r1 - 1) / p.G);
+  return span_of<PT, kTree>(p, s, (int)s.F + r0 / p.G, (int)s.F + (r1 - 1) / p.G);
 }
 
 // All threads of the CTA call; ends with a barrier.
@@ -97,11 +97,12 @@ __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   for (int b = tid; b < CAST_MAX_BATCH; b += blockDim.x) {
     ChunkSeq s = {0, 0, 0, 0, 0};
+    int F = 0;
     if (b < p.B) {
       const long long all = p.row_start ? p.rows : (long long)p.B * p.rows;
       s.L = max(p.kv_len[b], 0);
       s.n = p.n_new[b];
-      s.F = p.first_row ? p.first_row[b] : 0;
+      if (p.first_row) F = p.first_row[b];
       s.off = p.row_start ? p.row_start[b] : b * p.rows;
       const int most = kTree ? p.Nmax : p.rows;
       bool bad = false;
@@ -115,7 +116,8 @@ __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
         s.n = 0;
       }
       if (bad && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_TREE, b);
-      s.F = min(max(s.F, 0), s.n);
+      F = min(max(F, 0), s.n);  // (with a tree, so it fits)
+      s.F = (unsigned short)(kTree ? F : 0);
       if ((long long)s.L + s.n > p.g.max_pos() && s.n > s.F) {
         if (blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
         if (s.L > p.g.max_pos()) s.L = (int)p.g.max_pos();
@@ -131,7 +133,7 @@ __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
       if (kTree) {
         int d = CAST_MAX_TREE;
         for (int t = s.F + lane; t < s.n; t += 32) d = min(d, depth_of(p, s, t));
-        s.d0 = __reduce_min_sync(0xffffffffu, d);
+        s.d0 = (unsigned short)__reduce_min_sync(0xffffffffu, d);
         if (lane == 0) pl.seq[b].d0 = s.d0;
       }
       const int blocks = (int)(((long long)(s.n - s.F) * p.G + p.block_rows - 1) / p.block_rows);

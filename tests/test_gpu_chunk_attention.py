@@ -353,6 +353,7 @@ def test_refusals(binding):
             ctx.cast_reserve_chunk_attention(*bad)
         assert e.value.code == code
     ctx.cast_reserve_chunk_attention(torch.float32, D)
+    b16 = {w: base[w].bfloat16() for w in ("q", "k", "v", "out")}
     for tree in (False, True):
         call(tree)
         for code, kw in ((1, dict(kv_len=None)), (1, dict(n=None)), (1, dict(window=-1)), (1, dict(sinks=-1)), (1, dict(B=0)), (1, dict(cap=0)),
@@ -374,6 +375,9 @@ def test_refusals(binding):
     with pytest.raises(binding.CastError) as e:  # not aligned to 16 bytes
         call(False, out=flat[1:])
     assert e.value.code == 2
+    with pytest.raises(binding.CastError) as e:  # the workspace of fp32 calls is not that of bf16 calls
+        call(False, **b16)
+    assert e.value.code == 3
     assert ctx.cast_poll_status()[0] == 0
 
 
