@@ -54,7 +54,8 @@ struct Misc {
   using M = Mem<HD>;
   uint64_t q_full[2], q_free[2];
   uint64_t k_full[M::kStagesK], k_free[M::kStagesK];
-  uint64_t v_full[M::kStagesV], v_free[M::kStagesV], v_ok[M::kStagesV];
+  uint64_t v_full[M::kStagesV], v_free[M::kStagesV];
+  uint64_t v_raw[M::kStagesV];   // what v_full is to a tile that is cleaned first: the cleaner waits for these, in turn, and completes v_full
   uint64_t s_full[2], p_full[2], o_full[2];
   uint32_t tmem;
   int last[2];
@@ -109,7 +110,7 @@ __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : x >
 
 // 32 scores of this thread's row: P = 2^(s * scale + r) as bf16 pairs, the sum of the unrounded weights as a packed pair.
 template <bool kMasked>
-__device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long long sc2, unsigned long long ref2, uint32_t seen,
+__device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long sc2, unsigned long long ref2, uint32_t seen,
                                       unsigned long long& sum, uint32_t* pk) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
@@ -126,8 +127,117 @@ __device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long lon
   }
 }
 
-__device__ __forceinline__ void tmem_ld1(uint32_t at, uint32_t& r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at) : "memory");
+// Loads from tensor memory with their wait: between the two the registers hold nothing yet, and in a kernel under register pressure the compiler, which does not
+// know that, may move or spill them there.
+__device__ __forceinline__ void tmem_get1(uint32_t taddr, uint32_t& r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r)
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+}
+
+// An item's partials, joined by the four warps of a lane in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others). A warp takes U
+// rows side by side, HD / 32 columns a lane: the weights of 32 / U contributors of U rows come with one load, and the rows' loads of several contributors
+// are in flight together (one element at a time, a round trip to L2 each, joined 128 rows in 27 us).
+template <int HD, int U>
+__device__ __noinline__ void merge_rows(const ChunkParams& p, const ChunkSeq& s, int kvh, int tok0, int rows, int c_lo, int c_hi, size_t lane0) {
+  constexpr int NC = HD / 32, CP = 32 / U, KU = U == 1 ? 8 : 2;  // columns per lane, contributors per pass, contributors in flight
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  auto place = [&](int c) { return ((size_t)c * 2 + (c == c_lo ? 1 : 0)) * (2 * kRows) + lane0; };
+  const int u_mine = lane / CP, c_mine = lane % CP;
+  for (int r0 = warp * U; r0 < rows; r0 += 4 * U) {
+    auto pair_of = [&](int c) { return c <= c_hi && r0 + u_mine < rows ? __ldcg(p.part_ml + place(c) + r0 + u_mine) : make_float2(-INFINITY, 0.f); };
+    float2 ml = pair_of(c_lo + c_mine);
+    float top = ml.x;
+    for (int cb = c_lo + CP; cb <= c_hi; cb += CP) top = fmaxf(top, pair_of(cb + c_mine).x);
+#pragma unroll
+    for (int o = CP / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float acc[U][NC] = {}, l = 0.f;
+    for (int cb = c_lo; cb <= c_hi; cb += CP) {
+      if (cb > c_lo) ml = pair_of(cb + c_mine);
+      const float wt = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
+      l += ml.x > -INFINITY ? wt * ml.y : 0.f;
+#pragma unroll 1
+      for (int k0 = 0; k0 < CP && cb + k0 <= c_hi; k0 += KU) {
+        float x[KU][U][NC];
+#pragma unroll
+        for (int k = 0; k < KU; ++k)
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const float* src = p.part_o + (place(min(cb + k0 + k, c_hi)) + min(r0 + u, rows - 1)) * HD + lane * NC;
+            if constexpr (NC == 4) {
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+              x[k][u][0] = v.x; x[k][u][1] = v.y; x[k][u][2] = v.z; x[k][u][3] = v.w;
+            } else {
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+              x[k][u][0] = v.x; x[k][u][1] = v.y;
+            }
+          }
+#pragma unroll
+        for (int k = 0; k < KU; ++k)
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const float f = __shfl_sync(0xffffffffu, wt, u * CP + min(k0 + k, CP - 1));
+            if (k0 + k < CP && cb + k0 + k <= c_hi && f != 0.f) {
+#pragma unroll
+              for (int e = 0; e < NC; ++e) acc[u][e] = fmaf(f, x[k][u][e], acc[u][e]);
+            }
+          }
+      }
+    }
+#pragma unroll
+    for (int o = CP / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float lt = __shfl_sync(0xffffffffu, l, u * CP), inv = lt == 0.f ? 0.f : 1.f / lt;
+      const int rr = r0 + u;
+      if (rr < rows) {
+        uint32_t o[NC / 2];
+#pragma unroll
+        for (int e = 0; e < NC; e += 2) {
+          const __nv_bfloat162 b2 = __floats2bfloat162_rn(acc[u][e] * inv, acc[u][e + 1] * inv);
+          o[e / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+        }
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + (((size_t)s.off + tok0 + rr / p.G) * p.Hq + kvh * p.G + rr % p.G) * HD + lane * NC;
+        if constexpr (NC == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(o[0], o[1]);
+        else *reinterpret_cast<uint32_t*>(dst) = o[0];
+      }
+    }
+  }
 }
 
 template <int HD, bool kTree>
@@ -156,7 +266,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
     for (int i = 0; i < M::kStagesV; ++i) {
       mbar_init(&ms.v_full[i], 1);
       mbar_init(&ms.v_free[i], 1);
-      mbar_init(&ms.v_ok[i], 1);
+      mbar_init(&ms.v_raw[i], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
@@ -179,7 +289,10 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
   bool more = aligned && walk_begin<kTile, kTree>(p, plan, w, blockIdx.x);
   auto next = [&] { more = walk_next<kTile, kTree>(p, plan, w); };
 
+  // Registers: 384 x 168 at launch; the softmax threads take 208 (a tile's weights and half its scores are 128), the others give theirs: 256 x 208 + 128 x 80 = 63488 of 64512.
+  auto give = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); };
   if (warp == 8 || warp == 9) {
+    give();
     // =========================== loads: Q and K, or V ===========================
     const bool is_v = warp == 9;
     const int stages = is_v ? M::kStagesV : M::kStagesK;
@@ -187,7 +300,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
     uint64_t* free = is_v ? ms.v_free : ms.k_free;
     unsigned char* ring = smem + (is_v ? M::kAtV : M::kAtK);
     const CUtensorMap* map = is_v ? &map_v : &map_k;
-    int tile = 0, qc = 0;  // tiles and Q slots so far
+    int tile = 0, qc = 0, cleaned = 0;  // tiles, Q slots and tiles for the cleaner so far
     bool ok = true;
     const int per_tile = p.g.page_size == 0 ? 1 : kTile / a.box;  // copies per half
     const int copy = lane / M::kHalves, half = lane % M::kHalves;
@@ -229,17 +342,19 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         if (tile >= stages) ok = mbar_wait(&free[stage], ((tile / stages) - 1) & 1);
         if (!ok) break;
         unsigned char* dst = ring + stage * M::kTileBytes + half * kRegKV;
+        uint64_t* bar = &full[stage];
+        if (is_v && tile_to_clean(p, w.span, it, pos0)) bar = &ms.v_raw[cleaned++ % M::kStagesV];
         if (p.g.page_size == 0) {
-          if (lane == 0) mbar_expect_tx(&full[stage], M::kTileBytes);
+          if (lane == 0) mbar_expect_tx(bar, M::kTileBytes);
           __syncwarp();
-          if (lane < M::kHalves) tma_load_3d(map, dst, &full[stage], half * 64, w.h, w.b * p.g.seq_capacity + pos0);
+          if (lane < M::kHalves) tma_load_3d(map, dst, bar, half * 64, w.h, w.b * p.g.seq_capacity + pos0);
         } else {
           const int copies = __popc(__ballot_sync(0xffffffffu, now >= 0));
-          if (lane == 0) mbar_expect_tx(&full[stage], (uint32_t)(copies * a.box * 128));
+          if (lane == 0) mbar_expect_tx(bar, (uint32_t)(copies * a.box * 128));
           __syncwarp();
           if (now >= 0) {
             const int pos = pos0 + copy * a.box;
-            tma_load_4d(map, dst + copy * a.box * 128, &full[stage], half * 64, w.h, pos % p.g.page_size, now);
+            tma_load_4d(map, dst + copy * a.box * 128, bar, half * 64, w.h, pos % p.g.page_size, now);
           }
         }
         __syncwarp();
@@ -252,6 +367,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         for (int j = max(0, qc - 2); j < qc; ++j) mbar_wait(&ms.q_full[j & 1], (j >> 1) & 1);
     }
   } else if (warp == 10) {
+    give();
     // =========================== products ===========================
     const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
     const uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
@@ -261,13 +377,14 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
     const uint64_t dv = umma_desc(smem_u32(smem + M::kAtV), kRegKV, 1024);
     int kst = 0, kph = 0, vst = 0, vph = 0, qc = 0, turn = 0, newest = 1;
     uint32_t pph = 0;                 // phase of p_full, a bit per lane
-    int pend0 = 0, pend1 = 0;         // a lane's P V that waits: bit 0 there is one, 1 V's phase, 2 to be cleaned, 3 releases V, 4 the item's last, then the stage
+    // a lane's P V that waits: bit 0 there is one, 1 V's phase, 2 it releases V, 3 it is the item's last, then V's stage
+    int pend0 = 0, pend1 = 0;
     bool ok = true;
     auto flush = [&](int h) {         // the lane's P V
       const int f = h ? pend1 : pend0;
       if (!ok || !(f & 1)) return;
-      const int stage = f >> 5;
-      ok = mbar_wait(&ms.p_full[h], (pph >> h) & 1) && mbar_wait((f & 4) ? &ms.v_ok[stage] : &ms.v_full[stage], (f >> 1) & 1);
+      const int stage = f >> 4;
+      ok = mbar_wait(&ms.p_full[h], (pph >> h) & 1) && mbar_wait(&ms.v_full[stage], (f >> 1) & 1);
       if (!ok) return;
       pph ^= 1u << h;
       tc_fence_after();
@@ -275,8 +392,8 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
 #pragma unroll
       for (int ks = 0; ks < kTile / 16; ++ks)
         umma_bf16_ts(tm + kColO + h * kLaneCols, tm + kColS + h * kLaneCols + ks * 8, d + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
-      if (f & 8) umma_commit(&ms.v_free[stage]);
-      if (f & 16) umma_commit(&ms.o_full[h]);
+      if (f & 4) umma_commit(&ms.v_free[stage]);
+      if (f & 8) umma_commit(&ms.o_full[h]);
       if (h) pend1 = 0;
       else pend0 = 0;
     };
@@ -290,7 +407,6 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
       // the other lane's P V there. (While the lanes take turns the order is right by itself.)
       if (lanes == 2 && newest == 0) flush(1);
       for (int i = 0; i < T && ok; ++i) {
-        const int clean = __reduce_max_sync(0xffffffffu, tile_to_clean(p, w.span, it, w.span.tile(w.t0 + i) * kTile) ? 4 : 0);
         for (int j = 0; j < lanes && ok; ++j) {
           const int h = lanes == 2 ? j : (turn + i) & 1;
           flush(h);
@@ -308,7 +424,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
           umma_commit(&ms.s_full[h]);
           if (j == lanes - 1) umma_commit(&ms.k_free[kst]);
           if (i == T - 1) umma_commit(&ms.q_free[slot]);
-          const int f = 1 | (vph << 1) | clean | (j == lanes - 1 ? 8 : 0) | (i + (lanes == 2 ? 1 : 2) >= T ? 16 : 0) | (vst << 5);
+          const int f = 1 | (vph << 1) | (j == lanes - 1 ? 4 : 0) | (i + (lanes == 2 ? 1 : 2) >= T ? 8 : 0) | (vst << 4);
           if (h) pend1 = f;
           else pend0 = f;
           newest = h;
@@ -329,17 +445,19 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
     if (ok) flush(newest);
     if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   } else if (warp == 11) {
+    give();
     // =========================== V tiles that not every row sees whole ===========================
-    int tile = 0;
+    int tile = 0, cleaned = 0;
     bool ok = true;
     for (; more && ok; next()) {
       const ChunkSeq s = plan.seq[w.b];
       const Item it = w.t1 > w.t0 ? item_of<kTree>(p, s, w) : Item();
       for (int i = w.t0; i < w.t1; ++i, ++tile) {
         const int stage = tile % M::kStagesV, pos0 = w.span.tile(i) * kTile;
-        ok = mbar_wait(&ms.v_full[stage], (tile / M::kStagesV) & 1);
+        if (!tile_to_clean(p, w.span, it, pos0)) continue;
+        ok = mbar_wait(&ms.v_raw[cleaned % M::kStagesV], (cleaned / M::kStagesV) & 1);
         if (!ok) break;
-        if (tile_to_clean(p, w.span, it, pos0)) {
+        {
           unsigned char* v = smem + M::kAtV + stage * M::kTileBytes;
           const bool part = tile_in_part(p, w.span, it, pos0);
 #pragma unroll 1
@@ -368,11 +486,13 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
           fence_proxy_async();  // the product reads these rows through the async proxy
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&ms.v_ok[stage]);
+        if (lane == 0) mbar_arrive(&ms.v_full[stage]);
+        ++cleaned;
       }
     }
     if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // =========================== softmax and output ===========================
     const int h = warp >> 2, r = tid & (kRows - 1), bar_id = 1 + h;
     const uint32_t rowsel = (uint32_t)((warp & 3) * 32) << 16;
@@ -387,12 +507,12 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
       if (T <= 0 && !nothing) continue;
       const ChunkSeq s = plan.seq[w.b];
       const Item it = item_of<kTree>(p, s, w);
-      const int t_first = it.pair ? 0 : (h - turn) & 1, t_step = it.pair ? 1 : 2;  // this lane's tiles
+      const int t_first = it.pair ? 0 : (h - turn) & 1;  // this lane's first tile: it takes all, or every other one
       const bool both = !it.pair && T > 1, mine = it.pair || t_first < T;
       if (!it.pair) turn = (turn + T) & 1;
       const int vt0 = vtile;
       vtile += T;
-      if (!mine && !nothing) continue;
+      if (!mine && !nothing) continue;  // (one tile, the other lane's)
       // the row
       const int lane_rows = it.pair ? min(max(it.rows - h * a.tokens * p.G, 0), a.tokens * p.G) : it.rows;
       const bool row_ok = r < lane_rows, warp_live = (warp & 3) * 32 < lane_rows;
@@ -420,7 +540,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         for (int c = 0; c < HD; c += 32) tmem_st32(t_o + c, z);
         tmem_wait_st();
       }
-      for (int i = t_first; i < T; i += t_step, ++steps) {
+      for (int i = t_first; i < T; i += it.pair ? 1 : 2, ++steps) {
         if (ok) ok = mbar_wait(&ms.s_full[h], steps & 1);
         if (!ok) {
           tc_fence_before();
@@ -445,26 +565,22 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
           }
           return row_ok ? v : 0u;
         };
-        uint32_t sa[32], sb[32], pk[64];
+        uint32_t pk[64];
         unsigned long long sum2 = pack_f2(0.f, 0.f);
         {
           const unsigned long long ref2 = pack_f2(ref, ref);
-          tmem_ld32(t_s, sa);
-          tmem_wait_ld_regs(sa);
-          tmem_ld32(t_s + 32, sb);
-          if (plain) weigh<false>(sa, sc2, ref2, 0u, sum2, pk);
-          else weigh<true>(sa, sc2, ref2, seen_word(0), sum2, pk);
-          tmem_wait_ld_regs(sb);
-          tmem_ld32(t_s + 64, sa);
-          if (plain) weigh<false>(sb, sc2, ref2, 0u, sum2, pk + 16);
-          else weigh<true>(sb, sc2, ref2, seen_word(1), sum2, pk + 16);
-          tmem_wait_ld_regs(sa);
-          tmem_ld32(t_s + 96, sb);
-          if (plain) weigh<false>(sa, sc2, ref2, 0u, sum2, pk + 32);
-          else weigh<true>(sa, sc2, ref2, seen_word(2), sum2, pk + 32);
-          tmem_wait_ld_regs(sb);
-          if (plain) weigh<false>(sb, sc2, ref2, 0u, sum2, pk + 48);
-          else weigh<true>(sb, sc2, ref2, seen_word(3), sum2, pk + 48);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t x[64];
+            tmem_get64(t_s + j * 64, x);
+            if (plain) {
+              weigh<false>(x, sc2, ref2, 0u, sum2, pk + 32 * j);
+              weigh<false>(x + 32, sc2, ref2, 0u, sum2, pk + 32 * j + 16);
+            } else {
+              weigh<true>(x, sc2, ref2, seen_word(2 * j), sum2, pk + 32 * j);
+              weigh<true>(x + 32, sc2, ref2, seen_word(2 * j + 1), sum2, pk + 32 * j + 16);
+            }
+          }
         }
         float l0, l1;
         unpack_f2(sum2, l0, l1);
@@ -472,12 +588,12 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         const bool far = row_ok && !(l0 < 1.15e18f);  // 2^60
         const bool low = row_ok && l_run + l0 < 8.6e-19f && (plain || (seen_word(0) | seen_word(1) | seen_word(2) | seen_word(3)) != 0u);  // 2^-60, something seen
         if (__any_sync(0xffffffffu, far || low)) {
+          uint32_t sa[32];
           // (P V of this lane's tile before is over: the product that made these scores was issued behind it)
           float top = -INFINITY;
 #pragma unroll 1
           for (int j = 0; j < 4; ++j) {
-            tmem_ld32(t_s + j * 32, sa);
-            tmem_wait_ld_regs(sa);
+            tmem_get32(t_s + j * 32, sa);
             const uint32_t v = plain ? 0xffffffffu : seen_word(j);
 #pragma unroll
             for (int c = 0; c < 32; ++c) top = fmaxf(top, ((v >> c) & 1u) ? __uint_as_float(sa[c]) : -INFINITY);
@@ -493,8 +609,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
           if (__any_sync(0xffffffffu, alpha != 1.f)) {
 #pragma unroll 1
             for (int c = 0; c < HD; c += 32) {
-              tmem_ld32(t_o + c, sa);
-              tmem_wait_ld_regs(sa);
+              tmem_get32(t_o + c, sa);
 #pragma unroll
               for (int e = 0; e < 32; ++e) sa[e] = __float_as_uint(__uint_as_float(sa[e]) * alpha);
               tmem_st32(t_o + c, sa);
@@ -507,8 +622,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
           const unsigned long long ref2 = pack_f2(ref, ref);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {  // the tile again (rows that did not move get the same values)
-            tmem_ld32(t_s + j * 32, sa);
-            tmem_wait_ld_regs(sa);
+            tmem_get32(t_s + j * 32, sa);
             weigh<true>(sa, sc2, ref2, plain ? (row_ok ? 0xffffffffu : 0u) : seen_word(j), sum2, pk + 16 * j);
           }
           unpack_f2(sum2, l0, l1);
@@ -516,7 +630,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         }
         if (tile_in_part(p, w.span, it, pos0)) {
           const int vt = vt0 + i, stage = vt % M::kStagesV;
-          ok = mbar_wait(&ms.v_ok[stage], (vt / M::kStagesV) & 1);
+          ok = mbar_wait(&ms.v_full[stage], (vt / M::kStagesV) & 1);
           if (ok) {
 #pragma unroll 1
             for (int j = 0; j < 4; ++j) {
@@ -524,9 +638,8 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
               for (uint32_t left = ms.bad[stage][j]; left; left &= left - 1) {  // V rows that hold a NaN or an infinity, as the cleaner found them
                 const int bit = __ffs(left) - 1, pos = pos0 + j * 32 + bit;
                 if (!__any_sync(0xffffffffu, (v >> bit) & 1u)) continue;
-                uint32_t x;
-                tmem_ld1(t_s + j * 32 + bit, x);
-                tmem_wait_ld();
+                uint32_t x, sa[32];
+                tmem_get1(t_s + j * 32 + bit, x);
                 const float wt = ((v >> bit) & 1u) ? fast_exp2(fmaf(__uint_as_float(x), sc, ref)) : 0.f;
                 int page = 0, slot = 0;
                 if (!find_place(p.g, w.b, pos, page, slot)) page = 0;
@@ -534,8 +647,7 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
                 const __nv_bfloat16* row = reinterpret_cast<const __nv_bfloat16*>(p.v) + at;
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 32) {
-                  tmem_ld32(t_o + c, sa);
-                  tmem_wait_ld_regs(sa);
+                  tmem_get32(t_o + c, sa);
 #pragma unroll
                   for (int e = 0; e < 32; ++e) {
                     const float f = __bfloat162float(row[c + e]);
@@ -587,15 +699,13 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
         for (int c = 0; c < HD; c += 32) {
           uint32_t o[32];
           if (ok) {
-            tmem_ld32(t_o + c, o);
-            tmem_wait_ld_regs(o);
+            tmem_get32(t_o + c, o);
           }
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = ok && f0 != 0.f ? __uint_as_float(o[e]) * f0 : 0.f;
           if (both && ok) {
-            tmem_ld32(t_o + kLaneCols + c, o);
-            tmem_wait_ld_regs(o);
+            tmem_get32(t_o + kLaneCols + c, o);
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = f1 != 0.f ? fmaf(__uint_as_float(o[e]), f1, x[e]) : x[e];
           }
@@ -635,33 +745,10 @@ chunk_attn_tc_kernel(const ChunkParams p, const TcArgs a, const __grid_constant_
       }
       asm volatile("bar.sync %0, 128;" ::"r"(bar_id) : "memory");
       if (!ms.last[h]) continue;
-      // the item's partials in CTA order, a thread per four columns of a row
-      constexpr int C4 = HD / 4;
-      for (int e = r; e < lane_rows * C4; e += kRows) {
-        const int rr = e / C4, c4 = e % C4 * 4;
-        float top = -INFINITY;
-#pragma unroll 4
-        for (int c = c_lo; c <= c_hi; ++c) top = fmaxf(top, __ldcg(p.part_ml + place(c) + rr).x);
-        float lt = 0.f, x0 = 0.f, x1 = 0.f, x2 = 0.f, x3 = 0.f;
-#pragma unroll 4
-        for (int c = c_lo; c <= c_hi; ++c) {
-          const float2 ml = __ldcg(p.part_ml + place(c) + rr);
-          const float4 o = __ldcg(reinterpret_cast<const float4*>(p.part_o + (place(c) + rr) * HD + c4));
-          const float wt = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
-          lt = fmaf(wt, ml.y, lt);
-          if (wt != 0.f) {
-            x0 = fmaf(wt, o.x, x0);
-            x1 = fmaf(wt, o.y, x1);
-            x2 = fmaf(wt, o.z, x2);
-            x3 = fmaf(wt, o.w, x3);
-          }
-        }
-        const float iv = lt == 0.f ? 0.f : 1.f / lt;
-        const int tk = it.tf + (it.pair ? h * a.tokens : 0) + rr / p.G;
-        const __nv_bfloat162 b0 = __floats2bfloat162_rn(x0 * iv, x1 * iv), b1 = __floats2bfloat162_rn(x2 * iv, x3 * iv);
-        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + (((size_t)s.off + tk) * p.Hq + w.h * p.G + rr % p.G) * HD + c4) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
-      }
+      const size_t lane0 = it.pair ? h * kRows : 0;
+      const int tk0 = it.tf + (it.pair ? h * a.tokens : 0);
+      if (lane_rows <= 4) merge_rows<HD, 1>(p, s, w.h, tk0, lane_rows, c_lo, c_hi, lane0);
+      else merge_rows<HD, 8>(p, s, w.h, tk0, lane_rows, c_lo, c_hi, lane0);
     }
     if (!ok && r == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   }
