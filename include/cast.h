@@ -559,7 +559,7 @@ CAST_API cast_status cast_reserve_chunk_attention(cast_ctx* ctx, cast_dtype dtyp
  *   q, out       [B, rows, Hq, D], or packed, as for cast_append_kv: row_start [B], `rows` rows in all; rows behind n_new[b] are left
  *                untouched, n_new[b] is clamped to [0, rows]; the tokens' number is not bound to the context's trees
  *   window       0: none; sinks: with a window, the first positions that stay visible. Page-table entries all of whose positions no
- *                row of the sequence sees are not read (but for those of a tree's own tokens).
+ *                row of the sequence sees may hold anything (but for those of a tree's own tokens).
  * Sums and softmax in fp32, a weight of a bf16 call is rounded to bf16 once on its way into the product. What a row does not see reaches no output of it, NaN
  * and infinities included; a row that sees nothing gives zeros. The same inputs give the same bits. Never reads early.
  * Other arguments and errors as for cast_tree_attention; needs cast_reserve_chunk_attention, the context's device as the current one (INVALID_ARG)
@@ -575,7 +575,7 @@ CAST_API cast_status cast_chunk_attention(cast_ctx* ctx, const void* q, const vo
 /*
  * cast_tree_attention_rows under a sliding window: tree token t stands at position kv_len[b] + depth[b,t], and of the positions that the tree's mask shows
  * it, it sees those less than `window` below its own, and the first `sinks` (a tree token j counts as position kv_len[b] + depth[b,j]). depth [B, Ncap]
- * as cast_select_nodes writes it (read as 0..CAST_MAX_TREE). window 0: none. Precision, the pages that are read, workspace, capacities and page errors as for cast_chunk_attention,
+ * as cast_select_nodes writes it (read as 0..CAST_MAX_TREE). window 0: none. Precision, the pages that are looked at, workspace, capacities and page errors as for cast_chunk_attention,
  * all else as for cast_tree_attention_rows. Never reads early.
  */
 CAST_API cast_status cast_tree_attention_window(cast_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,

@@ -306,6 +306,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attn_cc_kernel(const ChunkPara
 template <typename T, int D, bool kTree>
 cast_status launch_cc(cast_ctx* c, ChunkParams& p, cudaStream_t s) {
   p.block_rows = kRB;
+  p.block_tokens = kRB % p.G == 0 ? kRB / p.G : 0;
   p.min_units = kItemCost + 2;
   const int grid = 2 * c->num_sms < kChunkGrid ? 2 * c->num_sms : kChunkGrid;
   p.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(c->chunk_ws) + kTicketBytes);
@@ -350,6 +351,7 @@ cast_status attend(cast_ctx* c, ChunkParams& p, cast_dtype dtype, int D, float s
       (long long)p.rows * (p.Hq / p.Hkv) > kMaxPositions || workspace(c, dtype, D) > c->chunk_ws_bytes)
     return CAST_ERR_CAPACITY;
   p.G = p.Hq / p.Hkv;
+  p.max_pos = (int)p.g.max_pos();
   p.scale = scale == 0.f ? 1.0f / sqrtf((float)D) : scale;
   p.st = c->state;
   cudaStream_t s = (cudaStream_t)stream;

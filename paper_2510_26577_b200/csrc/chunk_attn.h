@@ -24,6 +24,8 @@ struct ChunkParams {
   void* out;
   int B, rows, Hq, Hkv, G;  // rows: of a sequence in q and out, or of all where row_start is given
   int block_rows;           // rows of an item at most
+  int block_tokens;         // where they are whole tokens: how many; else 0
+  int max_pos;              // capacity of a sequence
   int min_units;            // a CTA's stretch at least
   int Nmax;                 // tree: most tokens
   int window, sinks;        // window 0: none
@@ -54,18 +56,19 @@ struct Span {
 
 template <int PT, bool kTree>
 __device__ __forceinline__ Span span_of(const ChunkParams& p, const ChunkSeq& s, int tf, int tl) {
-  const long long max_pos = p.g.max_pos();
   Span x;
   const long long end = (long long)s.L + (kTree ? s.n : tl + 1);
-  x.hi = (int)(end < max_pos ? end : max_pos);
-  const long long first = (long long)s.L + (kTree ? s.d0 : tf);
-  const long long lo = p.window > 0 ? first - p.window + 1 : 0;
-  x.lo = lo < 0 ? 0 : lo > x.hi ? x.hi : (int)lo;
+  x.hi = (int)(end < p.max_pos ? end : p.max_pos);
+  x.lo = 0;
+  if (p.window > 0) {
+    const long long lo = (long long)s.L + (kTree ? s.d0 : tf) - p.window + 1;
+    x.lo = lo < 0 ? 0 : lo > x.hi ? x.hi : (int)lo;
+  }
   x.s_end = x.lo > 0 ? (p.sinks < x.lo ? p.sinks : x.lo) : 0;
-  x.st = (x.s_end + PT - 1) / PT;
-  x.wt = x.lo / PT;
+  x.st = (int)((uint32_t)(x.s_end + PT - 1) / PT);
+  x.wt = (int)((uint32_t)x.lo / PT);
   if (x.wt < x.st) x.wt = x.st;
-  const int wt1 = (x.hi + PT - 1) / PT;
+  const int wt1 = (int)((uint32_t)(x.hi + PT - 1) / PT);
   x.n = x.st + (wt1 > x.wt ? wt1 - x.wt : 0);
   return x;
 }
@@ -84,93 +87,138 @@ struct ChunkPlan {
   int workers;
 };
 
+// First and last token of a row block.
+__device__ __forceinline__ int first_token(const ChunkParams& p, const ChunkSeq& s, int rb) {
+  return s.F + (p.block_tokens ? rb * p.block_tokens : rb * p.block_rows / p.G);
+}
+__device__ __forceinline__ int last_token(const ChunkParams& p, const ChunkSeq& s, int rb) {
+  if (p.block_tokens) return min((int)s.F + (rb + 1) * p.block_tokens, s.n) - 1;
+  return s.F + (min((rb + 1) * p.block_rows, (s.n - s.F) * p.G) - 1) / p.G;
+}
+__device__ __forceinline__ int blocks_of(const ChunkParams& p, const ChunkSeq& s) {
+  return (int)(p.block_tokens ? (uint32_t)(s.n - s.F + p.block_tokens - 1) / (uint32_t)p.block_tokens
+                              : ((uint32_t)(s.n - s.F) * p.G + p.block_rows - 1) / (uint32_t)p.block_rows);
+}
 template <int PT, bool kTree>
 __device__ __forceinline__ Span block_span(const ChunkParams& p, const ChunkSeq& s, int rb) {
-  const int r0 = rb * p.block_rows, rows = (s.n - s.F) * p.G;
-  const int r1 = min(r0 + p.block_rows, rows);
-  return span_of<PT, kTree>(p, s, (int)s.F + r0 / p.G, (int)s.F + (r1 - 1) / p.G);
+  return span_of<PT, kTree>(p, s, first_token(p, s, rb), last_token(p, s, rb));
 }
 
-// All threads of the CTA call; ends with a barrier.
+// a * b / c for c >= 1, in 32 bits where they hold it (a division in 64 is a chain of some hundred cycles, and this is on the way to the first tile).
+__device__ __forceinline__ long long mul_div(long long a, int b, long long c) {
+  const long long x = a * b;
+  return x < 0xffffffffll && c <= 0xffffffffll ? (long long)((uint32_t)x / (uint32_t)c) : x / c;
+}
+
+// A warp's plan, a lane per two sequences (lane l: sequences l and l + 32): the sequences, the units up to and including each, all units. Between the kernel's start and its
+// first load there is one round trip to memory and one scan. (A warp per sequence, with a barrier in front and behind, took 2.6 us for one sequence and 5.7 for 64.)
+constexpr int kPerLane = CAST_MAX_BATCH / 32;
+template <int PT, bool kTree>
+__device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[kPerLane], long long (&upto)[kPerLane], long long& units) {
+  const int lane = threadIdx.x & 31;
+  int L[kPerLane], n[kPerLane], F[kPerLane], off[kPerLane];
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j) {  // all loads first
+    const int b = j * 32 + lane;
+    const bool in = b < p.B;
+    L[j] = in ? p.kv_len[b] : 0;
+    n[j] = in ? p.n_new[b] : 0;
+    F[j] = in && p.first_row ? p.first_row[b] : 0;
+    off[j] = in && p.row_start ? p.row_start[b] : 0;
+  }
+  long long run = 0;
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j) {
+    const int b = j * 32 + lane;
+    ChunkSeq s = {max(L[j], 0), n[j], p.row_start ? off[j] : b * p.rows, 0, 0};
+    const int most = kTree ? p.Nmax : p.rows;
+    bool bad = kTree && s.n > most;  // (a chunk's count past its rows is cut to them)
+    s.n = min(max(s.n, 0), most);
+    if (p.row_start && s.n > 0 && (s.off < 0 || (long long)s.off + s.n > p.rows)) {
+      bad = true;
+      s.n = 0;
+    }
+    if (bad && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_TREE, b);
+    s.F = (unsigned short)(kTree ? min(max(F[j], 0), s.n) : 0);
+    if (s.n > s.F && (long long)s.L + s.n > p.max_pos) {
+      if (blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
+      s.L = min(s.L, p.max_pos);
+    }
+    if (kTree && p.first_row) {  // (a whole tree has its root, at depth 0)
+      for (unsigned left = __ballot_sync(0xffffffffu, s.n > s.F); left; left &= left - 1) {
+        const int l = __ffs(left) - 1;
+        ChunkSeq x = s;
+        x.n = __shfl_sync(0xffffffffu, s.n, l);
+        x.off = __shfl_sync(0xffffffffu, s.off, l);
+        int d = CAST_MAX_TREE;
+        for (int t = __shfl_sync(0xffffffffu, (int)s.F, l) + lane; t < x.n; t += 32) d = min(d, depth_of(p, x, t));
+        d = __reduce_min_sync(0xffffffffu, d);
+        if (lane == l) s.d0 = (unsigned short)d;
+      }
+    }
+    const int blocks = blocks_of(p, s);
+    long long u = 0;
+    if (blocks <= 4) {
+      for (int rb = 0; rb < blocks; ++rb) u += block_span<PT, kTree>(p, s, rb).n + kItemCost;
+    }
+    for (unsigned left = __ballot_sync(0xffffffffu, blocks > 4); left; left &= left - 1) {  // many row blocks: a lane each
+      const int l = __ffs(left) - 1, nb = __shfl_sync(0xffffffffu, blocks, l);
+      ChunkSeq x;
+      x.L = __shfl_sync(0xffffffffu, s.L, l);
+      x.n = __shfl_sync(0xffffffffu, s.n, l);
+      x.F = (unsigned short)__shfl_sync(0xffffffffu, (int)s.F, l);
+      x.d0 = (unsigned short)__shfl_sync(0xffffffffu, (int)s.d0, l);
+      long long y = 0;
+      for (int rb = lane; rb < nb; rb += 32) y += block_span<PT, kTree>(p, x, rb).n + kItemCost;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+      if (lane == l) u = y;
+    }
+    u *= p.Hkv;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, u, o);
+      if (lane >= o) u += y;
+    }
+    u += run;
+    run = __shfl_sync(0xffffffffu, u, 31);
+    seq[j] = s;
+    upto[j] = u;
+  }
+  units = run;
+}
+// CTAs that get a stretch.
+__device__ __forceinline__ int workers_of(const ChunkParams& p, long long units) {
+  const long long w = mul_div(units, 1, p.min_units);
+  return (int)(w < 1 ? 1 : w < (long long)gridDim.x ? w : (long long)gridDim.x);
+}
+
+// The plan in shared memory. All threads of the CTA call; ends with a barrier.
 template <int PT, bool kTree>
 __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  for (int b = tid; b < CAST_MAX_BATCH; b += blockDim.x) {
-    ChunkSeq s = {0, 0, 0, 0, 0};
-    int F = 0;
-    if (b < p.B) {
-      const long long all = p.row_start ? p.rows : (long long)p.B * p.rows;
-      s.L = max(p.kv_len[b], 0);
-      s.n = p.n_new[b];
-      if (p.first_row) F = p.first_row[b];
-      s.off = p.row_start ? p.row_start[b] : b * p.rows;
-      const int most = kTree ? p.Nmax : p.rows;
-      bool bad = false;
-      if (s.n > most) {
-        bad = kTree;  // (a chunk's count past its rows is cut to them)
-        s.n = most;
-      }
-      s.n = max(s.n, 0);
-      if (p.row_start && (s.off < 0 || (long long)s.off + s.n > all)) {
-        bad = s.n > 0;
-        s.n = 0;
-      }
-      if (bad && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_TREE, b);
-      F = min(max(F, 0), s.n);  // (with a tree, so it fits)
-      s.F = (unsigned short)(kTree ? F : 0);
-      if ((long long)s.L + s.n > p.g.max_pos() && s.n > s.F) {
-        if (blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
-        if (s.L > p.g.max_pos()) s.L = (int)p.g.max_pos();
-      }
-    }
-    pl.seq[b] = s;
-  }
-  __syncthreads();
-  for (int b = warp; b < CAST_MAX_BATCH; b += warps) {
-    long long u = 0;
-    if (b < p.B) {
-      ChunkSeq s = pl.seq[b];
-      if (kTree) {
-        int d = CAST_MAX_TREE;
-        for (int t = s.F + lane; t < s.n; t += 32) d = min(d, depth_of(p, s, t));
-        s.d0 = (unsigned short)__reduce_min_sync(0xffffffffu, d);
-        if (lane == 0) pl.seq[b].d0 = s.d0;
-      }
-      const int blocks = (int)(((long long)(s.n - s.F) * p.G + p.block_rows - 1) / p.block_rows);
-      for (int rb = lane; rb < blocks; rb += 32) u += block_span<PT, kTree>(p, s, rb).n + kItemCost;
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x < 32) {
+    ChunkSeq seq[kPerLane];
+    long long upto[kPerLane], units;
+    plan_warp<PT, kTree>(p, seq, upto, units);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-    }
-    if (lane == 0) pl.pre[b + 1] = u * p.Hkv;
-  }
-  __syncthreads();
-  if (warp == 0) {
-    long long run = 0;
-#pragma unroll
-    for (int j = 0; j < CAST_MAX_BATCH / 32; ++j) {
-      long long x = pl.pre[j * 32 + lane + 1];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      x += run;
-      __syncwarp();
-      pl.pre[j * 32 + lane + 1] = x;
-      run = __shfl_sync(0xffffffffu, x, 31);
+    for (int j = 0; j < kPerLane; ++j) {
+      pl.seq[j * 32 + lane] = seq[j];
+      pl.pre[j * 32 + lane + 1] = upto[j];
     }
     if (lane == 0) {
       pl.pre[0] = 0;
-      pl.units = run;
-      const long long w = run / p.min_units;
-      pl.workers = (int)(w < 1 ? 1 : w < (long long)gridDim.x ? w : (long long)gridDim.x);
+      pl.units = units;
+      pl.workers = workers_of(p, units);
     }
   }
   __syncthreads();
 }
 
-__device__ __forceinline__ long long bound_of(const ChunkPlan& pl, int c) { return pl.units * c / pl.workers; }
-__device__ __forceinline__ int owner_of(const ChunkPlan& pl, long long u) { return (int)(((u + 1) * pl.workers - 1) / pl.units); }
+__device__ __forceinline__ long long bound_of(long long units, int workers, int c) { return mul_div(units, c, workers); }
+__device__ __forceinline__ int owner_of(long long units, int workers, long long u) { return (int)mul_div((u + 1) * workers - 1, 1, units); }
+__device__ __forceinline__ long long bound_of(const ChunkPlan& pl, int c) { return bound_of(pl.units, pl.workers, c); }
+__device__ __forceinline__ int owner_of(const ChunkPlan& pl, long long u) { return owner_of(pl.units, pl.workers, u); }
 
 // A CTA's way along its stretch, item by item; every warp that follows it computes the same (all 32 lanes call).
 struct ChunkWalk {
@@ -204,8 +252,9 @@ __device__ __forceinline__ bool walk_begin(const ChunkParams& p, const ChunkPlan
     w.b += __popc(__ballot_sync(0xffffffffu, pl.pre[j * 32 + lane + 1] <= w.at));
   long long left = w.at - pl.pre[w.b], base = pl.pre[w.b];
   const ChunkSeq s = pl.seq[w.b];
-  w.blocks = (int)(((long long)(s.n - s.F) * p.G + p.block_rows - 1) / p.block_rows);
-  for (int rb0 = 0;; rb0 += 32) {  // the row block that the stretch begins in
+  w.blocks = blocks_of(p, s);
+  w.rb = 0;
+  for (int rb0 = 0; w.blocks > 1; rb0 += 32) {  // the row block that the stretch begins in
     const int rb = rb0 + lane;
     const long long own = rb < w.blocks ? (long long)(block_span<PT, kTree>(p, s, rb).n + kItemCost) * p.Hkv : 0;
     long long x = own;
@@ -228,7 +277,7 @@ __device__ __forceinline__ bool walk_begin(const ChunkParams& p, const ChunkPlan
   }
   walk_block<PT, kTree>(p, pl, w);
   const int len = w.span.n + kItemCost;
-  w.h = (int)(left / len);
+  w.h = (int)mul_div(left, 1, len);
   w.item0 = base + (long long)w.h * len;
   walk_item<PT, kTree>(p, pl, w);
   return true;
@@ -246,7 +295,7 @@ __device__ __forceinline__ bool walk_next(const ChunkParams& p, const ChunkPlan&
       do ++w.b;
       while (pl.pre[w.b + 1] == pl.pre[w.b]);  // (units are left, so a sequence with rows follows)
       const ChunkSeq s = pl.seq[w.b];
-      w.blocks = (int)(((long long)(s.n - s.F) * p.G + p.block_rows - 1) / p.block_rows);
+      w.blocks = blocks_of(p, s);
     }
     walk_block<PT, kTree>(p, pl, w);
   }
@@ -260,10 +309,10 @@ struct RowSight {
 };
 template <bool kTree>
 __device__ __forceinline__ RowSight sight_of(const ChunkParams& p, const ChunkSeq& s, int t, int depth) {
-  const long long pos = (long long)s.L + (kTree ? depth : t), max_pos = p.g.max_pos();
+  const long long pos = (long long)s.L + (kTree ? depth : t);
   RowSight r;
   const long long hi = kTree ? s.L : pos + 1;
-  r.hi = (int)(hi < max_pos ? hi : max_pos);
+  r.hi = (int)(hi < p.max_pos ? hi : p.max_pos);
   const long long lo = p.window > 0 ? pos - p.window + 1 : 0;
   r.lo = lo < 0 ? 0 : lo > 0x7fffffffll ? 0x7fffffff : (int)lo;
   r.sinks = p.window > 0 ? p.sinks : 0;
