@@ -6,13 +6,13 @@
 // when its softmax has done with a step. An item's rows decide how the two lanes share it:
 //   more than one block of rows (prompts, wide trees): lane 0 and lane 1 take a block each, and the K and V tiles serve both;
 //   one block (decoding, small trees): lane 0 takes the first half of every tile and lane 1 the second, each with its own running sums, and they join at the end.
-// Twenty warps: eight of softmax per lane (two threads a row, 32 positions of a step each), one that walks the line, hands the items out through a ring in shared
-// memory and loads Q and K (TMA), one that loads V and cleans it, and per lane one that issues its products: a
+// Twelve warps: four of softmax per lane (a thread a row), one that walks the line, hands the items out through a ring in shared memory and loads Q and K (TMA), one that
+// loads V and cleans it, and per lane one that issues its products: a
 // buffer's P V, then the next Q K^T into it, across the items' ends, so loads, products and softmax of the next item run under the output of the last.
 // What the single warps do per tile is a chain of dependent instructions and as much a bound as bytes and products are: one issuer for both lanes, loads of 64
-// positions, integer divisions by the page size, a load of the page table per tile were 1 us each or more. With one thread a row (two softmax warps per scheduler)
-// a step took a lane 2100 cycles, half of them exponentials, which both lanes wanted at the same time, and half the chain around them. With every warp walking the line
-// for itself the walk's state was spilled, and beside 227 KB of shared memory local memory does not stay in L1: few instructions between two steps took 600 cycles.
+// positions, integer divisions by the page size, a load of the page table per tile were 1 us each or more. With every warp walking the line for itself the walk's
+// state was spilled, and beside 227 KB of shared memory local memory does not stay in L1: few instructions between two steps took 600 cycles. (Two threads a row, half
+// of a step's positions each or every other step, took the softmax no less time, and the issuers more.)
 //
 // Softmax in one pass: P = 2^(s * scale + r) with a reference r per row that starts at 0 and moves, by a whole power of two, only when a tile's row sum
 // reaches 2^60 or all that a row has seen sums to less than 2^-60; the scores are still in tensor memory then, O is scaled there.
@@ -33,9 +33,9 @@ namespace {
 constexpr int kRows = 128;       // query rows of a lane (UMMA M)
 constexpr int kTile = 128;       // positions per tile
 constexpr int kStep = 64;        // positions per buffer of scores
-constexpr int kThreadsC = 640;
+constexpr int kThreadsC = 384;
 constexpr int kItems = 4;          // items handed out ahead
-constexpr int kItemReaders = 19;   // warps that read them
+constexpr int kItemReaders = 11;   // warps that read them
 constexpr int kRegQ = kRows * 128;   // a 64-dim half of a row block, 128-byte rows
 constexpr int kRegKV = kTile * 128;  // a 64-dim half of a tile
 constexpr uint32_t kColS = 0, kColO = 256, kLaneCols = 128, kTmemColumns = 512;  // a lane: two buffers of 64 scores; its output
@@ -94,7 +94,6 @@ struct TcArgs {
   int page_shift;  // position / page size = position * page_mul >> page_shift (an integer division is a chain of 130 cycles, and a loader has four a tile)
   uint32_t page_mul;
   float scale_log2;
-  float* mail;     // [grid][lane][2][128 rows][4]: between the threads of a row, in rare cases
 };
 
 // Whether n positions from pos0 on hold some that some rows of the item see and others do not.
@@ -191,13 +190,22 @@ __device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t (&r)[32]) {
       : "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_get16(uint32_t taddr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
       : "r"(taddr)
       : "memory");
 }
@@ -211,12 +219,11 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* dst, float a, float b,
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
-// An item's partials of one lane, joined by its 256 threads in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others): many rows two threads each,
+// An item's partials of one lane, joined by its 128 threads in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others): many rows a thread each,
 // 8 x 2 loads in flight; few rows four columns a thread, with eight contributors in flight.
 template <int HD>
-__device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out0, int tid, int rows, int c_lo, int c_hi, int lane_of) {
+__device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out0, int r, int rows, int c_lo, int c_hi, int lane_of) {
   constexpr int C4 = HD / 4;
-  const int r = tid & (kRows - 1);
   const float4* part = reinterpret_cast<const float4*>(p.part_o);
   auto block = [&](int c) { return part_block(c, c == c_lo, lane_of); };
   auto pair_of = [&](int c, int row) { return __ldcg(p.part_ml + block(c) * kRows + row); };
@@ -235,7 +242,7 @@ __device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out
     const float inv = l == 0.f ? 0.f : 1.f / l;
     __nv_bfloat16* dst = out_of(r);
 #pragma unroll 1
-    for (int k = tid >= kRows ? C4 / 2 : 0, end = k + C4 / 2; k < end; k += 8) {
+    for (int k = 0; k < C4; k += 8) {
       float4 acc[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -261,7 +268,7 @@ __device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out
     }
     return;
   }
-  for (int e = tid; e < rows * C4; e += 2 * kRows) {
+  for (int e = r; e < rows * C4; e += kRows) {
     const int row = e / C4, k = e % C4;
     float top = -INFINITY;
 #pragma unroll 8
@@ -307,7 +314,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       mbar_init(&ms.q_free[i], 4);  // (by both lanes' products and softmax)
       for (int j = 0; j < 2; ++j) {
         mbar_init(&ms.s_full[i][j], 1);
-        mbar_init(&ms.p_full[i][j], 2 * kRows / 32);
+        mbar_init(&ms.p_full[i][j], kRows / 32);
         mbar_init(&ms.pv_done[i][j], 1);
       }
     }
@@ -327,15 +334,15 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool aligned = (smem_u32(smem) & 1023u) == 0u;  // the swizzled regions need it
   if (!aligned && tid == 0) report(p.st, CAST_ERR_CUDA, 1024);
-  if (warp == 18) {
+  if (warp == 10) {
     // Tensor memory is taken behind the wait (a predecessor may hold some until it ends), and the dependents are released behind that.
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ms.tmem)), "n"(kTmemColumns));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
-  if (warp < 16 || warp == 18 || warp == 19) {  // who needs its address
+  if (warp < 8 || warp >= 10) {  // who needs its address
     tc_fence_before();
-    asm volatile("bar.sync 12, 576;" ::: "memory");
+    asm volatile("bar.sync 12, 320;" ::: "memory");
     tc_fence_after();
   }
   const uint32_t tmem = ms.tmem;
@@ -355,9 +362,9 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
     if (lane == 0) mbar_arrive(&ms.item_free[taken % kItems]);
     ++taken;
   };
-  if (warp == 16 || warp == 17) {
+  if (warp == 8 || warp == 9) {
     // =========================== loads: Q and K, or V ===========================
-    const bool is_v = warp == 17;
+    const bool is_v = warp == 9;
     const int stages = is_v ? M::kStagesV : M::kStagesK;
     int stage = 0, round = 0;  // of the next tile
     auto page_at = [&](int pos) { return (int)(((unsigned long long)(uint32_t)pos * a.page_mul) >> a.page_shift); };
@@ -624,13 +631,13 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       for (int j = cleaned; j < to_clean; ++j) mbar_wait(&ms.v_raw[j % M::kStagesV], (j / M::kStagesV) & 1);
       for (int j = max(0, qc - 2); j < qc; ++j) mbar_wait(&ms.q_full[j & 1], (j >> 1) & 1);
     }
-  } else if (warp >= 18) {
+  } else if (warp >= 10) {
     // =========================== a lane's products ===========================
     const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kStep >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
     const uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
     // Counts and conditions pass through warp reductions and votes of equal values: the compiler then knows this control flow to be uniform and keeps what the
     // products' operands are made from in uniform registers, where the instructions take them (moved there one by one they are 100 cycles a product).
-    const int h = __reduce_max_sync(0xffffffffu, warp - 18);
+    const int h = __reduce_max_sync(0xffffffffu, warp - 10);
     const uint32_t tm = __reduce_or_sync(0xffffffffu, tmem) + h * kLaneCols;
     const uint64_t dq = umma_desc(smem_u32(smem + M::kAtQ), 16, 1024);
     const uint64_t dk = umma_desc(smem_u32(smem + M::kAtK), 16, 1024);
@@ -647,7 +654,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       const uint64_t d = dv + (uint64_t)(stage * (M::kTileBytes >> 4) + ((e0 >> 4) & 1) * (kStep * 128 >> 4));
 #pragma unroll
       for (int ks = 0; ks < kStep / 16; ++ks)
-        umma_bf16_ts(tm + kColO, tm + kColS + buf * kStep + (ks >> 1) * 32 + (ks & 1) * 8, d + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
+        umma_bf16_ts(tm + kColO, tm + kColS + buf * kStep + ks * 8, d + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
       umma_commit(&ms.pv_done[h][buf]);
       if (e0 & 8) umma_commit(&ms.v_free[stage]);
       e0 = e1;
@@ -711,26 +718,13 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
     if (!ok && lane == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   } else {
     // =========================== softmax and output ===========================
-    // h: the lane; g: which 32 positions of a step; quad: which 32 rows (a warp reaches the tensor-memory lanes of its number modulo four)
-    const int h = warp >> 3, g = (warp >> 2) & 1, quad = warp & 3, r = quad * 32 + lane, tid_lane = tid & 255;
+    // (a warp reaches the 32 tensor-memory lanes of its number modulo four)
+    const int h = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
     const uint32_t rowsel = (uint32_t)(quad * 32) << 16;
-    const uint32_t t_s0 = tmem + kColS + h * kLaneCols + rowsel + g * 32, t_o = tmem + kColO + rowsel;  // (t_o: lane 0's output, lane 1's behind it)
-    const int pair_id = 1 + h * 4 + quad, lane_id = 9 + h;
-    auto sync_pair = [&] { asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory"); };
-    auto sync_lane = [&] { asm volatile("bar.sync %0, 256;" ::"r"(lane_id) : "memory"); };
-    auto sync_both = [&] { asm volatile("bar.sync 11, 512;" ::: "memory"); };
-    auto any_of_pair = [&](bool x) {  // of both threads of any of these 32 rows
-      int y;
-      asm volatile(
-          "{\n\t.reg .pred p, q;\n\t"
-          "setp.ne.s32 p, %1, 0;\n\t"
-          "barrier.cta.red.or.pred q, %2, 64, p;\n\t"
-          "selp.s32 %0, 1, 0, q;\n\t}"
-          : "=r"(y)
-          : "r"(x ? 1 : 0), "r"(pair_id)
-          : "memory");
-      return y != 0;
-    };
+    const uint32_t t_s0 = tmem + kColS + h * kLaneCols + rowsel, t_o = tmem + kColO + rowsel;  // (t_o: lane 0's output, lane 1's behind it)
+    const int lane_id = 1 + h;
+    auto sync_lane = [&] { asm volatile("bar.sync %0, 128;" ::"r"(lane_id) : "memory"); };
+    auto sync_both = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
     const float sc = a.scale_log2;
     const unsigned long long sc2 = pack_f2(sc, sc);
     const int r_tok = r / p.G, r_head = r - r_tok * p.G;
@@ -746,7 +740,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       const bool row_ok = r < lane_rows, warp_live = quad * 32 < lane_rows;
       const int tok = tok0 + (row_ok ? r_tok : 0);
       if (T == 0) {
-        if (row_ok && g == 0 && (pair || h == 0)) {
+        if (row_ok && (pair || h == 0)) {
           __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (((size_t)it.off + tok) * p.Hq + it.h * p.G + r_head) * HD;
           for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(out + c * 8) = make_uint4(0u, 0u, 0u, 0u);
         }
@@ -766,7 +760,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
 #pragma unroll
         for (int c = 0; c < 32; ++c) z[c] = 0u;
 #pragma unroll
-        for (int c = 0; c < HD / 2; c += 32) tmem_st32(t_o + h * kLaneCols + g * (HD / 2) + c, z);
+        for (int c = 0; c < HD; c += 32) tmem_st32(t_o + h * kLaneCols + c, z);
         tmem_wait_st();
       }
       const int count = pair ? 2 * T : T, hi_plain = hi_all - kStep;
@@ -797,118 +791,120 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
         const uint32_t t_s = t_s0 + buf * kStep;
         tc_fence_after();
         const bool plain = here <= hi_plain && (here >= lo_all || here + kStep <= rs.sinks);
-        auto seen_bits = [&]() -> uint32_t {  // what the row sees of this thread's 32 positions
-          const int base = here + g * 32;
+        auto seen_word = [&](int j) -> uint32_t {  // what the row sees of positions here + 32 j on
+          if (plain) return row_ok ? 0xffffffffu : 0u;
+          const int base = here + j * 32;
           uint32_t v = bits_below(rs.hi - base) & (~bits_below(rs.lo - base) | bits_below(rs.sinks - base));
           if (kTree) {
-            const int st = base - s.L, wi = st >> 5, sh = st & 31;  // (arithmetic shift)
+            const int st = base - it.L, wi = st >> 5, sh = st & 31;  // (arithmetic shift)
             auto word = [&](int x) { return x == 0 ? aw[0] : x == 1 ? aw[1] : x == 2 ? aw[2] : x == 3 ? aw[3] : 0u; };
             v |= __funnelshift_r(word(wi), word(wi + 1), sh);
           }
           return row_ok ? v : 0u;
         };
-        uint32_t pk[16];
-        unsigned long long sum = pack_f2(0.f, 0.f), check = sum;
-        uint32_t seen = row_ok ? 0xffffffffu : 0u;
-        {
-          const unsigned long long ref2 = pack_f2(ref, ref);
-          uint32_t x[32];
-          tmem_get32(t_s, x);
-          if (plain) {
-            weigh<false>(x, sc2, ref2, 0u, sum, check, pk);
-          } else {
-            seen = seen_bits();
-            weigh<true>(x, sc2, ref2, seen, sum, check, pk);
-          }
-        }
+        uint32_t pk[32];
         float l0, l1;
-        unpack_f2(add_f2(sum, check), l0, l1);
-        l0 += l1;
+        {
+          unsigned long long sum_a = pack_f2(0.f, 0.f), sum_b = sum_a, check = sum_a;
+          const unsigned long long ref2 = pack_f2(ref, ref);
+          uint32_t x[64];
+          tmem_get64(t_s, x);
+          if (plain) {
+            weigh<false>(x, sc2, ref2, 0u, sum_a, check, pk);
+            weigh<false>(x + 32, sc2, ref2, 0u, sum_b, check, pk + 16);
+          } else {
+            weigh<true>(x, sc2, ref2, seen_word(0), sum_a, check, pk);
+            weigh<true>(x + 32, sc2, ref2, seen_word(1), sum_b, check, pk + 16);
+          }
+          unpack_f2(add_f2(add_f2(sum_a, sum_b), check), l0, l1);
+          l0 += l1;
+        }
         // far: 2^60 or more (or no number); low: less than 2^-60 so far, and something seen
-        if (any_of_pair((row_ok && !(l0 < 1.15e18f)) || (seen != 0u && l_run + l0 < 8.6e-19f))) {
-          uint32_t sa[32];
-          tmem_get32(t_s, sa);
+        const bool far = row_ok && !(l0 < 1.15e18f);
+        bool low = row_ok && l_run + l0 < 8.6e-19f;
+        if (!plain) low = low && (seen_word(0) | seen_word(1)) != 0u;
+        if (__any_sync(0xffffffffu, far || low)) {
           float top = -INFINITY;
+#pragma unroll 1
+          for (int j = 0; j < 2; ++j) {
+            uint32_t x[32];
+            tmem_get32(t_s + j * 32, x);
+            const uint32_t v = seen_word(j);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) top = fmaxf(top, ((seen >> c) & 1u) ? __uint_as_float(sa[c]) : -INFINITY);
-          // both threads of the row see both halves' largest exponent and sums, and come to the same step
-          float4* const mail = reinterpret_cast<float4*>(a.mail) + (size_t)(blockIdx.x * 2 + h) * 2 * kRows + r;
-          const float4 mine = make_float4(top > -INFINITY ? fmaf(top, sc, ref) : -INFINITY, l_run, l0, seen != 0u ? 1.f : 0.f);
-          __stcg(mail + g * kRows, mine);
-          sync_pair();
-          const float4 theirs = __ldcg(mail + (g ^ 1) * kRows);
-          const float l_old = mine.y + theirs.y, l_new = mine.z + theirs.z;
+            for (int c = 0; c < 32; ++c) top = fmaxf(top, ((v >> c) & 1u) ? __uint_as_float(x[c]) : -INFINITY);
+          }
           float kf = 0.f;
-          if (row_ok && (!(l_new < 1.15e18f) || (mine.w + theirs.w > 0.f && l_old + l_new < 8.6e-19f))) {
-            const float e = fmaxf(fmaxf(mine.x, theirs.x), l_old > 0.f ? log2f(l_old) : -INFINITY);
+          if (far || low) {
+            const float e = fmaxf(top > -INFINITY ? fmaf(top, sc, ref) : -INFINITY, l_run > 0.f ? log2f(l_run) : -INFINITY);
             if (e > -INFINITY && e < INFINITY) kf = fminf(fmaxf(ceilf(e), -1.0e9f), 1.0e9f);
           }
-          const float alpha = l_old > 0.f ? ldexpf(1.f, -(int)kf) : 1.f;
+          const float alpha = l_run > 0.f ? ldexpf(1.f, -(int)kf) : 1.f;
           if (__any_sync(0xffffffffu, alpha != 1.f)) {
             settle();
 #pragma unroll 1
-            for (int c = 0; c < HD / 2; c += 32) {
-              const uint32_t to = t_o + h * kLaneCols + g * (HD / 2) + c;
-              tmem_get32(to, sa);
+            for (int c = 0; c < HD; c += 32) {
+              uint32_t x[32];
+              tmem_get32(t_o + h * kLaneCols + c, x);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) sa[e] = __float_as_uint(__uint_as_float(sa[e]) * alpha);
-              tmem_st32(to, sa);
+              for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
+              tmem_st32(t_o + h * kLaneCols + c, x);
             }
             tmem_wait_st();
           }
           l_run *= alpha;
           ref -= kf;
           // the step again, for the rows that it is about (the others keep what they have: a row's bits are not its neighbours' business)
-          const bool redo = kf != 0.f || !(l_new < 1.15e18f);
-          uint32_t again[16];
-          sum = check = pack_f2(0.f, 0.f);
-          tmem_get32(t_s, sa);
-          weigh<true>(sa, sc2, pack_f2(ref, ref), seen, sum, check, again);
-          unpack_f2(sum, top, l1);
-          l0 = redo ? top + l1 : l0;
+          const bool mine = far || kf != 0.f;
+          float again = 0.f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) pk[e] = redo ? again[e] : pk[e];
+          for (int j = 0; j < 2; ++j) {
+            uint32_t x[32], q[16];
+            unsigned long long sum = pack_f2(0.f, 0.f), check = sum;
+            tmem_get32(t_s + j * 32, x);
+            weigh<true>(x, sc2, pack_f2(ref, ref), seen_word(j), sum, check, q);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) pk[16 * j + e] = mine ? q[e] : pk[16 * j + e];
+            float s0, s1;
+            unpack_f2(sum, s0, s1);
+            again += s0 + s1;
+          }
+          l0 = mine ? again : l0;
         }
         if (in_part(it, here, kStep)) {  // (also where this warp's rows see it whole)
           const int stage = (vtile + at) % M::kStagesV;
           if (ok) ok = mbar_wait(&ms.v_full[stage], ((vtile + at) / M::kStagesV) & 1);
-          const uint32_t bad0 = ms.bad[stage][half * 2], bad1 = ms.bad[stage][half * 2 + 1];
-          if (bad0 | bad1) {
-            // V rows that hold a NaN or an infinity, found when the tile was cleaned: one thread of a row after the other adds those of its positions
+          if (ms.bad[stage][half * 2] | ms.bad[stage][half * 2 + 1]) {
+            // V rows that hold a NaN or an infinity, found when the tile was cleaned: their weighted values go to the output from here
             settle();
-            if (g == 1) {
-              sync_pair();
-              tc_fence_after();
-            }
-            for (uint32_t left = g ? bad1 : bad0; left; left &= left - 1) {
-              const int bit = __ffs(left) - 1;
-              if (!__any_sync(0xffffffffu, (seen >> bit) & 1u)) continue;
-              uint32_t x, sa[32];
-              tmem_get1(t_s + bit, x);
-              const float wt = ((seen >> bit) & 1u) ? fast_exp2(fmaf(__uint_as_float(x), sc, ref)) : 0.f;
-              int page = 0, slot = 0;
-              if (!find_place(p.g, it.b, here + g * 32 + bit, page, slot)) page = 0;
-              const size_t place = (((size_t)page * (p.g.page_size == 0 ? p.g.seq_capacity : p.g.page_size) + slot) * p.Hkv + it.h) * HD;
-              const __nv_bfloat16* row = reinterpret_cast<const __nv_bfloat16*>(p.v) + place;
 #pragma unroll 1
-              for (int c = 0; c < HD; c += 32) {
-                tmem_get32(t_o + h * kLaneCols + c, sa);
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t seen = seen_word(j);
+              for (uint32_t left = ms.bad[stage][half * 2 + j]; left; left &= left - 1) {
+                const int bit = __ffs(left) - 1;
+                if (!__any_sync(0xffffffffu, (seen >> bit) & 1u)) continue;
+                uint32_t x, sa[32];
+                tmem_get1(t_s + j * 32 + bit, x);
+                const float wt = ((seen >> bit) & 1u) ? fast_exp2(fmaf(__uint_as_float(x), sc, ref)) : 0.f;
+                int page = 0, slot = 0;
+                if (!find_place(p.g, it.b, here + j * 32 + bit, page, slot)) page = 0;
+                const size_t place = (((size_t)page * (p.g.page_size == 0 ? p.g.seq_capacity : p.g.page_size) + slot) * p.Hkv + it.h) * HD;
+                const __nv_bfloat16* row = reinterpret_cast<const __nv_bfloat16*>(p.v) + place;
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 32) {
+                  tmem_get32(t_o + h * kLaneCols + c, sa);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  const float f = __bfloat162float(row[c + e]);
-                  if ((seen >> bit) & 1u) sa[e] = __float_as_uint(fmaf(wt, f, __uint_as_float(sa[e])));
+                  for (int e = 0; e < 32; ++e) {
+                    const float f = __bfloat162float(row[c + e]);
+                    if ((seen >> bit) & 1u) sa[e] = __float_as_uint(fmaf(wt, f, __uint_as_float(sa[e])));
+                  }
+                  tmem_st32(t_o + h * kLaneCols + c, sa);
                 }
-                tmem_st32(t_o + h * kLaneCols + c, sa);
+                tmem_wait_st();
               }
-              tmem_wait_st();
-            }
-            if (g == 0) {
-              tc_fence_before();
-              sync_pair();
             }
           }
         }
-        tmem_st16(t_s, pk);
+        tmem_st32(t_s, pk);
         l_run += l0;
         tmem_wait_st();
         tc_fence_before();
@@ -922,27 +918,15 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       if (!ok) l_run = 0.f;  // a wait ran out: nothing of this counts
       const bool whole = it.whole != 0;
       // The row's sum, and what its outputs are multiplied by: the threads of a row tell one another.
-      float m = -INFINITY, l = 0.f, f0 = 0.f, f1 = 0.f;
-      if (g == 1) (&ms.row[r].x)[h] = l_run;
-      sync_pair();
-      if (g == 0) {
-        l = l_run + (&ms.row[r].x)[h];
-        m = l == 0.f ? -INFINITY : -ref;
-      }
+      float m = l_run == 0.f ? -INFINITY : -ref, l = l_run, f0 = 1.f, f1 = 0.f;
       if (pair) {
-        if (g == 0) {
-          f0 = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-          (&ms.row[r].x)[h] = f0;
-        }
-        sync_pair();
-        f0 = (&ms.row[r].x)[h];
-      } else {  // lane 0 joins both
-        sync_both();
-        if (h == 1 && g == 0) ms.row[r] = make_float2(m, l);
+        if (whole) f0 = l == 0.f ? 0.f : 1.f / l;
+      } else {  // the lanes join: lane 0 puts the two together, each writes half of the columns
+        if (h == 1) ms.row[r] = make_float2(m, l);
         tc_fence_before();
         sync_both();
         tc_fence_after();
-        if (h == 0 && g == 0) {
+        if (h == 0) {
           const float2 o = ms.row[r];
           const float top = fmaxf(m, o.x);
           f0 = m > -INFINITY ? exp2f(m - top) : 0.f;
@@ -970,24 +954,23 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       const int slot = (pair ? qc + h : qc) & 1;
       unsigned char* const stage_rows = smem + M::kAtQ + slot * M::kQ;
       constexpr int CH = HD / 8;
-      // a thread's columns: half of them, or where both lanes share the rows a quarter
-      const int cols = pair ? HD / 2 : HD / 4, col0 = pair ? g * (HD / 2) : (h * 2 + g) * (HD / 4);
+      const int cols = pair ? HD : HD / 2, col0 = pair ? 0 : h * (HD / 2);  // this thread's columns
       if (warp_live) {
 #pragma unroll 1
-        for (int c = col0; c < col0 + cols; c += 16) {
-          uint32_t o[16];
-          float x[16];
-          tmem_get16(t_o + (pair ? h : 0) * kLaneCols + c, o);
+        for (int c = col0; c < col0 + cols; c += 32) {
+          uint32_t o[32];
+          float x[32];
+          tmem_get32(t_o + (pair ? h : 0) * kLaneCols + c, o);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = f0 != 0.f ? __uint_as_float(o[e]) * f0 : 0.f;
+          for (int e = 0; e < 32; ++e) x[e] = f0 != 0.f ? __uint_as_float(o[e]) * f0 : 0.f;
           if (!pair) {
-            tmem_get16(t_o + kLaneCols + c, o);
+            tmem_get32(t_o + kLaneCols + c, o);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = f1 != 0.f ? fmaf(__uint_as_float(o[e]), f1, x[e]) : x[e];
+            for (int e = 0; e < 32; ++e) x[e] = f1 != 0.f ? fmaf(__uint_as_float(o[e]), f1, x[e]) : x[e];
           }
           if (whole) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 8) {
+            for (int e = 0; e < 32; e += 8) {
               uint32_t u[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
@@ -998,17 +981,17 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
             }
           } else if (row_ok) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) __stcg(part + (size_t)((c + e) / 4) * kRows, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+            for (int e = 0; e < 32; e += 4) __stcg(part + (size_t)((c + e) / 4) * kRows, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
           }
         }
       }
       tc_fence_before();
-      if (!whole && row_ok && g == 0 && (pair || h == 0)) __stcg(p.part_ml + mine_at * kRows + r, make_float2(m, l));
+      if (!whole && row_ok && (pair || h == 0)) __stcg(p.part_ml + mine_at * kRows + r, make_float2(m, l));
       if (pair) sync_lane();
       else sync_both();
       tc_fence_after();
       if (whole) {
-        const int at = pair ? tid_lane : tid, by = pair ? 256 : 512;
+        const int at = pair ? r : tid, by = pair ? kRows : 2 * kRows;
         for (int e = at; e < lane_rows * CH; e += by) {
           const int rr = e / CH, c = e % CH, tk = rr / p.G;
           const uint4 x = *reinterpret_cast<const uint4*>(stage_rows + rr * (HD * 2) + ((c ^ (rr & (CH - 1))) << 4));
@@ -1016,7 +999,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
         }
         fence_proxy_async();  // (the next copy of Q into this place goes by the async proxy)
         sync_lane();
-      } else if ((pair || h == 0) && tid_lane == 0) {
+      } else if ((pair || h == 0) && r == 0) {
         // releases this CTA's partial (the barrier made it this thread's to release), acquires those that came earlier
         int32_t* ticket = p.ticket + 2 * c_lo + lane_of;
         int t;
@@ -1024,20 +1007,20 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
         ms.last[h] = t == c_hi - c_lo;
         if (t == c_hi - c_lo) *ticket = 0;  // ready for the next launch
       }
-      if (tid_lane == 0) {
+      if (r == 0) {
         mbar_arrive(&ms.q_free[qc & 1]);
         if (pair) mbar_arrive(&ms.q_free[(qc + 1) & 1]);
       }
       qc += pair ? 2 : 1;
       if (whole || (!pair && h == 1)) continue;
       sync_lane();
-      if (ms.last[h]) merge_rows<HD>(p, out0, tid_lane, lane_rows, c_lo, c_hi, lane_of);
+      if (ms.last[h]) merge_rows<HD>(p, out0, r, lane_rows, c_lo, c_hi, lane_of);
     }
-    if (!ok && tid_lane == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
+    if (!ok && r == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 18) {
+  if (warp == 10) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns));
   }
@@ -1099,10 +1082,10 @@ cast_status launch(const ChunkParams& p, const TcArgs& a, int grid, const CUtens
 
 }  // namespace
 
-// Bytes behind the tickets: two partials of two row blocks per CTA, and the rows' mail.
+// Bytes behind the tickets: two partials of two row blocks per CTA.
 size_t chunk_attention_tc_workspace(const cast_ctx* c, int D) {
   const size_t grid = c->num_sms < kChunkGrid ? c->num_sms : kChunkGrid;
-  return grid * 2 * (2 * kRows) * (D + 2) * sizeof(float) + grid * 2 * 2 * kRows * 4 * sizeof(float);
+  return grid * 2 * (2 * kRows) * (D + 2) * sizeof(float);
 }
 
 // False where the shape is not this path's: a page that is no multiple of 8 positions (a copy is 8 at least), a group of more heads than a
@@ -1132,7 +1115,6 @@ bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspa
   const int grid = c->num_sms < kChunkGrid ? c->num_sms : kChunkGrid;
   p.part_o = reinterpret_cast<float*>(workspace);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)grid * 2 * (2 * kRows) * D);
-  a.mail = reinterpret_cast<float*>(p.part_ml + (size_t)grid * 2 * (2 * kRows));
   if (p.anc) *status = D == 64 ? launch<64, true>(p, a, grid, mq, mk, mv, s) : launch<128, true>(p, a, grid, mq, mk, mv, s);
   else *status = D == 64 ? launch<64, false>(p, a, grid, mq, mk, mv, s) : launch<128, false>(p, a, grid, mq, mk, mv, s);
   return true;
