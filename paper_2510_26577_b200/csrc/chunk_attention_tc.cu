@@ -219,47 +219,59 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* dst, float a, float b,
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
-// An item's partials of one lane, joined by its 128 threads in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others): many rows a thread each,
-// 8 x 2 loads in flight; few rows four columns a thread, with eight contributors in flight.
+// An item's partials of one lane, joined in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others) by `threads` threads: many rows 128 threads to a
+// part of the columns, two contributors of eight times four columns in flight; few rows four columns a thread, with eight contributors in flight.
 template <int HD>
-__device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out0, int r, int rows, int c_lo, int c_hi, int lane_of) {
+__device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out0, int t, int threads, int rows, int c_lo, int c_hi, int lane_of) {
   constexpr int C4 = HD / 4;
   const float4* part = reinterpret_cast<const float4*>(p.part_o);
   auto block = [&](int c) { return part_block(c, c == c_lo, lane_of); };
   auto pair_of = [&](int c, int row) { return __ldcg(p.part_ml + block(c) * kRows + row); };
   auto out_of = [&](int row) { return out0 + ((size_t)(row / p.G) * p.Hq + row % p.G) * HD; };
   if (rows > 16) {
+    const int r = t & (kRows - 1), cols = C4 * kRows / threads, col0 = t / kRows * cols;
     if (r >= rows) return;
-    float top = -INFINITY;
-#pragma unroll 4
-    for (int c = c_lo; c <= c_hi; ++c) top = fmaxf(top, pair_of(c, r).x);
-    float l = 0.f;
-#pragma unroll 4
-    for (int c = c_lo; c <= c_hi; ++c) {
-      const float2 ml = pair_of(c, r);
-      if (ml.x > -INFINITY) l = fmaf(exp2f(ml.x - top), ml.y, l);
+    float top = -INFINITY, l = 0.f;
+    for (int c0 = c_lo; c0 <= c_hi; c0 += 8) {
+      float2 ml[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ml[k] = c0 + k <= c_hi ? pair_of(c0 + k, r) : make_float2(-INFINITY, 0.f);
+      const float before = top;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+      if (l != 0.f) l *= exp2f(before - top);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (ml[k].x > -INFINITY) l = fmaf(exp2f(ml[k].x - top), ml[k].y, l);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     __nv_bfloat16* dst = out_of(r);
 #pragma unroll 1
-    for (int k = 0; k < C4; k += 8) {
+    for (int k = col0; k < col0 + cols; k += 8) {
       float4 acc[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-      for (int c = c_lo; c <= c_hi; ++c) {
-        float4 x[8];
-        const float m = pair_of(c, r).x;
+#pragma unroll 1
+      for (int c0 = c_lo; c0 <= c_hi; c0 += 2) {
+        float4 x[2][8];
+        float f[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __ldcg(part + (block(c) * C4 + k + e) * kRows + r);
-        if (m > -INFINITY) {
-          const float f = exp2f(m - top);
+        for (int u = 0; u < 2; ++u) {
+          const int c = min(c0 + u, c_hi);
+          f[u] = c0 + u <= c_hi ? pair_of(c, r).x : -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[u][e] = __ldcg(part + (block(c) * C4 + k + e) * kRows + r);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (f[u] == -INFINITY) continue;
+          const float w = exp2f(f[u] - top);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            acc[e].x = fmaf(f, x[e].x, acc[e].x);
-            acc[e].y = fmaf(f, x[e].y, acc[e].y);
-            acc[e].z = fmaf(f, x[e].z, acc[e].z);
-            acc[e].w = fmaf(f, x[e].w, acc[e].w);
+            acc[e].x = fmaf(w, x[u][e].x, acc[e].x);
+            acc[e].y = fmaf(w, x[u][e].y, acc[e].y);
+            acc[e].z = fmaf(w, x[u][e].z, acc[e].z);
+            acc[e].w = fmaf(w, x[u][e].w, acc[e].w);
           }
         }
       }
@@ -268,7 +280,7 @@ __device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out
     }
     return;
   }
-  for (int e = r; e < rows * C4; e += kRows) {
+  for (int e = t; e < rows * C4; e += threads) {
     const int row = e / C4, k = e % C4;
     float top = -INFINITY;
 #pragma unroll 8
@@ -456,7 +468,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
             x.tf = first_token(p, cur, rb);
             const int tl = last_token(p, cur, rb);
             x.rows = (tl + 1 - x.tf) * p.G;
-            x.pair = x.rows * 2 > p.block_rows;
+            x.pair = x.rows > a.tokens * p.G;
             const long long hm = (long long)cur.L + (kTree ? 0 : x.tf + 1);
             x.hi_min = (int)(hm < sp.hi ? hm : sp.hi);
             const long long lm = p.window > 0 ? (long long)cur.L + (kTree ? CAST_MAX_TREE : tl) - p.window + 1 : 0;
@@ -1012,9 +1024,10 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
         if (pair) mbar_arrive(&ms.q_free[(qc + 1) & 1]);
       }
       qc += pair ? 2 : 1;
-      if (whole || (!pair && h == 1)) continue;
-      sync_lane();
-      if (ms.last[h]) merge_rows<HD>(p, out0, r, lane_rows, c_lo, c_hi, lane_of);
+      if (whole) continue;
+      if (pair) sync_lane();
+      else sync_both();  // (both lanes join the partials)
+      if (ms.last[lane_of]) merge_rows<HD>(p, out0, pair ? r : tid, pair ? kRows : 2 * kRows, lane_rows, c_lo, c_hi, lane_of);
     }
     if (!ok && r == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   }
@@ -1104,8 +1117,11 @@ bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspa
   a.page_shift = 31 + lg;  // (exact for positions below 2^31: the multiplier is at most page_size - 1 too large in 2^shift)
   a.page_mul = p.g.page_size ? (uint32_t)(((1ull << a.page_shift) + p.g.page_size - 1) / p.g.page_size) : 0u;
   a.scale_log2 = p.scale * 1.4426950408889634f;
-  p.block_rows = 2 * a.tokens * p.G;
-  p.block_tokens = 2 * a.tokens;
+  // Pairs of row blocks share their tiles' loads. Where there are fewer of them than SMs, blocks by themselves spread over twice as many, and their lanes take half of the
+  // positions each (one sequence of 8192, 60 tokens, 32/8 heads under a window of 1024: 36 -> 26 us).
+  const long long pairs = p.Hkv * (p.row_start ? p.rows / (2 * a.tokens) + (long long)p.B : (long long)p.B * ((most + 2 * a.tokens - 1) / (2 * a.tokens)));
+  p.block_tokens = pairs < c->num_sms ? a.tokens : 2 * a.tokens;
+  p.block_rows = p.block_tokens * p.G;
   p.min_units = kItemCost + 2;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   CUtensorMap mq, mk, mv;
