@@ -16,14 +16,13 @@ using namespace cast;
 namespace {
 
 constexpr int kThreadsA = 256;
-constexpr int kMaxRows = 4;  // rows per CTA at most
 constexpr int kMaxPairs = 64;
 
 struct AppendParams {
   const unsigned char *q, *k, *v;
   size_t q_stride, k_stride, v_stride;  // bytes from a row to the next
   unsigned char *q_out, *k_cache, *v_cache;
-  int B, rows, Hq, Hkv, rb;             // rb: rows per CTA
+  int B, rows, Hq, Hkv, parts_log2;     // warps per row
   const int32_t *row_start, *first_row, *n_rows, *depth, *position, *start;
   const double* inv_freq;
   int rot_dim, interleaved;
@@ -56,20 +55,34 @@ template <> struct Piece<__nv_bfloat16> {
   }
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreadsA) append_kernel(const AppendParams p) {
-  constexpr int CH = Piece<T>::N, LPH = D / CH, HPW = 32 / LPH;  // dims per lane, lanes per head, heads per warp at a time
-  constexpr int kGroups = kThreadsA / LPH, UN = 4;
+// Where a rotating dim's partner lies: beside it; half a rotation away and that is a whole number of lanes; half a rotation away anywhere.
+enum { kBeside, kLanes, kAnywhere };
+
+template <typename T, int D, int MODE>
+__global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_constant__ AppendParams p) {
+  constexpr int CH = Piece<T>::N, LPH = D / CH, HPW = 32 / LPH;  // dims per lane, lanes per head, heads per piece
+  constexpr int kPiece = 512, UN = 4;                            // bytes a warp takes at a time; pieces in flight
   constexpr int KB = CAST_MAX_BATCH / 32;
-  __shared__ float2 cs[kMaxRows][kMaxPairs];
-  __shared__ long long place_s[kMaxRows];                          // row of the cache, -1: none
-  __shared__ alignas(16) float turn_s[kThreadsA / 32][HPW * D];
+  __shared__ float2 cs[kThreadsA / 32][kMaxPairs];
+  __shared__ float w_s[2][D];
+  __shared__ alignas(16) unsigned char turn_s[MODE == kAnywhere ? kThreadsA / 32 : 1][kPiece];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int group = tid / LPH, lig = tid % LPH;                    // lane in its group
-  const int heads = (p.q ? p.Hq : 0) + (p.k ? 2 * p.Hkv : 0), q_heads = p.q ? p.Hq : 0;
+  const int d0 = lane % LPH * CH, half = p.rot_dim / 2;            // first dim of the lane
+  const int nq = p.q ? (p.Hq + HPW - 1) / HPW : 0, nk = p.k ? (p.Hkv + HPW - 1) / HPW : 0, pieces = nq + 2 * nk;
+  const uint32_t q_bytes = (uint32_t)p.Hq * (uint32_t)(D * sizeof(T)), k_bytes = (uint32_t)p.Hkv * (uint32_t)(D * sizeof(T));
   const long long all_rows = p.row_start ? p.rows : (long long)p.B * p.rows;
+  const long long max_pos = p.g.max_pos();
+
+  // what no row changes: frequencies in turns, weights
+  double freq[kMaxPairs / 32];
+#pragma unroll
+  for (int j = 0; j < kMaxPairs / 32; ++j) freq[j] = j * 32 + lane < half ? p.inv_freq[j * 32 + lane] * 0.15915494309189533577 : 0.;
+  for (int d = tid; d < 2 * D; d += kThreadsA) {
+    const float* w = d < D ? p.q_weight : p.k_weight;
+    w_s[d / D][d % D] = w ? w[d % D] : 1.f;
+  }
 
   // live rows of the sequences: lane b % 32 holds sequence b's
   int cnt[KB], first[KB], off[KB], before[KB];
@@ -100,9 +113,12 @@ __global__ void __launch_bounds__(kThreadsA) append_kernel(const AppendParams p)
     before[j] = live + x - cnt[j];
     live += __shfl_sync(0xffffffffu, x, 31);
   }
-  // row i of the live ones: its sequence and token (the whole warp calls)
-  auto find = [&](int i, int& b, int& t, int& row) {
-    b = t = row = 0;
+  __syncthreads();  // the weights
+
+  const int parts = 1 << p.parts_log2;
+  for (int u = (int)blockIdx.x * (kThreadsA / 32) + warp; u >> p.parts_log2 < live; u += (int)gridDim.x * (kThreadsA / 32)) {
+    const int i = u >> p.parts_log2;
+    int b = 0, t = 0, row = 0;  // the i-th live row: its sequence, its token, its place among all
 #pragma unroll
     for (int j = 0; j < KB; ++j) {
       const unsigned hit = __ballot_sync(0xffffffffu, i >= before[j] && i - before[j] < cnt[j]);
@@ -113,136 +129,127 @@ __global__ void __launch_bounds__(kThreadsA) append_kernel(const AppendParams p)
         row = __shfl_sync(0xffffffffu, off[j], l) + t;
       }
     }
-  };
-
-  const int half = p.rot_dim / 2, d0 = lig * CH;
-  const long long max_pos = p.g.max_pos();
-  for (int i0 = (int)blockIdx.x * p.rb; i0 < live; i0 += (int)gridDim.x * p.rb) {
-    const int here = min(p.rb, live - i0);
-    int b[kMaxRows], t[kMaxRows], row[kMaxRows];
-#pragma unroll
-    for (int r = 0; r < kMaxRows; ++r) {
-      b[r] = t[r] = row[r] = 0;
-      if (r < here) find(i0 + r, b[r], t[r], row[r]);
-    }
-    auto pick = [&](const int (&x)[kMaxRows], int r) { return r == 0 ? x[0] : r == 1 ? x[1] : r == 2 ? x[2] : x[3]; };
-    // (head, row) pairs, a group of lanes each: the first loads go out before the angles are formed
-    const int units = here * heads;
-    auto source = [&](int u) {
-      const int r = u / heads, h = u - r * heads;
-      const size_t at = (size_t)pick(row, r);
-      const unsigned char* base = h < q_heads ? p.q + at * p.q_stride + (size_t)h * (D * sizeof(T))
-                                  : h < q_heads + p.Hkv ? p.k + at * p.k_stride + (size_t)(h - q_heads) * (D * sizeof(T))
-                                                        : p.v + at * p.v_stride + (size_t)(h - q_heads - p.Hkv) * (D * sizeof(T));
-      return *reinterpret_cast<const uint4*>(base + lig * 16);
+    // A piece is 512 bytes of one tensor's row, sixteen a lane.
+    const unsigned char *q_row = p.q + (size_t)row * p.q_stride, *k_row = p.k + (size_t)row * p.k_stride, *v_row = p.v + (size_t)row * p.v_stride;
+    auto load = [&](int j) {
+      const unsigned char* base = j < nq ? q_row : j < nq + nk ? k_row : v_row;
+      const uint32_t o = (uint32_t)(j < nq ? j : j < nq + nk ? j - nq : j - nq - nk) * kPiece + lane * 16;
+      return o < (j < nq ? q_bytes : k_bytes) ? __ldcs(reinterpret_cast<const uint4*>(base + o)) : make_uint4(0u, 0u, 0u, 0u);
     };
     uint4 x[UN];
+    int j_load = u & (parts - 1), j_now = j_load;
 #pragma unroll
-    for (int k = 0; k < UN; ++k) x[k] = group + k * kGroups < units ? source(group + k * kGroups) : make_uint4(0u, 0u, 0u, 0u);
-    for (int a = tid; a < here * half; a += kThreadsA) {
-      const int r = a / half, i = a - r * half, bb = pick(b, r);
-      const long long pos = (long long)(p.position ? p.position[bb] : p.start ? p.start[bb] : 0) + (p.depth ? p.depth[pick(row, r)] : pick(t, r));
-      const double turns = (double)pos * (p.inv_freq[i] * 0.15915494309189533577);
-      float s, c;
-      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-      cs[r][i] = make_float2(c * p.magnitude, s * p.magnitude);
+    for (int k = 0; k < UN; ++k) {
+      x[k] = j_load < pieces ? load(j_load) : make_uint4(0u, 0u, 0u, 0u);
+      j_load += parts;
     }
-    if (p.k && tid >= kThreadsA - kMaxRows) {
-      const int r = tid - (kThreadsA - kMaxRows);
-      if (r < here) {
-        const int bb = pick(b, r);
-        const long long pos = (long long)(p.start ? p.start[bb] : 0) + pick(t, r);
-        int page = 0, slot = 0;
-        const bool ok = pos >= 0 && pos < max_pos && find_place(p.g, bb, (int)pos, page, slot);
-        if (!ok) report(p.st, CAST_ERR_BAD_PAGE, bb);
-        place_s[r] = ok ? (long long)page * (p.g.page_size == 0 ? p.g.seq_capacity : p.g.page_size) + slot : -1;
+    // the row's place in the cache
+    long long place = -1;
+    const int begin = p.start ? p.start[b] : 0;
+    if (p.k) {
+      const long long pos = (long long)begin + t;
+      int page = 0, slot = 0;
+      const bool ok = pos >= 0 && pos < max_pos && find_place(p.g, b, (int)pos, page, slot);
+      if (ok) place = (long long)page * (p.g.page_size == 0 ? p.g.seq_capacity : p.g.page_size) + slot;
+      else if (lane == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
+    }
+    // its cosines and sines, a pair or two a lane, and what they make of the lane's dims: out = a x + b partner, the weights within
+    float qa[CH], qb[CH], ka[CH], kb[CH];
+    if (half > 0) {
+      const long long pos = (long long)(p.position ? p.position[b] : begin) + (p.depth ? p.depth[row] : t);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < kMaxPairs / 32; ++j) {
+        const double turns = (double)pos * freq[j];
+        float s, c;
+        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+        cs[warp][j * 32 + lane] = make_float2(c * p.magnitude, s * p.magnitude);
       }
+      __syncwarp();
     }
-    __syncthreads();
-    for (int u0 = group; __any_sync(0xffffffffu, u0 < units); u0 += UN * kGroups) {
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+      const int d = d0 + e;
+      const bool turns = d < p.rot_dim, low = MODE == kBeside ? (e & 1) == 0 : d < half;
+      const int o = !turns ? d : MODE == kBeside ? d ^ 1 : low ? d + half : d - half;
+      const float2 a = turns ? cs[warp][MODE == kBeside ? d >> 1 : low ? d : o] : make_float2(1.f, 0.f);
+      const float s = low || !turns ? -a.y : a.y;  // (-0 leaves a zero's sign alone)
+      qa[e] = a.x * w_s[0][d]; qb[e] = s * w_s[0][o];
+      ka[e] = a.x * w_s[1][d]; kb[e] = s * w_s[1][o];
+    }
+
+    auto turn = [&](uint4& y, const float (&a)[CH], const float (&bb)[CH], bool norm) {
+      float f[CH], g[CH];
+      Piece<T>::unpack(y, f);
+      if (MODE == kBeside) {
+#pragma unroll
+        for (int e = 0; e < CH; ++e) g[e] = d0 + e < p.rot_dim ? f[e ^ 1] : 0.f;
+      } else if (MODE == kLanes) {
+        const int from = (d0 < half ? d0 + half : d0 - half) / CH;
+        uint4 z;
+        z.x = __shfl_sync(0xffffffffu, y.x, from, LPH); z.y = __shfl_sync(0xffffffffu, y.y, from, LPH);
+        z.z = __shfl_sync(0xffffffffu, y.z, from, LPH); z.w = __shfl_sync(0xffffffffu, y.w, from, LPH);
+        if (d0 >= p.rot_dim) z = make_uint4(0u, 0u, 0u, 0u);
+        Piece<T>::unpack(z, g);
+      } else {
+        __syncwarp();
+        *reinterpret_cast<uint4*>(turn_s[warp] + lane * 16) = y;
+        __syncwarp();
+        const T* mine = reinterpret_cast<const T*>(turn_s[warp]) + lane / LPH * D;
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+          const int d = d0 + e;
+          g[e] = d < p.rot_dim ? (float)mine[d < half ? d + half : d - half] : 0.f;
+        }
+      }
+      float inv = 1.f;
+      if (norm) {
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < CH; ++e) sq = fmaf(f[e], f[e], sq);
+#pragma unroll
+        for (int o = LPH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        inv = rsqrtf(sq * (1.f / D) + p.eps);
+      }
+#pragma unroll
+      for (int e = 0; e < CH; ++e) f[e] = fmaf(f[e], a[e], g[e] * bb[e]) * inv;
+      y = Piece<T>::pack(f);
+    };
+    const bool q_norm = p.q_weight != nullptr, k_norm = p.k_weight != nullptr;
+    unsigned char* q_to = p.q_out + (size_t)row * q_bytes;
+    const size_t cache_at = (size_t)place * k_bytes;
+    while (j_now < pieces) {
 #pragma unroll
       for (int k = 0; k < UN; ++k) {
-        const int u = u0 + k * kGroups;
-        const bool on = u < units;
-        const int r = on ? u / heads : 0, h = on ? u - r * heads : 0;
-        const bool is_q = h < q_heads, is_v = h >= q_heads + p.Hkv;
+        if (j_now >= pieces) break;
         uint4 y = x[k];
-        if (u + UN * kGroups < units) x[k] = source(u + UN * kGroups);
-        const bool rotate = !is_v && half > 0;
-        const float* w = is_q ? p.q_weight : is_v ? nullptr : p.k_weight;
-        if (__any_sync(0xffffffffu, on && (rotate || w != nullptr))) {
-          float f[CH];
-          Piece<T>::unpack(y, f);
-          float sq = 0.f;
-#pragma unroll
-          for (int e = 0; e < CH; ++e) sq = fmaf(f[e], f[e], sq);
-#pragma unroll
-          for (int o = LPH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-          if (w != nullptr) {
-            const float inv = rsqrtf(sq * (1.f / D) + p.eps);
-#pragma unroll
-            for (int e = 0; e < CH; e += 4) {
-              const float4 w4 = __ldg(reinterpret_cast<const float4*>(w + d0 + e));
-              f[e] *= inv * w4.x; f[e + 1] *= inv * w4.y; f[e + 2] *= inv * w4.z; f[e + 3] *= inv * w4.w;
-            }
-          }
-          if (p.interleaved) {
-            if (rotate && d0 < p.rot_dim) {
-#pragma unroll
-              for (int e = 0; e < CH; e += 2) {
-                if (d0 + e < p.rot_dim) {
-                  const float2 a = cs[r][(d0 + e) >> 1];
-                  const float lo = f[e], hi = f[e + 1];
-                  f[e] = lo * a.x - hi * a.y;
-                  f[e + 1] = hi * a.x + lo * a.y;
-                }
-              }
-            }
-          } else if (half > 0) {
-            // dim e of lane l lies at [e / 4][l][e % 4]: 16-byte stores without bank conflicts
-            float* mine = turn_s[warp] + (lane / LPH) * D;
-#pragma unroll
-            for (int e = 0; e < CH; e += 4)
-              *reinterpret_cast<float4*>(mine + (e / 4) * (LPH * 4) + lig * 4) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-            __syncwarp();
-            if (rotate && d0 < p.rot_dim) {
-#pragma unroll
-              for (int e = 0; e < CH; ++e) {
-                const int d = d0 + e;
-                if (d < p.rot_dim) {
-                  const bool low = d < half;
-                  const int o = low ? d + half : d - half;
-                  const float other = mine[(o % CH / 4) * (LPH * 4) + (o / CH) * 4 + o % 4];
-                  const float2 a = cs[r][low ? d : o];
-                  f[e] = f[e] * a.x + (low ? -other : other) * a.y;
-                }
-              }
-            }
-            __syncwarp();
-          }
-          if (rotate || w != nullptr) y = Piece<T>::pack(f);  // (values stay as they are, bit by bit)
+        if (j_load < pieces) x[k] = load(j_load);
+        j_load += parts;
+        if (j_now < nq) {
+          if (half > 0 || q_norm) turn(y, qa, qb, q_norm);  // (values stay as they are, bit by bit, where neither is asked for)
+          const uint32_t o = (uint32_t)j_now * kPiece + lane * 16;
+          if (o < q_bytes) *reinterpret_cast<uint4*>(q_to + o) = y;
+        } else {
+          const bool is_v = j_now >= nq + nk;
+          if (!is_v && (half > 0 || k_norm)) turn(y, ka, kb, k_norm);
+          const uint32_t o = (uint32_t)(j_now - nq - (is_v ? nk : 0)) * kPiece + lane * 16;
+          if (o < k_bytes && place >= 0) *reinterpret_cast<uint4*>((is_v ? p.v_cache : p.k_cache) + cache_at + o) = y;
         }
-        if (on) {
-          if (is_q) {
-            *reinterpret_cast<uint4*>(p.q_out + ((size_t)pick(row, r) * p.Hq + h) * (D * sizeof(T)) + lig * 16) = y;
-          } else if (place_s[r] >= 0) {
-            unsigned char* cache = is_v ? p.v_cache : p.k_cache;
-            const int kh = h - q_heads - (is_v ? p.Hkv : 0);
-            *reinterpret_cast<uint4*>(cache + ((size_t)place_s[r] * p.Hkv + kh) * (D * sizeof(T)) + lig * 16) = y;
-          }
-        }
+        j_now += parts;
       }
     }
-    __syncthreads();
   }
 }
 
 template <typename T, int D>
 cast_status launch_append(const cast_ctx* c, AppendParams& p, cudaStream_t s) {
+  constexpr int CH = Piece<T>::N, HPW = 32 / (D / CH), kWarps = kThreadsA / 32;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
-  // Four rows per CTA share its start, one keeps a small call's chain short: four from the count on that gives every SM two CTAs.
-  p.rb = rows >= 8ll * c->num_sms ? kMaxRows : 1;
-  const long long want = (rows + p.rb - 1) / p.rb, most = 8ll * c->num_sms;
+  const int pieces = (p.q ? (p.Hq + HPW - 1) / HPW : 0) + (p.k ? 2 * ((p.Hkv + HPW - 1) / HPW) : 0);
+  const long long resident = 2ll * c->num_sms * kWarps;
+  p.parts_log2 = 0;
+  while (p.parts_log2 < 3 && rows << p.parts_log2 < 1 * resident && 2 << p.parts_log2 <= pieces) ++p.parts_log2;
+  const long long want = ((rows << p.parts_log2) + kWarps - 1) / kWarps, most = 2ll * c->num_sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(want < most ? want : most), 1, 1);
   cfg.blockDim = dim3(kThreadsA, 1, 1);
@@ -252,7 +259,11 @@ cast_status launch_append(const cast_ctx* c, AppendParams& p, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, append_kernel<T, D>, p) != cudaSuccess) {
+  const int half = p.rot_dim / 2;
+  const cudaError_t e = p.interleaved     ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kBeside>, p)
+                        : half % CH == 0 ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kLanes>, p)
+                                         : cudaLaunchKernelEx(&cfg, append_kernel<T, D, kAnywhere>, p);
+  if (e != cudaSuccess) {
     cudaGetLastError();
     return CAST_ERR_CUDA;
   }
