@@ -59,12 +59,12 @@ template <> struct Piece<__nv_bfloat16> {
 enum { kBeside, kLanes, kAnywhere };
 
 template <typename T, int D, int MODE>
-__global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int CH = Piece<T>::N, LPH = D / CH, HPW = 32 / LPH;  // dims per lane, lanes per head, heads per piece
-  constexpr int kPiece = 512, UN = 4;                            // bytes a warp takes at a time; pieces in flight
-  constexpr int KB = CAST_MAX_BATCH / 32;
+  constexpr int kPiece = 512, UN = 2;                            // bytes a warp takes at a time; pieces in flight
   __shared__ float2 cs[kThreadsA / 32][kMaxPairs];
   __shared__ float w_s[2][D];
+  __shared__ int before_s[CAST_MAX_BATCH], first_s[CAST_MAX_BATCH], off_s[CAST_MAX_BATCH], live_s;
   __shared__ alignas(16) unsigned char turn_s[MODE == kAnywhere ? kThreadsA / 32 : 1][kPiece];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -84,51 +84,46 @@ __global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_const
     w_s[d / D][d % D] = w ? w[d % D] : 1.f;
   }
 
-  // live rows of the sequences: lane b % 32 holds sequence b's
-  int cnt[KB], first[KB], off[KB], before[KB];
+  // The live rows in front of every sequence, its first token, and where that token's row lies. (In shared memory: held in registers
+  // they took a third of a thread's, and it is warps that hide this kernel's latency.)
+  if (warp == 0) {
+    int live = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+      const int b = b0 + lane;
+      int n = b < p.B ? min(max(p.n_rows[b], 0), p.rows) : 0;
+      const int off = b >= p.B ? 0 : p.row_start ? p.row_start[b] : b * p.rows;
+      int first = b < p.B && p.first_row ? p.first_row[b] : 0;
+      if (p.row_start && (off < 0 || (long long)off + n > all_rows)) {
+        if (n > 0 && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_TREE, b);
+        n = 0;
+      }
+      first = min(max(first, 0), n);
+      n -= first;
+      int x = n;
 #pragma unroll
-  for (int j = 0; j < KB; ++j) {
-    const int b = j * 32 + lane;
-    const bool in = b < p.B;
-    cnt[j] = in ? p.n_rows[b] : 0;
-    first[j] = in && p.first_row ? p.first_row[b] : 0;
-    off[j] = !in ? 0 : p.row_start ? p.row_start[b] : b * p.rows;
-  }
-  int live = 0;
-#pragma unroll
-  for (int j = 0; j < KB; ++j) {
-    int n = min(max(cnt[j], 0), p.rows);
-    if (p.row_start && (off[j] < 0 || (long long)off[j] + n > all_rows)) {
-      if (n > 0 && blockIdx.x == 0 && warp == 0) report(p.st, CAST_ERR_BAD_TREE, j * 32 + lane);
-      n = 0;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      before_s[b] = live + x - n;
+      first_s[b] = first;
+      off_s[b] = off;
+      live += __shfl_sync(0xffffffffu, x, 31);
     }
-    first[j] = min(max(first[j], 0), n);
-    cnt[j] = n - first[j];
-    int x = cnt[j];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    before[j] = live + x - cnt[j];
-    live += __shfl_sync(0xffffffffu, x, 31);
+    if (lane == 0) live_s = live;
   }
-  __syncthreads();  // the weights
+  __syncthreads();
+  const int live = live_s;
 
   const int parts = 1 << p.parts_log2;
   for (int u = (int)blockIdx.x * (kThreadsA / 32) + warp; u >> p.parts_log2 < live; u += (int)gridDim.x * (kThreadsA / 32)) {
     const int i = u >> p.parts_log2;
-    int b = 0, t = 0, row = 0;  // the i-th live row: its sequence, its token, its place among all
-#pragma unroll
-    for (int j = 0; j < KB; ++j) {
-      const unsigned hit = __ballot_sync(0xffffffffu, i >= before[j] && i - before[j] < cnt[j]);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        b = j * 32 + l;
-        t = i - __shfl_sync(0xffffffffu, before[j], l) + __shfl_sync(0xffffffffu, first[j], l);
-        row = __shfl_sync(0xffffffffu, off[j], l) + t;
-      }
+    int b = 0;  // the i-th live row: the last sequence with i rows or fewer in front of it
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+      const unsigned hit = __ballot_sync(0xffffffffu, b0 + lane < p.B && before_s[b0 + lane] <= i);
+      if (hit) b = b0 + 31 - __clz(hit);
     }
+    const int t = i - before_s[b] + first_s[b], row = off_s[b] + t;
     // A piece is 512 bytes of one tensor's row, sixteen a lane.
     const unsigned char *q_row = p.q + (size_t)row * p.q_stride, *k_row = p.k + (size_t)row * p.k_stride, *v_row = p.v + (size_t)row * p.v_stride;
     auto load = [&](int j) {
@@ -153,8 +148,7 @@ __global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_const
       if (ok) place = (long long)page * (p.g.page_size == 0 ? p.g.seq_capacity : p.g.page_size) + slot;
       else if (lane == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
     }
-    // its cosines and sines, a pair or two a lane, and what they make of the lane's dims: out = a x + b partner, the weights within
-    float qa[CH], qb[CH], ka[CH], kb[CH];
+    // its cosines and sines, a pair or two a lane
     if (half > 0) {
       const long long pos = (long long)(p.position ? p.position[b] : begin) + (p.depth ? p.depth[row] : t);
       __syncwarp();
@@ -167,18 +161,28 @@ __global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_const
       }
       __syncwarp();
     }
+    // and what they make of the lane's dims, the weights within: out = a x + b partner. A warp's pieces lie in order, so queries'
+    // give way to keys' once.
+    float ca[CH], cb[CH];
+    bool norm = false, changes = false;
+    int sec = -1;
+    auto section = [&](int now) {
+      sec = now;
+      norm = now == 0 ? p.q_weight != nullptr : now == 1 && p.k_weight != nullptr;
+      changes = norm || (now < 2 && half > 0);
+      if (!changes) return;
 #pragma unroll
-    for (int e = 0; e < CH; ++e) {
-      const int d = d0 + e;
-      const bool turns = d < p.rot_dim, low = MODE == kBeside ? (e & 1) == 0 : d < half;
-      const int o = !turns ? d : MODE == kBeside ? d ^ 1 : low ? d + half : d - half;
-      const float2 a = turns ? cs[warp][MODE == kBeside ? d >> 1 : low ? d : o] : make_float2(1.f, 0.f);
-      const float s = low || !turns ? -a.y : a.y;  // (-0 leaves a zero's sign alone)
-      qa[e] = a.x * w_s[0][d]; qb[e] = s * w_s[0][o];
-      ka[e] = a.x * w_s[1][d]; kb[e] = s * w_s[1][o];
-    }
+      for (int e = 0; e < CH; ++e) {
+        const int d = d0 + e;
+        const bool turns = d < p.rot_dim, low = MODE == kBeside ? (e & 1) == 0 : d < half;
+        const int o = !turns ? d : MODE == kBeside ? d ^ 1 : low ? d + half : d - half;
+        const float2 a = turns ? cs[warp][MODE == kBeside ? d >> 1 : low ? d : o] : make_float2(1.f, 0.f);
+        ca[e] = a.x * w_s[now][d];
+        cb[e] = (low || !turns ? -a.y : a.y) * w_s[now][o];  // (-0 leaves a zero's sign alone)
+      }
+    };
 
-    auto turn = [&](uint4& y, const float (&a)[CH], const float (&bb)[CH], bool norm) {
+    auto turn = [&](uint4& y) {
       float f[CH], g[CH];
       Piece<T>::unpack(y, f);
       if (MODE == kBeside) {
@@ -212,12 +216,9 @@ __global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_const
         inv = rsqrtf(sq * (1.f / D) + p.eps);
       }
 #pragma unroll
-      for (int e = 0; e < CH; ++e) f[e] = fmaf(f[e], a[e], g[e] * bb[e]) * inv;
+      for (int e = 0; e < CH; ++e) f[e] = fmaf(f[e], ca[e], g[e] * cb[e]) * inv;
       y = Piece<T>::pack(f);
     };
-    const bool q_norm = p.q_weight != nullptr, k_norm = p.k_weight != nullptr;
-    unsigned char* q_to = p.q_out + (size_t)row * q_bytes;
-    const size_t cache_at = (size_t)place * k_bytes;
     while (j_now < pieces) {
 #pragma unroll
       for (int k = 0; k < UN; ++k) {
@@ -225,16 +226,12 @@ __global__ void __launch_bounds__(kThreadsA, 2) append_kernel(const __grid_const
         uint4 y = x[k];
         if (j_load < pieces) x[k] = load(j_load);
         j_load += parts;
-        if (j_now < nq) {
-          if (half > 0 || q_norm) turn(y, qa, qb, q_norm);  // (values stay as they are, bit by bit, where neither is asked for)
-          const uint32_t o = (uint32_t)j_now * kPiece + lane * 16;
-          if (o < q_bytes) *reinterpret_cast<uint4*>(q_to + o) = y;
-        } else {
-          const bool is_v = j_now >= nq + nk;
-          if (!is_v && (half > 0 || k_norm)) turn(y, ka, kb, k_norm);
-          const uint32_t o = (uint32_t)(j_now - nq - (is_v ? nk : 0)) * kPiece + lane * 16;
-          if (o < k_bytes && place >= 0) *reinterpret_cast<uint4*>((is_v ? p.v_cache : p.k_cache) + cache_at + o) = y;
-        }
+        const int now = (j_now >= nq) + (j_now >= nq + nk);
+        if (now != sec) section(now);
+        if (changes) turn(y);  // (else the values stay as they are, bit by bit)
+        const uint32_t o = (uint32_t)(j_now - (now > 0 ? nq : 0) - (now > 1 ? nk : 0)) * kPiece + lane * 16;
+        unsigned char* to = now == 0 ? p.q_out + (size_t)row * q_bytes : (now == 1 ? p.k_cache : p.v_cache) + (size_t)place * k_bytes;
+        if (now == 0 ? o < q_bytes : place >= 0 && o < k_bytes) *reinterpret_cast<uint4*>(to + o) = y;
         j_now += parts;
       }
     }
@@ -246,10 +243,10 @@ cast_status launch_append(const cast_ctx* c, AppendParams& p, cudaStream_t s) {
   constexpr int CH = Piece<T>::N, HPW = 32 / (D / CH), kWarps = kThreadsA / 32;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   const int pieces = (p.q ? (p.Hq + HPW - 1) / HPW : 0) + (p.k ? 2 * ((p.Hkv + HPW - 1) / HPW) : 0);
-  const long long resident = 2ll * c->num_sms * kWarps;
+  const long long resident = 3ll * c->num_sms * kWarps;
   p.parts_log2 = 0;
   while (p.parts_log2 < 3 && rows << p.parts_log2 < 1 * resident && 2 << p.parts_log2 <= pieces) ++p.parts_log2;
-  const long long want = ((rows << p.parts_log2) + kWarps - 1) / kWarps, most = 2ll * c->num_sms;
+  const long long want = ((rows << p.parts_log2) + kWarps - 1) / kWarps, most = 3ll * c->num_sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(want < most ? want : most), 1, 1);
   cfg.blockDim = dim3(kThreadsA, 1, 1);
