@@ -5,10 +5,16 @@
 // (a, b) -> magnitude (a cos - b sin, b cos + a sin) with the angle position * inv_freq[i]; rounded once, on the way out. The angle is
 // formed in turns and in fp64 and only its fraction becomes fp32: in fp32 a position of 100 000 leaves 0.006 of a radian.
 //
-// One pass: a row is read once and written once. A CTA takes one or four rows; its threads form the rows' cosines and sines once for all
-// heads (shared memory), then every group of D * sizeof / 16 lanes takes a head at a time, 16 bytes a lane, eight heads in flight per
-// warp of bf16 rows of 128 dims. The partner of a dim (half a rotation away in the halves layout) comes through shared memory, so any even number of rotating
-// dims goes one way. The live rows are enumerated on the device: sequences without rows cost nothing.
+// One pass: a row is read once and written once, so memory bounds a long call: 10 400 rows of 32/8 heads of 128 dims in bf16 (255 MB in
+// and out) take 53 us, 5.2 TB/s, 79 % of a copy's rate. What comes next is instructions, 74 % of the issue slots; hence:
+// - A warp takes a row, or a part of one where rows are few, 512 bytes of one tensor at a time. It needs no other warp.
+// - Loads run ahead by cp.async into a ring of the warp's own, over the ends of rows, so that the loop need not be unrolled over
+//   registers in flight (with it: 61 us, and more registers in flight were slower, at 65 to 86, for they cost warps).
+// - A lane has two chunks of eight bytes, half a rotation apart in the halves layout, so that a dim meets its partner in the lane; cosine, sine
+//   and weight become one factor each for a dim and its partner, in registers, once per row and tensor (formed per head: 124 us; with
+//   the head and row found by division: 149). A rotation that is no whole number of chunks reads the partner from the ring.
+// A small call is a chain of two reads of memory behind its launch: 7 us.
+// The live rows are enumerated on the device: sequences without rows cost nothing.
 #include "kv_q4.h"
 
 using namespace cast;
@@ -32,46 +38,62 @@ struct AppendParams {
   DevState* st;
 };
 
-// Sixteen bytes of a row as fp32 and back (rounded to nearest even).
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& a, float (&x)[4]) { Vec<float>::unpack(a, x); }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  }
+// Two fp32 in a register pair, for the packed forms of multiply and fused multiply-add.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 z, x, y, z; mov.b64 {%0, %1}, z;}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
+// Eight bytes of a row as pairs of fp32 and back (rounded to nearest even).
+template <typename T> struct Chunk;
+template <> struct Chunk<float> {
+  static constexpr int N = 1;  // pairs
+  static __device__ __forceinline__ void unpack(const uint2& a, float2* x) { x[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y)); }
+  static __device__ __forceinline__ uint2 pack(const float2* x) { return make_uint2(__float_as_uint(x[0].x), __float_as_uint(x[0].y)); }
 };
-template <> struct Piece<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& a, float (&x)[8]) { Vec<__nv_bfloat16>::unpack(a, x); }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+template <> struct Chunk<__nv_bfloat16> {
+  static constexpr int N = 2;
+  static __device__ __forceinline__ void unpack(const uint2& a, float2* x) {
+    x[0] = make_float2(__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u));
+    x[1] = make_float2(__uint_as_float(a.y << 16), __uint_as_float(a.y & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint2 pack(const float2* x) {
+    const __nv_bfloat162 a = __float22bfloat162_rn(x[0]), b = __float22bfloat162_rn(x[1]);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
   }
 };
 
-// Where a rotating dim's partner lies: beside it; half a rotation away and that is a whole number of lanes; half a rotation away anywhere.
-enum { kBeside, kLanes, kAnywhere };
+// Where a rotating dim's partner lies: in the same pair of the lane's first or second chunk; at the same place of its other chunk; anywhere.
+enum { kBeside, kAcross, kAnywhere };
 
 template <typename T, int D, int MODE>
-__global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_constant__ AppendParams p) {
-  constexpr int CH = Piece<T>::N, LPH = D / CH, HPW = 32 / LPH;  // dims per lane, lanes per head, heads per piece
-  constexpr int kPiece = 512, UN = 2;                            // bytes a warp takes at a time; pieces in flight
+__global__ void __launch_bounds__(kThreadsA, MODE == kAnywhere ? 2 : 3) append_kernel(const __grid_constant__ AppendParams p) {
+  constexpr int N = Chunk<T>::N, C = 2 * N;          // pairs and dims of a chunk of eight bytes; a lane has two
+  constexpr int LPH = D / (2 * C), HPW = 32 / LPH;   // lanes per head, heads per piece
+  constexpr int kPiece = 512, UN = 4;                // bytes a warp takes at a time; pieces in its ring
   __shared__ float2 cs[kThreadsA / 32][kMaxPairs];
   __shared__ float w_s[2][D];
   __shared__ int before_s[CAST_MAX_BATCH], first_s[CAST_MAX_BATCH], off_s[CAST_MAX_BATCH], live_s;
-  __shared__ alignas(16) unsigned char turn_s[MODE == kAnywhere ? kThreadsA / 32 : 1][kPiece];
+  __shared__ int start_s[CAST_MAX_BATCH], position_s[CAST_MAX_BATCH];
+  __shared__ alignas(16) unsigned char in_s[kThreadsA / 32][UN][kPiece];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int d0 = lane % LPH * CH, half = p.rot_dim / 2;            // first dim of the lane
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lig = lane % LPH;
+  const int half = p.rot_dim / 2;
+  // The lane's chunks. Where halves rotate, the lanes of the rotating dims take a chunk of each half, so that partners meet in a lane.
+  const bool across = MODE == kAcross && lig * 2 * C < p.rot_dim;
+  const int d0 = across ? lig * C : lig * 2 * C, d1 = across ? half + lig * C : d0 + C;
+  const bool rotates = MODE != kAnywhere && half > 0 && lig * 2 * C < p.rot_dim;
+  auto dim = [&](int e) { return e < C ? d0 + e : d1 + e - C; };
   const int nq = p.q ? (p.Hq + HPW - 1) / HPW : 0, nk = p.k ? (p.Hkv + HPW - 1) / HPW : 0, pieces = nq + 2 * nk;
   const uint32_t q_bytes = (uint32_t)p.Hq * (uint32_t)(D * sizeof(T)), k_bytes = (uint32_t)p.Hkv * (uint32_t)(D * sizeof(T));
+  const uint32_t at0 = (uint32_t)((lane / LPH * D + d0) * sizeof(T)), gap = (uint32_t)((d1 - d0) * sizeof(T));
   const long long all_rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   const long long max_pos = p.g.max_pos();
 
@@ -84,8 +106,12 @@ __global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_const
     w_s[d / D][d % D] = w ? w[d % D] : 1.f;
   }
 
-  // The live rows in front of every sequence, its first token, and where that token's row lies. (In shared memory: held in registers
-  // they took a third of a thread's, and it is warps that hide this kernel's latency.)
+  // The live rows in front of every sequence, its first token, and where that token's row lies. (In shared memory: registers are
+  // better spent on warps, which hide this kernel's latency.)
+  for (int b = tid; b < p.B; b += kThreadsA) {
+    start_s[b] = p.start ? p.start[b] : 0;
+    if (p.position) position_s[b] = p.position[b];
+  }
   if (warp == 0) {
     int live = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
@@ -115,32 +141,68 @@ __global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_const
   __syncthreads();
   const int live = live_s;
 
-  const int parts = 1 << p.parts_log2;
-  for (int u = (int)blockIdx.x * (kThreadsA / 32) + warp; u >> p.parts_log2 < live; u += (int)gridDim.x * (kThreadsA / 32)) {
-    const int i = u >> p.parts_log2;
-    int b = 0;  // the i-th live row: the last sequence with i rows or fewer in front of it
+  auto find = [&](int i) {  // the sequence of the i-th live row: the last one with i rows or fewer in front of it
+    int b = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
       const unsigned hit = __ballot_sync(0xffffffffu, b0 + lane < p.B && before_s[b0 + lane] <= i);
       if (hit) b = b0 + 31 - __clz(hit);
     }
-    const int t = i - before_s[b] + first_s[b], row = off_s[b] + t;
-    // A piece is 512 bytes of one tensor's row, sixteen a lane.
-    const unsigned char *q_row = p.q + (size_t)row * p.q_stride, *k_row = p.k + (size_t)row * p.k_stride, *v_row = p.v + (size_t)row * p.v_stride;
-    auto load = [&](int j) {
-      const unsigned char* base = j < nq ? q_row : j < nq + nk ? k_row : v_row;
-      const uint32_t o = (uint32_t)(j < nq ? j : j < nq + nk ? j - nq : j - nq - nk) * kPiece + lane * 16;
-      return o < (j < nq ? q_bytes : k_bytes) ? __ldcs(reinterpret_cast<const uint4*>(base + o)) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    uint4 x[UN];
-    int j_load = u & (parts - 1), j_now = j_load;
-#pragma unroll
-    for (int k = 0; k < UN; ++k) {
-      x[k] = j_load < pieces ? load(j_load) : make_uint4(0u, 0u, 0u, 0u);
-      j_load += parts;
+    return b;
+  };
+  // A piece is 512 bytes of one tensor's row: the rows of q, k and v in that order, a warp's pieces `parts` apart. A cursor walks them:
+  // `end` is where its tensor ends, `lim` where the lane's share of it does (the last piece may be a part).
+  const int parts = 1 << p.parts_log2, units = (int)gridDim.x * (kThreadsA / 32);
+  const int u0 = (int)blockIdx.x * (kThreadsA / 32) + warp, part = warp & (parts - 1);
+  const uint32_t stride = (uint32_t)kPiece << p.parts_log2;
+  struct Cursor {
+    int j, end, lim;
+    uint32_t at;
+  };
+  auto seat = [&](Cursor& c, uint32_t at) {
+    const int sec = (c.j >= nq) + (c.j >= nq + nk), from = sec == 0 ? 0 : sec == 1 ? nq : nq + nk;
+    const uint32_t bytes = sec == 0 ? q_bytes : k_bytes;
+    c.end = sec == 0 ? nq : sec == 1 ? nq + nk : pieces;
+    c.at = (uint32_t)(c.j - from) * kPiece + at;
+    c.lim = c.j >= pieces ? 0 : c.end - ((uint32_t)(c.end - 1 - from) * kPiece + at < bytes ? 0 : 1);
+    return sec;
+  };
+  // Loads run UN - 1 pieces ahead, over the ends of rows, into shared memory: a warp's own ring.
+  int u_load = u0, row_load = -1;
+  Cursor in = {0, 0, 0, 0u};
+  const unsigned char* from = nullptr;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&in_s[warp][0][lane * 16]);
+  uint32_t slot_load = 0, slot = 0;
+  auto load = [&]() {
+    if (in.j >= in.end && u_load >> p.parts_log2 < live) {
+      if (row_load < 0) {
+        const int i = u_load >> p.parts_log2, b = find(i);
+        row_load = off_s[b] + first_s[b] + i - before_s[b];
+        in.j = part;
+      }
+      const int sec = seat(in, lane * 16);
+      from = sec == 0 ? p.q + (size_t)row_load * p.q_stride : sec == 1 ? p.k + (size_t)row_load * p.k_stride : p.v + (size_t)row_load * p.v_stride;
+      from += in.at;
     }
+    if (in.j < in.lim) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot_load), "l"(from) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    slot_load = (slot_load + kPiece) % (UN * kPiece);
+    in.j += parts;
+    from += stride;
+    if (in.j >= pieces) {
+      in.end = 0;
+      in.lim = 0;
+      u_load += row_load >= 0 ? units : 0;
+      row_load = -1;
+    }
+  };
+#pragma unroll 1
+  for (int k = 0; k < UN - 1; ++k) load();
+  for (int u = u0; u >> p.parts_log2 < live; u += units) {
+    const int i = u >> p.parts_log2, b = find(i), t = i - before_s[b] + first_s[b], row = off_s[b] + t;
+    Cursor out = {part, 0, 0, 0u};
     // the row's place in the cache
     long long place = -1;
-    const int begin = p.start ? p.start[b] : 0;
+    const int begin = start_s[b];
     if (p.k) {
       const long long pos = (long long)begin + t;
       int page = 0, slot = 0;
@@ -150,7 +212,7 @@ __global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_const
     }
     // its cosines and sines, a pair or two a lane
     if (half > 0) {
-      const long long pos = (long long)(p.position ? p.position[b] : begin) + (p.depth ? p.depth[row] : t);
+      const long long pos = (long long)(p.position ? position_s[b] : begin) + (p.depth ? p.depth[row] : t);
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kMaxPairs / 32; ++j) {
@@ -163,90 +225,106 @@ __global__ void __launch_bounds__(kThreadsA, 3) append_kernel(const __grid_const
     }
     // and what they make of the lane's dims, the weights within: out = a x + b partner. A warp's pieces lie in order, so queries'
     // give way to keys' once.
-    float ca[CH], cb[CH];
+    float2 ca[C], cb[C];
     bool norm = false, changes = false;
-    int sec = -1;
-    auto section = [&](int now) {
-      sec = now;
-      norm = now == 0 ? p.q_weight != nullptr : now == 1 && p.k_weight != nullptr;
-      changes = norm || (now < 2 && half > 0);
+    unsigned char* to = nullptr;
+    auto enter = [&]() {
+      const int sec = seat(out, at0);
+      to = sec == 0 ? p.q_out + (size_t)row * q_bytes : (sec == 1 ? p.k_cache : p.v_cache) + (size_t)place * k_bytes;
+      to += out.at;
+      if (sec > 0 && place < 0) out.lim = 0;
+      norm = sec == 0 ? p.q_weight != nullptr : sec == 1 && p.k_weight != nullptr;
+      changes = norm || (sec < 2 && half > 0);
       if (!changes) return;
+      const float* w = w_s[sec];
 #pragma unroll
-      for (int e = 0; e < CH; ++e) {
-        const int d = d0 + e;
-        const bool turns = d < p.rot_dim, low = MODE == kBeside ? (e & 1) == 0 : d < half;
-        const int o = !turns ? d : MODE == kBeside ? d ^ 1 : low ? d + half : d - half;
-        const float2 a = turns ? cs[warp][MODE == kBeside ? d >> 1 : low ? d : o] : make_float2(1.f, 0.f);
-        ca[e] = a.x * w_s[now][d];
-        cb[e] = (low || !turns ? -a.y : a.y) * w_s[now][o];  // (-0 leaves a zero's sign alone)
-      }
-    };
-
-    auto turn = [&](uint4& y) {
-      float f[CH], g[CH];
-      Piece<T>::unpack(y, f);
-      if (MODE == kBeside) {
-#pragma unroll
-        for (int e = 0; e < CH; ++e) g[e] = d0 + e < p.rot_dim ? f[e ^ 1] : 0.f;
-      } else if (MODE == kLanes) {
-        const int from = (d0 < half ? d0 + half : d0 - half) / CH;
-        uint4 z;
-        z.x = __shfl_sync(0xffffffffu, y.x, from, LPH); z.y = __shfl_sync(0xffffffffu, y.y, from, LPH);
-        z.z = __shfl_sync(0xffffffffu, y.z, from, LPH); z.w = __shfl_sync(0xffffffffu, y.w, from, LPH);
-        if (d0 >= p.rot_dim) z = make_uint4(0u, 0u, 0u, 0u);
-        Piece<T>::unpack(z, g);
-      } else {
-        __syncwarp();
-        *reinterpret_cast<uint4*>(turn_s[warp] + lane * 16) = y;
-        __syncwarp();
-        const T* mine = reinterpret_cast<const T*>(turn_s[warp]) + lane / LPH * D;
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          const int d = d0 + e;
-          g[e] = d < p.rot_dim ? (float)mine[d < half ? d + half : d - half] : 0.f;
+      for (int e = 0; e < 2 * C; ++e) {
+        const int d = dim(e);
+        const bool turns = d < p.rot_dim, low = p.interleaved ? (e & 1) == 0 : d < half;
+        const int o = !turns ? d : p.interleaved ? d ^ 1 : low ? d + half : d - half;
+        const float2 a = turns ? cs[warp][p.interleaved ? d >> 1 : low ? d : o] : make_float2(1.f, 0.f);
+        const float x = a.x * w[d], y = (low || !turns ? -a.y : a.y) * w[o];  // (-0 leaves a zero's sign alone)
+        if (e & 1) {
+          ca[e / 2].y = x; cb[e / 2].y = y;
+        } else {
+          ca[e / 2].x = x; cb[e / 2].x = y;
         }
       }
-      float inv = 1.f;
-      if (norm) {
-        float sq = 0.f;
-#pragma unroll
-        for (int e = 0; e < CH; ++e) sq = fmaf(f[e], f[e], sq);
-#pragma unroll
-        for (int o = LPH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        inv = rsqrtf(sq * (1.f / D) + p.eps);
-      }
-#pragma unroll
-      for (int e = 0; e < CH; ++e) f[e] = fmaf(f[e], ca[e], g[e] * cb[e]) * inv;
-      y = Piece<T>::pack(f);
     };
-    while (j_now < pieces) {
+#pragma unroll 1
+    while (out.j < pieces) {
+      load();
+      asm volatile("cp.async.wait_group %0;" ::"n"(UN - 1) : "memory");
+      __syncwarp();
+      const unsigned char* piece = in_s[warp][0] + slot + lane / LPH * (D * sizeof(T));
+      uint2 y[2] = {*reinterpret_cast<const uint2*>(piece + d0 * sizeof(T)), *reinterpret_cast<const uint2*>(piece + d1 * sizeof(T))};
+      if (out.j >= out.end) enter();
+      if (changes) {  // (else the values stay as they are, bit by bit)
+        float2 f[C], g[C];
+        Chunk<T>::unpack(y[0], f);
+        Chunk<T>::unpack(y[1], f + N);
+        if (MODE == kAnywhere) {
+          const T* head = reinterpret_cast<const T*>(piece);
 #pragma unroll
-      for (int k = 0; k < UN; ++k) {
-        if (j_now >= pieces) break;
-        uint4 y = x[k];
-        if (j_load < pieces) x[k] = load(j_load);
-        j_load += parts;
-        const int now = (j_now >= nq) + (j_now >= nq + nk);
-        if (now != sec) section(now);
-        if (changes) turn(y);  // (else the values stay as they are, bit by bit)
-        const uint32_t o = (uint32_t)(j_now - (now > 0 ? nq : 0) - (now > 1 ? nk : 0)) * kPiece + lane * 16;
-        unsigned char* to = now == 0 ? p.q_out + (size_t)row * q_bytes : (now == 1 ? p.k_cache : p.v_cache) + (size_t)place * k_bytes;
-        if (now == 0 ? o < q_bytes : place >= 0 && o < k_bytes) *reinterpret_cast<uint4*>(to + o) = y;
-        j_now += parts;
+          for (int e = 0; e < 2 * C; ++e) {
+            const int d = d0 + e;
+            const float o = d < p.rot_dim ? (float)head[p.interleaved ? d ^ 1 : d < half ? d + half : d - half] : 0.f;
+            if (e & 1) g[e / 2].y = o; else g[e / 2].x = o;
+          }
+        }
+        float inv = 1.f;
+        if (norm) {
+          float2 sq = mul2(f[0], f[0]);
+#pragma unroll
+          for (int e = 1; e < C; ++e) sq = fma2(f[e], f[e], sq);
+          float sum = sq.x + sq.y;
+#pragma unroll
+          for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          inv = rsqrtf(sum * (1.f / D) + p.eps);
+        }
+#pragma unroll
+        for (int e = 0; e < C; ++e) {
+          if (MODE == kBeside) g[e] = make_float2(f[e].y, f[e].x);
+          if (MODE == kAcross) g[e] = f[e < N ? e + N : e - N];
+        }
+        if (MODE == kAnywhere || rotates) {
+#pragma unroll
+          for (int e = 0; e < C; ++e) f[e] = fma2(f[e], ca[e], mul2(g[e], cb[e]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < C; ++e) f[e] = mul2(f[e], ca[e]);
+        }
+        if (norm) {
+#pragma unroll
+          for (int e = 0; e < C; ++e) f[e] = mul2(f[e], make_float2(inv, inv));
+        }
+        y[0] = Chunk<T>::pack(f);
+        y[1] = Chunk<T>::pack(f + N);
       }
+      if (out.j < out.lim) {
+        *reinterpret_cast<uint2*>(to) = y[0];
+        *reinterpret_cast<uint2*>(to + gap) = y[1];
+      }
+      out.j += parts;
+      to += stride;
+      slot = (slot + kPiece) % (UN * kPiece);
+      __syncwarp();  // (the next load takes this slot)
     }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename T, int D>
 cast_status launch_append(const cast_ctx* c, AppendParams& p, cudaStream_t s) {
-  constexpr int CH = Piece<T>::N, HPW = 32 / (D / CH), kWarps = kThreadsA / 32;
+  constexpr int C = 2 * Chunk<T>::N, HPW = 32 / (D / (2 * C)), kWarps = kThreadsA / 32;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   const int pieces = (p.q ? (p.Hq + HPW - 1) / HPW : 0) + (p.k ? 2 * ((p.Hkv + HPW - 1) / HPW) : 0);
-  const long long resident = 3ll * c->num_sms * kWarps;
+  // Warps per row: as many as the device has places for (a warp's pieces are a chain, 0.3 us each: 64 rows of 32/8 heads take 9.2 us
+  // with two warps a row, 8.2 with four, 7.2 with eight), one from there on (each forms the row's angles for itself).
+  const long long most = 3ll * c->num_sms;  // CTAs
   p.parts_log2 = 0;
-  while (p.parts_log2 < 3 && rows << p.parts_log2 < 1 * resident && 2 << p.parts_log2 <= pieces) ++p.parts_log2;
-  const long long want = ((rows << p.parts_log2) + kWarps - 1) / kWarps, most = 3ll * c->num_sms;
+  while (1 << p.parts_log2 < kWarps && rows << p.parts_log2 < most * kWarps && 2 << p.parts_log2 <= pieces) ++p.parts_log2;
+  const long long want = ((rows << p.parts_log2) + kWarps - 1) / kWarps;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(want < most ? want : most), 1, 1);
   cfg.blockDim = dim3(kThreadsA, 1, 1);
@@ -256,10 +334,10 @@ cast_status launch_append(const cast_ctx* c, AppendParams& p, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const int half = p.rot_dim / 2;
-  const cudaError_t e = p.interleaved     ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kBeside>, p)
-                        : half % CH == 0 ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kLanes>, p)
-                                         : cudaLaunchKernelEx(&cfg, append_kernel<T, D, kAnywhere>, p);
+  // (a lane's rotating dims have their partners in the lane: chunks of eight bytes are whole)
+  const cudaError_t e = p.rot_dim % (2 * C) != 0 ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kAnywhere>, p)
+                        : p.interleaved          ? cudaLaunchKernelEx(&cfg, append_kernel<T, D, kBeside>, p)
+                                                 : cudaLaunchKernelEx(&cfg, append_kernel<T, D, kAcross>, p);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return CAST_ERR_CUDA;
