@@ -219,16 +219,31 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* dst, float a, float b,
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
-// An item's partials of one lane, joined in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others) by `threads` threads: many rows 128 threads to a
-// part of the columns, two contributors of eight times four columns in flight; few rows four columns a thread, with eight contributors in flight.
+// Rows on their way out, in Q's place: 16 bytes of row r, swizzled, so that the threads of a row and then rows in one piece pass without conflicts.
 template <int HD>
-__device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out0, int t, int threads, int rows, int c_lo, int c_hi, int lane_of) {
+__device__ __forceinline__ uint4* staged(unsigned char* stage, int r, int chunk) {
+  return reinterpret_cast<uint4*>(stage + r * (HD * 2) + ((chunk ^ (r & (HD / 8 - 1))) << 4));
+}
+template <int HD>
+__device__ __forceinline__ void stage_row8(unsigned char* stage, int r, int chunk, float4 a, float4 b) {
+  uint2 u[2];
+  store_row4(reinterpret_cast<__nv_bfloat16*>(&u[0]), a.x, a.y, a.z, a.w);
+  store_row4(reinterpret_cast<__nv_bfloat16*>(&u[1]), b.x, b.y, b.z, b.w);
+  *staged<HD>(stage, r, chunk) = make_uint4(u[0].x, u[0].y, u[1].x, u[1].y);
+}
+
+// An item's partials of one lane, joined in CTA order (contributors c_lo..c_hi; place 1 of the first, 0 of the others) by `threads` threads: many rows 128 threads to a
+// part of the columns, two contributors of eight times four columns in flight, into `stage` (the layout in which rows leave the CTA: straight to their places, eight bytes of
+// 32 rows at a time, cost 4 us); few rows four columns a thread, with eight contributors in flight, straight to their places.
+constexpr int kFewRows = 16;
+template <int HD>
+__device__ __noinline__ void merge_rows(const ChunkParams& p, unsigned char* stage, __nv_bfloat16* out0, int t, int threads, int rows, int c_lo, int c_hi, int lane_of) {
   constexpr int C4 = HD / 4;
   const float4* part = reinterpret_cast<const float4*>(p.part_o);
   auto block = [&](int c) { return part_block(c, c == c_lo, lane_of); };
   auto pair_of = [&](int c, int row) { return __ldcg(p.part_ml + block(c) * kRows + row); };
   auto out_of = [&](int row) { return out0 + ((size_t)(row / p.G) * p.Hq + row % p.G) * HD; };
-  if (rows > 16) {
+  if (rows > kFewRows) {
     const int r = t & (kRows - 1), cols = C4 * kRows / threads, col0 = t / kRows * cols;
     if (r >= rows) return;
     float top = -INFINITY, l = 0.f;
@@ -245,7 +260,6 @@ __device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out
         if (ml[k].x > -INFINITY) l = fmaf(exp2f(ml[k].x - top), ml[k].y, l);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    __nv_bfloat16* dst = out_of(r);
 #pragma unroll 1
     for (int k = col0; k < col0 + cols; k += 8) {
       float4 acc[8];
@@ -276,7 +290,9 @@ __device__ __noinline__ void merge_rows(const ChunkParams& p, __nv_bfloat16* out
         }
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) store_row4(dst + (k + e) * 4, acc[e].x * inv, acc[e].y * inv, acc[e].z * inv, acc[e].w * inv);
+      for (int e = 0; e < 8; e += 2)
+        stage_row8<HD>(stage, r, (k + e) / 2, make_float4(acc[e].x * inv, acc[e].y * inv, acc[e].z * inv, acc[e].w * inv),
+                       make_float4(acc[e + 1].x * inv, acc[e + 1].y * inv, acc[e + 1].z * inv, acc[e + 1].w * inv));
     }
     return;
   }
@@ -962,7 +978,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       const int lane_of = pair ? h : 0;
       const size_t mine_at = part_block(blockIdx.x, (int)blockIdx.x == c_lo, lane_of);
       float4* const part = reinterpret_cast<float4*>(p.part_o) + mine_at * (HD / 4) * kRows + r;
-      // Q is done with: its place takes the rows on their way out (chunks of 16 bytes, swizzled, so that the threads of a row and then rows in one piece pass without conflicts)
+      // Q is done with: its place takes the rows on their way out
       const int slot = (pair ? qc + h : qc) & 1;
       unsigned char* const stage_rows = smem + M::kAtQ + slot * M::kQ;
       constexpr int CH = HD / 8;
@@ -982,15 +998,8 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           }
           if (whole) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t u[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const __nv_bfloat162 b2 = __floats2bfloat162_rn(x[e + 2 * k], x[e + 2 * k + 1]);
-                u[k] = *reinterpret_cast<const uint32_t*>(&b2);
-              }
-              *reinterpret_cast<uint4*>(stage_rows + r * (HD * 2) + ((((c + e) / 8) ^ (r & (CH - 1))) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
-            }
+            for (int e = 0; e < 32; e += 8)
+              stage_row8<HD>(stage_rows, r, (c + e) / 8, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]), make_float4(x[e + 4], x[e + 5], x[e + 6], x[e + 7]));
           } else if (row_ok) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) __stcg(part + (size_t)((c + e) / 4) * kRows, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
@@ -1002,32 +1011,41 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       if (pair) sync_lane();
       else sync_both();
       tc_fence_after();
-      if (whole) {
+      auto sync_rows = [&] {
+        if (pair) sync_lane();
+        else sync_both();
+      };
+      bool staged_all = whole;
+      if (!whole) {
+        if ((pair || h == 0) && r == 0) {
+          // releases this CTA's partial (the barrier made it this thread's to release), acquires those that came earlier
+          int32_t* ticket = p.ticket + 2 * c_lo + lane_of;
+          int t;
+          asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(t) : "l"(ticket) : "memory");
+          ms.last[h] = t == c_hi - c_lo;
+          if (t == c_hi - c_lo) *ticket = 0;  // ready for the next launch
+        }
+        sync_rows();
+        if (ms.last[lane_of]) {  // (both lanes join the partials of a single block)
+          merge_rows<HD>(p, stage_rows, out0, pair ? r : tid, pair ? kRows : 2 * kRows, lane_rows, c_lo, c_hi, lane_of);
+          staged_all = lane_rows > kFewRows;
+          if (staged_all) sync_rows();
+        }
+      }
+      if (staged_all) {
         const int at = pair ? r : tid, by = pair ? kRows : 2 * kRows;
         for (int e = at; e < lane_rows * CH; e += by) {
           const int rr = e / CH, c = e % CH, tk = rr / p.G;
-          const uint4 x = *reinterpret_cast<const uint4*>(stage_rows + rr * (HD * 2) + ((c ^ (rr & (CH - 1))) << 4));
-          *reinterpret_cast<uint4*>(out0 + ((size_t)tk * p.Hq + rr - tk * p.G) * HD + c * 8) = x;
+          *reinterpret_cast<uint4*>(out0 + ((size_t)tk * p.Hq + rr - tk * p.G) * HD + c * 8) = *staged<HD>(stage_rows, rr, c);
         }
         fence_proxy_async();  // (the next copy of Q into this place goes by the async proxy)
         sync_lane();
-      } else if ((pair || h == 0) && r == 0) {
-        // releases this CTA's partial (the barrier made it this thread's to release), acquires those that came earlier
-        int32_t* ticket = p.ticket + 2 * c_lo + lane_of;
-        int t;
-        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(t) : "l"(ticket) : "memory");
-        ms.last[h] = t == c_hi - c_lo;
-        if (t == c_hi - c_lo) *ticket = 0;  // ready for the next launch
       }
       if (r == 0) {
         mbar_arrive(&ms.q_free[qc & 1]);
         if (pair) mbar_arrive(&ms.q_free[(qc + 1) & 1]);
       }
       qc += pair ? 2 : 1;
-      if (whole) continue;
-      if (pair) sync_lane();
-      else sync_both();  // (both lanes join the partials)
-      if (ms.last[lane_of]) merge_rows<HD>(p, out0, pair ? r : tid, pair ? kRows : 2 * kRows, lane_rows, c_lo, c_hi, lane_of);
     }
     if (!ok && r == 0) report(p.st, CAST_ERR_TIMEOUT, blockIdx.x);
   }
