@@ -62,6 +62,7 @@ struct Item {
   int tile0, st, wt;          // index of the first of them; index i is tile i below st, else wt + i - st
   int lo, hi, s_end;          // positions that some row sees: [lo, hi) and [0, s_end)
   int tf, rows;               // first token, query rows
+  int no0, no1a, no1b;        // pairs pass over the halves of tiles that no row sees: the first half of tile no0 here, the second of no1a and no1b (-1: of none)
   int hi_min, lo_max, sinks;  // every row sees up to hi_min, as far as the window allows, and from lo_max on or below `sinks`
   int L, n, off;              // of the sequence
   int c_lo, c_hi;             // CTAs that share the item
@@ -484,6 +485,15 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
             x.tf = first_token(p, cur, rb);
             const int tl = last_token(p, cur, rb);
             x.rows = (tl + 1 - x.tf) * p.G;
+            // (only at the edges: the sinks' last tile, the window's first, the last)
+            const int a1 = sp.st - 1 - tile0, b0 = sp.st - tile0, c1 = sp.n - 1 - tile0, here = stop - tile0;
+            auto half_seen = [&](int i, int f) {
+              const int pos0 = sp.tile(tile0 + i) * kTile + f * kStep;
+              return pos0 < sp.s_end || (pos0 < sp.hi && pos0 + kStep > sp.lo);
+            };
+            x.no1a = a1 >= 0 && a1 < here && !half_seen(a1, 1) ? a1 : -1;
+            x.no0 = b0 >= 0 && b0 < here && !half_seen(b0, 0) ? b0 : -1;
+            x.no1b = c1 > a1 && c1 < here && !half_seen(c1, 1) ? c1 : -1;
             x.pair = x.rows > a.tokens * p.G;
             const long long hm = (long long)cur.L + (kTree ? 0 : x.tf + 1);
             x.hi_min = (int)(hm < sp.hi ? hm : sp.hi);
@@ -706,15 +716,17 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       wait_load(&ms.item_full[taken % kItems], (taken / kItems) & 1);
       if (!ok || !__any_sync(0xffffffffu, (ip = take()) != nullptr)) break;
       const int T = __reduce_max_sync(0xffffffffu, ip->T), pair = __reduce_max_sync(0xffffffffu, ip->pair);
+      const int no0 = __reduce_max_sync(0xffffffffu, ip->no0), no1a = __reduce_max_sync(0xffffffffu, ip->no1a), no1b = __reduce_max_sync(0xffffffffu, ip->no1b);
       give_back();
       if (T == 0) continue;
       for (int j = 0; j <= pair && ok; ++j) wait_load(&ms.q_full[(qc + j) & 1], ((qc + j) >> 1) & 1);
       const uint64_t q = dq + (uint64_t)(((pair ? qc + h : qc) & 1) * (M::kQ >> 4));
       for (int i = 0; i < T && ok; ++i) {
-        for (int f = pair ? 0 : h; f <= (pair ? 1 : h) && ok; ++f, ++steps) {
+        const int f0 = pair ? i == no0 : h, f1 = pair ? i != no1a && i != no1b : h;
+        for (int f = f0; f <= f1 && ok; ++f, ++steps) {
           const int buf = steps & 1;
           if (queued == 2) pop();
-          if (ok && (f == 0 || !pair)) wait_load(&ms.k_full[kst], kph);
+          if (ok && f == f0) wait_load(&ms.k_full[kst], kph);
           if (!ok) break;
           tc_fence_after();
           const uint64_t k = dk + (uint64_t)(kst * (M::kTileBytes >> 4) + f * (kStep * 128 >> 4));
@@ -723,7 +735,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
             umma_bf16(tm + kColS + buf * kStep, q + (uint64_t)((ks >> 2) * (kRegQ >> 4) + (ks & 3) * 2),
                       k + (uint64_t)((ks >> 2) * (kRegKV >> 4) + (ks & 3) * 2), idesc_qk, ks > 0);
           umma_commit(&ms.s_full[h][buf]);
-          const int last = f == 1 || !pair ? 1 : 0;
+          const int last = f == f1 ? 1 : 0;
           if (last) umma_commit(&ms.k_free[kst]);
           const int e = buf | (((steps >> 1) & 1) << 1) | (vph << 2) | (last << 3) | (f << 4) | (vst << 5);
           if (queued == 0) e0 = e;
@@ -791,18 +803,21 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
         for (int c = 0; c < HD; c += 32) tmem_st32(t_o + h * kLaneCols + c, z);
         tmem_wait_st();
       }
-      const int count = pair ? 2 * T : T, hi_plain = hi_all - kStep;
-      int pos0 = it.pos(0) + (pair ? 0 : h * kStep), ti = 0;
+      const int no0 = pair ? it.no0 : -1, no1a = pair ? it.no1a : -1, no1b = pair ? it.no1b : -1;
+      const int count = pair ? 2 * T - (no0 >= 0) - (no1a >= 0) - (no1b >= 0) : T, hi_plain = hi_all - kStep;
+      int ti = 0, step_half = pair ? no0 == 0 : h, pos0 = it.pos(0) + step_half * kStep;
 #pragma unroll 1
       for (int i = 0; i < count; ++i, ++steps) {
         const int buf = steps & 1;
         if (ok && !mbar_poll(&ms.s_full[h][buf], (steps >> 1) & 1)) ok = mbar_wait(&ms.s_full[h][buf], (steps >> 1) & 1);
-        const int half = pair ? i & 1 : h, here = pos0, at = ti;
-        if (half == 1 || !pair) {  // the next step's place
-          ++ti;
-          pos0 = it.pos(ti) + (pair ? 0 : h * kStep);
-        } else {
+        const int half = step_half, here = pos0, at = ti;
+        if (pair && half == 0 && ti != no1a && ti != no1b) {  // the next step's place
+          step_half = 1;
           pos0 += kStep;
+        } else {
+          ++ti;
+          if (pair) step_half = ti == no0;
+          pos0 = it.pos(ti) + step_half * kStep;
         }
         if (!warp_live) {
           tc_fence_before();
