@@ -134,6 +134,18 @@ def test_append(binding, dtype, Hq, Hkv, D, page, rows, rot, inter, norm, packed
     assert torch.equal(vc.cpu().view(torch.uint8), want_v.view(torch.uint8))
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_append_mixes(binding, seed):
+    """Any rotation, heads that fill no whole piece, few rows and more than the device has warps."""
+    rng = np.random.default_rng(500 + seed)
+    dtype, D = ["bf16", "bf16", "f32"][seed % 3], [64, 128][seed % 2]
+    Hq, Hkv = int(rng.integers(1, 20)), int(rng.integers(1, 9))
+    rows = [1, 3, 40, 900][int(rng.integers(0, 4))] if seed else 1500
+    rot = int(rng.choice([0, 2, 8, 12, 16, 20, 40, D // 2, D - 4, D]))
+    test_append(binding, dtype, Hq, Hkv, D, int(rng.choice([0, 3, 16, 64])), rows, rot, bool(rng.integers(0, 2)), bool(rng.integers(0, 2)), seed % 2 == 1, False,
+                int(rng.choice([0, 5000])))
+
+
 def simple(ctx, q, k, v, B, rows, Hq, Hkv, D, n, cap, start, q_out, kc, vc, inv, **kw):
     e = k.element_size() if k is not None else q.element_size()
     a = dict(row_start=None, first=None, depth=None, position=None, page=0, table=None, pages=0)

@@ -112,8 +112,8 @@ class Batch:
         return out
 
     def check(self, out, sample=400):
-        """Within: half a step of the output; with bf16, half a step of every weight, which moves an output by sum_p w_p |v_p| of it; and in 32
-        bits: a score by D half steps of sum_d |q_d k_d|, its exponent in powers of two by 3 half steps of it (up to 1.5 times the score) and
+        """Within: half a step of the output; with bf16, half a step of every weight, which moves an output by sum_p w_p |v_p| of it (2^-8 of it;
+        a weight in bf16 is off by 2^-9 of itself, and the cubic that forms a quarter of them by 2^-13.7); and in 32 bits: a score by D half steps of sum_d |q_d k_d|, its exponent in powers of two by 3 half steps of it (up to 1.5 times the score) and
         the exponential by 2^-21, so the weights by e, an output by 2 e sum_p w_p |v_p| (numerator and sum), and the sums over P positions
         by P half steps of the same."""
         got = out.double().cpu().numpy()
@@ -196,6 +196,32 @@ def test_tree_window(binding, dtype, Hq, Hkv, D, page, L, n, window, sinks):
     first = np.minimum(n, [3, 0, 50, 1, 2][:len(n)])  # a layer of a growing tree
     y = Batch(Hq * 100 + sum(n), dtype, Hq, Hkv, D, page, L, n, window, sinks, tree=True, first=first)
     y.check(y.run(binding))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_mixes(binding, seed):
+    """Prompts, single tokens, empty sequences and trees side by side, windows and sinks anywhere within a tile, and the same bits again."""
+    rng = np.random.default_rng(1000 + seed)
+    tree = seed % 4 == 3
+    D, G, Hkv = int(rng.choice([64, 128])), int(rng.choice([1, 3, 4, 7, 8, 16])), int(rng.choice([1, 2, 8, 24]))
+    B, page = int(rng.integers(1, 9)), int(rng.choice([0, 8, 16, 24, 40, 128]))
+    n = np.where(rng.random(B) < 0.4, rng.integers(0, 2, B), rng.integers(2, 125 if tree else 400, B))
+    n[rng.integers(0, B)] = max(1, int(n.max()))
+    L = rng.integers(0, 600, B) * rng.integers(0, 4, B)
+    window, sinks = (int(rng.integers(1, 500)), int(rng.integers(0, 200))) if seed % 3 else (0, 0)
+    x = Batch(seed, "bf16", G * Hkv, Hkv, D, page, L.tolist(), n.tolist(), window, sinks, packed=seed % 2 == 0 and not tree, tree=tree)
+    out = x.run(binding)
+    x.check(out, sample=60)
+    assert torch.equal(x.run(binding).view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("lo", [0, 1, 63, 64, 65, 127])
+@pytest.mark.parametrize("length,sinks", [(64, 0), (65, 64), (300, 65), (1, 300)])
+def test_edges_of_half_tiles(binding, lo, length, sinks):
+    """The window's first position, the sinks' and the chunk's last in each half of a tile, for two blocks of rows that share their tiles."""
+    window = 100
+    x = Batch(lo + length, "bf16", 160, 40, 128, 16, [window - 1 + 256 + lo - length % 64] * 2, [length] * 2, window, sinks)
+    x.check(x.run(binding), sample=40)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
