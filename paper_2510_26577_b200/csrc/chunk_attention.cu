@@ -6,6 +6,7 @@
 // both in fp32 in shared memory; S = Q K^T by packed multiply-adds, an online softmax, O += P V in registers. Positions that no row of the
 // item sees are neither loaded nor looked up (pages outside the window may be gone) and stand as zeros; a tile that some rows see only in
 // part takes the products with hidden positions out one by one, so that no value of a hidden row, NaN or infinity, reaches a row's output.
+// Bound by the chain of a tile: products by packed multiply-adds from shared memory, a warp's softmax, four barriers, 5 us in all, so small calls spread over all CTAs tile by tile.
 #include <math.h>
 
 #include "chunk_attn.h"
@@ -45,7 +46,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4], fl
 template <bool V> struct Choice { static constexpr bool value = V; };
 
 template <typename T, int D, bool kTree>
-__global__ void __launch_bounds__(kThreads) chunk_attn_cc_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(kThreads, 2) chunk_attn_cc_kernel(const ChunkParams p) {
   constexpr int KS = D + 4, SS = kPT + 4;     // row strides (floats)
   constexpr int CH = Vec<T>::N, CPR = D / CH; // elements per 16-byte chunk, chunks per row
   constexpr int DC = D / 32;                  // output columns per lane
@@ -125,27 +126,42 @@ __global__ void __launch_bounds__(kThreads) chunk_attn_cc_kernel(const ChunkPara
 #pragma unroll
       for (int e = 0; e < DC; ++e) o[i][e] = 0.f;
 
+    // A tile's rows on their way, in registers: they are read under the softmax and the products of the tile before as far as
+    // 128 registers a thread, two CTAs per SM, hold them: of 128 dims the keys alone, in fp32 none.
+    constexpr int NL = kPT * CPR / kThreads;
+    constexpr bool kAheadK = NL <= 4, kAheadV = D == 64;
+    uint4 next_k[NL], next_v[NL];
+    auto row_of = [&](int i, int x, const T* cache) {
+      const int j = tid + x * kThreads;
+      const long long slot = slot_s[i & 1][j / CPR];
+      return slot >= 0 ? *reinterpret_cast<const uint4*>(cache + ((size_t)slot * p.Hkv + kvh) * D + j % CPR * CH) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto fetch = [&](int i) {
+#pragma unroll
+      for (int x = 0; x < NL; ++x) {
+        if (kAheadK) next_k[x] = row_of(i, x, kc);
+        if (kAheadV) next_v[x] = row_of(i, x, vc);
+      }
+    };
+    __syncthreads();  // the slots, Qs, sight, anc_s
+    if (w.t0 < w.t1) fetch(w.t0);
     for (int i = w.t0; i < w.t1; ++i) {
       const int pbase = sp.tile(i) * kPT;
-      __syncthreads();  // previous tile consumed; the slots (and Qs, sight, anc_s on the first pass) visible
+      __syncthreads();  // previous tile consumed
 #pragma unroll 4
-      for (int j = tid; j < kPT * CPR; j += kThreads) {
-        const int pl = j / CPR, ch = j % CPR;
-        const long long slot = slot_s[i & 1][pl];
-        float fk[CH] = {}, fv[CH] = {};
-        if (slot >= 0) {
-          const size_t at = ((size_t)slot * p.Hkv + kvh) * D + ch * CH;
-          Vec<T>::unpack(*reinterpret_cast<const uint4*>(kc + at), fk);
-          Vec<T>::unpack(*reinterpret_cast<const uint4*>(vc + at), fv);
-        }
+      for (int x = 0; x < NL; ++x) {
+        const int j = tid + x * kThreads, pl = j / CPR, ch = j % CPR;
+        float fk[CH], fv[CH];
+        Vec<T>::unpack(kAheadK ? next_k[x] : row_of(i, x, kc), fk);
+        Vec<T>::unpack(kAheadV ? next_v[x] : row_of(i, x, vc), fv);
 #pragma unroll
         for (int e = 0; e < CH; e += 4) {
           *reinterpret_cast<float4*>(Ks + pl * KS + ch * CH + e) = make_float4(fk[e], fk[e + 1], fk[e + 2], fk[e + 3]);
           *reinterpret_cast<float4*>(Vs + pl * D + ch * CH + e) = make_float4(fv[e], fv[e + 1], fv[e + 2], fv[e + 3]);
         }
       }
-      __syncthreads();
       find_slots(i + 1);
+      __syncthreads();
       {  // S: thread (ty, tx) owns rows 2ty, 2ty+1 and positions tx, tx+16, tx+32, tx+48
         f32x2 acc[2][4] = {};
 #pragma unroll 8
@@ -173,6 +189,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attn_cc_kernel(const ChunkPara
         }
       }
       __syncthreads();
+      if (i + 1 < w.t1) fetch(i + 1);
       // online softmax and O += P V: warp w owns rows 4w .. 4w+3
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr) {
@@ -307,7 +324,7 @@ template <typename T, int D, bool kTree>
 cast_status launch_cc(cast_ctx* c, ChunkParams& p, cudaStream_t s) {
   p.block_rows = kRB;
   p.block_tokens = kRB % p.G == 0 ? kRB / p.G : 0;
-  p.min_units = kItemCost + 2;
+  p.min_units = kItemCost + 1;  // (a tile is 5 us here, more than what a split costs; 3 sequences of 20-131 tokens under a window of 256, 8/8 heads of 64 dims: 38 us, from two tiles on 45)
   const int grid = 2 * c->num_sms < kChunkGrid ? 2 * c->num_sms : kChunkGrid;
   p.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(c->chunk_ws) + kTicketBytes);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)kChunkGrid * 2 * kRB * D);
