@@ -536,8 +536,8 @@ CAST_API cast_status cast_evict_kv_q4(cast_ctx* ctx, void* k_codes, void* k_rang
  * [first_row, n_rows) of q_out and the cache are left untouched; n_rows[b] is clamped to [0, rows].
  * Under cast_set_attention_early_reads the call is one of the caller's own: it writes q and the rows at start + t, which the promise
  * allows right before an attention call whose kv_len is start, and nothing else.
- * Needs D in {64, 128}, pointers and strides that are multiples of 16 bytes. CAPACITY: B beyond max_batch, B * rows or a sequence's positions past
- * 2^31 - 2^16. Device errors: BAD_PAGE (a position below 0 or past the capacity, a page id out of range: keys and values of that row are not stored),
+ * Needs D in {64, 128}, pointers (but for those of numbers per sequence, row or pair) and strides that are multiples of 16 bytes. CAPACITY: B beyond
+ * max_batch, B * rows or a sequence's positions past 2^31 - 2^16, more than 65536 heads. Device errors: BAD_PAGE (a position below 0 or past the capacity, a page id out of range: keys and values of that row are not stored),
  * BAD_TREE (packed: rows of the sequence outside [0, rows): it is left out).
  */
 CAST_API cast_status cast_append_kv(cast_ctx* ctx, const void* q, size_t q_stride_bytes, const void* k, size_t k_stride_bytes,
@@ -560,7 +560,8 @@ CAST_API cast_status cast_reserve_chunk_attention(cast_ctx* ctx, cast_dtype dtyp
  *                untouched, n_new[b] is clamped to [0, rows]; the tokens' number is not bound to the context's trees
  *   window       0: none; sinks: with a window, the first positions that stay visible. Page-table entries all of whose positions no
  *                row of the sequence sees may hold anything (but for those of a tree's own tokens).
- * Sums and softmax in fp32, a weight of a bf16 call is rounded to bf16 once on its way into the product. What a row does not see reaches no output of it, NaN
+ * Sums and softmax in fp32, a weight of a bf16 call is right to 2^-13 (a quarter of the exponentials are a cubic) and
+ * rounded to bf16 once on its way into the product. What a row does not see reaches no output of it, NaN
  * and infinities included; a row that sees nothing gives zeros. The same inputs give the same bits. Never reads early.
  * Other arguments and errors as for cast_tree_attention; needs cast_reserve_chunk_attention, the context's device as the current one (INVALID_ARG)
  * and q, out, caches aligned to 16 bytes. INVALID_ARG: window or sinks below 0. CAPACITY: B beyond max_batch; positions of a sequence, B * rows or rows * Hq / Hkv past

@@ -372,7 +372,7 @@ extern "C" cast_status cast_append_kv(cast_ctx* c, const void* q, size_t q_strid
     if (k_stride_bytes < (size_t)Hkv * D * e || v_stride_bytes < (size_t)Hkv * D * e) return CAST_ERR_SHAPE;
     all |= (uintptr_t)k | (uintptr_t)v | k_stride_bytes | v_stride_bytes | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)k_weight;
   }
-  if (all & 15) return CAST_ERR_SHAPE;
+  if (all & 15 || (uintptr_t)inv_freq & 7) return CAST_ERR_SHAPE;
   AppendParams p;
   p.g = {page_table, page_size, seq_capacity, num_pages};
   // (the count of live rows, with a grid's step behind it, is 32-bit)

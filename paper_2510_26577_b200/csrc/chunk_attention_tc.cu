@@ -82,7 +82,7 @@ struct Misc {
   uint64_t v_raw[M::kStagesV];   // what v_full is to a tile that is cleaned first: V's warp waits for these, in turn, and completes v_full
   uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];  // [lane][buffer]: scores there, weights there, their P V over
   uint32_t tmem;
-  int last[2];
+  int last[3];  // this CTA joins the partials: of lane 0's block, lane 1's, of a single block
   uint32_t bad[M::kStagesV][kTile / 32];  // positions of the V tile that the softmax threads take over
   float2 row[kRows];                      // what the threads of a row tell one another at an item's end
   Item item[kItems];
@@ -1037,11 +1037,11 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           int32_t* ticket = p.ticket + 2 * c_lo + lane_of;
           int t;
           asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(t) : "l"(ticket) : "memory");
-          ms.last[h] = t == c_hi - c_lo;
+          ms.last[pair ? h : 2] = t == c_hi - c_lo;
           if (t == c_hi - c_lo) *ticket = 0;  // ready for the next launch
         }
         sync_rows();
-        if (ms.last[lane_of]) {  // (both lanes join the partials of a single block)
+        if (ms.last[pair ? h : 2]) {  // (both lanes join the partials of a single block)
           merge_rows<HD>(p, stage_rows, out0, pair ? r : tid, pair ? kRows : 2 * kRows, lane_rows, c_lo, c_hi, lane_of);
           staged_all = lane_rows > kFewRows;
           if (staged_all) sync_rows();
