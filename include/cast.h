@@ -566,7 +566,8 @@ CAST_API cast_status cast_reserve_chunk_attention(cast_ctx* ctx, cast_dtype dtyp
  * Other arguments and errors as for cast_tree_attention; needs cast_reserve_chunk_attention, the context's device as the current one (INVALID_ARG)
  * and q, out, caches aligned to 16 bytes. INVALID_ARG: window or sinks below 0. CAPACITY: B beyond max_batch; positions of a sequence, B * rows or rows * Hq / Hkv past
  * 2^31 - 2^16. Device errors: BAD_TREE (packed: rows outside [0, rows), the sequence is left out), BAD_PAGE (kv_len + n_new past the capacity: the
- * positions behind it are not seen; a page id out of range: which row of the cache stands in for it is not defined).
+ * positions behind it are not seen; a page id out of range: which row of the cache stands in for it is not defined), TIMEOUT (a wait in the
+ * kernel ran out; the context is not used for these two calls again).
  */
 CAST_API cast_status cast_chunk_attention(cast_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, cast_dtype dtype,
                                           int B, int rows, const int32_t* row_start, int Hq, int Hkv, int D, int page_size,

@@ -6,7 +6,7 @@
 // formed in turns and in fp64 and only its fraction becomes fp32: in fp32 a position of 100 000 leaves 0.006 of a radian.
 //
 // One pass: a row is read once and written once, so memory bounds a long call: 10 400 rows of 32/8 heads of 128 dims in bf16 (255 MB in
-// and out) take 53 us, 5.2 TB/s, 79 % of a copy's rate. What comes next is instructions, 74 % of the issue slots; hence:
+// and out) take 53 us, 4.8 TB/s, 73 % of a copy's rate (the loop without its arithmetic: the same). What comes next is instructions, 74 % of the issue slots; hence:
 // - A warp takes a row, or a part of one where rows are few, 512 bytes of one tensor at a time. It needs no other warp.
 // - Loads run ahead by cp.async into a ring of the warp's own, over the ends of rows, so that the loop need not be unrolled over
 //   registers in flight (with it: 61 us, and more registers in flight were slower, at 65 to 86, for they cost warps).

@@ -7,8 +7,7 @@
 //   more than one block of rows (prompts, wide trees): lane 0 and lane 1 take a block each, and the K and V tiles serve both;
 //   one block (decoding, small trees): lane 0 takes the first half of every tile and lane 1 the second, each with its own running sums, and they join at the end.
 // Twelve warps: four of softmax per lane (a thread a row), one that walks the line, hands the items out through a ring in shared memory and loads Q and K (TMA), one that
-// loads V and cleans it, and per lane one that issues its products: a
-// buffer's P V, then the next Q K^T into it, across the items' ends, so loads, products and softmax of the next item run under the output of the last.
+// loads V and cleans it, and per lane one that issues its products: a buffer's P V, then the next Q K^T into it, across the items' ends, so loads, products and softmax of the next item run under the output of the last.
 // What the single warps do per tile is a chain of dependent instructions and as much a bound as bytes and products are: one issuer for both lanes, loads of 64
 // positions, integer divisions by the page size, a load of the page table per tile were 1 us each or more. With every warp walking the line for itself the walk's
 // state was spilled, and beside 227 KB of shared memory local memory does not stay in L1: few instructions between two steps took 600 cycles. (Two threads a row, half
@@ -21,6 +20,14 @@
 // V rows nobody sees to zero (they may never have been loaded), looks through those that some rows see, zeroes the ones that hold a NaN or an
 // infinity and notes them; the softmax threads that do see such a row add its weighted values to O themselves, in fp32. Scores of hidden
 // positions are masked by select.
+//
+// What it measures (bf16, heads of 128) and what bounds it:
+//   two sequences of 32768 + 1000 new tokens, 28/4 heads: 0.93 ms, 1030 TFLOP/s, 63 % of a dense product's rate. A step of both lanes is worth 1020 cycles of softmax (exponentials,
+//     masks, sums, rounding: 64 columns of 256 rows) behind a chain of 760 from scores to weights; softmax alone takes 0.75 ms, products and issuers alone 0.70. Issue slots 46 % busy, tensor pipe 44 %;
+//   one prompt of 4096, 32/8 heads: 167 us, 824 TFLOP/s: the same, with half of the diagonal's tiles masked, and starts and ends;
+//   64 sequences of 512-4096, one token each, 32/8 heads: 125 us, 4.8 TB/s, 74 % of a copy's rate over pages of 16 at scattered places (without pages 109 us, 5.6 TB/s);
+//   one sequence of 8192, 60 tokens of a tree under a window of 1024: 24 us, a chain: launch and plan 3.8, first scores 2, two to four tiles of 1.1 to 1.5, output 2, the join of an
+//     item's partials 6.
 #include <math.h>
 
 #include "chunk_attn.h"
