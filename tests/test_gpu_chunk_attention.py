@@ -215,6 +215,16 @@ def test_mixes(binding, seed):
     assert torch.equal(x.run(binding).view(torch.int16), out.view(torch.int16))
 
 
+@pytest.mark.parametrize("G,Hkv,D,n,page", [(128, 1, 128, 3, 16), (100, 2, 64, 2, 136), (43, 4, 128, 50, 384), (5, 40, 64, 70, 512), (16, 148, 128, 9, 8),
+                                            (127, 3, 128, 1, 0), (1, 75, 64, 300, 0), (64, 1, 128, 200, 1000)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_groups_and_pages(binding, G, Hkv, D, n, page, tree):
+    """Groups that fill a block of rows or leave most of it empty, more kv-heads than SMs, pages around and above a tile."""
+    n = min(n, 128) if tree else n
+    x = Batch(G * 7 + n, "bf16", G * Hkv, Hkv, D, page, [333, 0], [n, max(1, n // 2)], 150, 5, tree=tree)
+    x.check(x.run(binding), sample=12)
+
+
 @pytest.mark.parametrize("lo", [0, 1, 63, 64, 65, 127])
 @pytest.mark.parametrize("length,sinks", [(64, 0), (65, 64), (300, 65), (1, 300)])
 def test_edges_of_half_tiles(binding, lo, length, sinks):
