@@ -25,7 +25,7 @@
 //   two sequences of 32768 + 1000 new tokens, 28/4 heads: 0.93 ms, 1030 TFLOP/s, 63 % of a dense product's rate. A step of both lanes is worth 1020 cycles of softmax (exponentials,
 //     masks, sums, rounding: 64 columns of 256 rows) behind a chain of 760 from scores to weights; softmax alone takes 0.75 ms, products and issuers alone 0.70. Issue slots 46 % busy, tensor pipe 44 %;
 //   one prompt of 4096, 32/8 heads: 167 us, 824 TFLOP/s: the same, with half of the diagonal's tiles masked, and starts and ends;
-//   64 sequences of 512-4096, one token each, 32/8 heads: 125 us, 4.8 TB/s, 74 % of a copy's rate over pages of 16 at scattered places (without pages 109 us, 5.6 TB/s);
+//   64 sequences of 512-4096, one token each, 32/8 heads: 125 us, 4.8 TB/s, 74 % of a copy's rate, whatever the pages (16 scattered or in order, 128, none);
 //   one sequence of 8192, 60 tokens of a tree under a window of 1024: 24 us, a chain: launch and plan 3.8, first scores 2, two to four tiles of 1.1 to 1.5, output 2, the join of an
 //     item's partials 6.
 #include <math.h>
