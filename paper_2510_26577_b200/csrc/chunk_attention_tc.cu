@@ -437,8 +437,9 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
     };
     static_assert(kPerLane == 2, "a lane holds two sequences");
     if (!is_v) {
-      plan_warp<kTile, kTree>(p, seq, upto, units);
-      workers = workers_of(p, units);
+      long long items;
+      plan_warp<kTile, kTree>(p, seq, upto, units, items);
+      workers = workers_of(p, units, items);
       if (aligned && units > 0 && (int)blockIdx.x < workers) {
         line_at = bound_of(units, workers, blockIdx.x);
         line_end = bound_of(units, workers, blockIdx.x + 1);
@@ -1163,6 +1164,8 @@ bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspa
   p.block_tokens = pairs < c->num_sms ? a.tokens : 2 * a.tokens;
   p.block_rows = p.block_tokens * p.G;
   p.min_units = kItemCost + 2;
+  // Only few items can be cut into more parts than pay (131 072 positions, one kv-head: 32 tokens 175 -> 95 us, one token 122 -> 73); with more of them the rule would cost a small call 0.5 us.
+  p.join = (long long)p.B * p.Hkv <= 4 ? 2.f : 0.f;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   CUtensorMap mq, mk, mv;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)p.Hq, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)p.Hq * D * 2};

@@ -27,6 +27,7 @@ struct ChunkParams {
   int block_tokens;         // where they are whole tokens: how many; else 0
   int max_pos;              // capacity of a sequence
   int min_units;            // a CTA's stretch at least
+  float join;               // partials that are joined in the time of a tile (0: any number)
   int Nmax;                 // tree: most tokens
   int window, sinks;        // window 0: none
   const int32_t *row_start, *kv_len, *n_new, *first_row, *depth;
@@ -110,11 +111,11 @@ __device__ __forceinline__ long long mul_div(long long a, int b, long long c) {
   return x < 0xffffffffll && c <= 0xffffffffll ? (long long)((uint32_t)x / (uint32_t)c) : x / c;
 }
 
-// A warp's plan, a lane per two sequences (lane l: sequences l and l + 32): the sequences, the units up to and including each, all units. Between the kernel's start and its
+// A warp's plan, a lane per two sequences (lane l: sequences l and l + 32): the sequences, the units up to and including each, all units, all items. Between the kernel's start and its
 // first load there is one round trip to memory and one scan. (A warp per sequence, with a barrier in front and behind, took 2.6 us for one sequence and 5.7 for 64.)
 constexpr int kPerLane = CAST_MAX_BATCH / 32;
 template <int PT, bool kTree>
-__device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[kPerLane], long long (&upto)[kPerLane], long long& units) {
+__device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[kPerLane], long long (&upto)[kPerLane], long long& units, long long& items) {
   const int lane = threadIdx.x & 31;
   int L[kPerLane], n[kPerLane], F[kPerLane], off[kPerLane];
 #pragma unroll
@@ -127,6 +128,7 @@ __device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[
     off[j] = in && p.row_start ? p.row_start[b] : 0;
   }
   long long run = 0;
+  items = 0;
 #pragma unroll
   for (int j = 0; j < kPerLane; ++j) {
     const int b = j * 32 + lane;
@@ -157,6 +159,7 @@ __device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[
       }
     }
     const int blocks = blocks_of(p, s);
+    items += (long long)__reduce_add_sync(0xffffffffu, (unsigned)blocks) * p.Hkv;
     long long u = 0;
     if (blocks <= 4) {
       for (int rb = 0; rb < blocks; ++rb) u += block_span<PT, kTree>(p, s, rb).n + kItemCost;
@@ -187,9 +190,11 @@ __device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[
   }
   units = run;
 }
-// CTAs that get a stretch.
-__device__ __forceinline__ int workers_of(const ChunkParams& p, long long units) {
-  const long long w = mul_div(units, 1, p.min_units);
+// CTAs that get a stretch. One CTA joins the partials of an item, one behind the other, so n stretches of an item of A tiles take A / n + n / join tiles' time: n is
+// sqrt(join A) at most, over all items sqrt(join units items).
+__device__ __forceinline__ int workers_of(const ChunkParams& p, long long units, long long items) {
+  long long w = mul_div(units, 1, p.min_units);
+  if (p.join > 0.f) w = min(w, (long long)fminf(sqrtf(p.join * (float)units * (float)items), 1e6f));
   return (int)(w < 1 ? 1 : w < (long long)gridDim.x ? w : (long long)gridDim.x);
 }
 
@@ -199,8 +204,8 @@ __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
   const int lane = threadIdx.x & 31;
   if (threadIdx.x < 32) {
     ChunkSeq seq[kPerLane];
-    long long upto[kPerLane], units;
-    plan_warp<PT, kTree>(p, seq, upto, units);
+    long long upto[kPerLane], units, items;
+    plan_warp<PT, kTree>(p, seq, upto, units, items);
 #pragma unroll
     for (int j = 0; j < kPerLane; ++j) {
       pl.seq[j * 32 + lane] = seq[j];
@@ -209,7 +214,7 @@ __device__ __forceinline__ void make_plan(const ChunkParams& p, ChunkPlan& pl) {
     if (lane == 0) {
       pl.pre[0] = 0;
       pl.units = units;
-      pl.workers = workers_of(p, units);
+      pl.workers = workers_of(p, units, items);
     }
   }
   __syncthreads();
