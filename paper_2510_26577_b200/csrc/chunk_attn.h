@@ -4,7 +4,8 @@
 // A query row is a (new token, head of the GQA group) pair; an item is a block of rows of one (sequence, kv-head). Row t of a chunk
 // stands at position L + t and sees the positions p <= L + t, with a window those of them with p > L + t - window or p < sinks. Row t of
 // a tree stands at L + depth[t]; of the prefix it sees the same, of the tree its ancestors that lie in the window (by depth) or among the sinks.
-// An item walks the tiles that some row of it sees: those of the sinks, then those from the window's start on.
+// An item walks the tiles that some row of it sees: those of the sinks, then those from the window's start on. (A tree's token j lies at L + j but
+// stands at L + depth[j], so as a sink it may lie behind the sinks and before the window: a tree's own places are walked whatever the window.)
 //
 // The line: items one behind the other (sequence, row block, kv-head fastest), each as long as its tiles plus kItemCost for its queries and
 // output; CTA c of n takes the stretch [c U / n, (c + 1) U / n) of it, so ragged batches load the machine evenly. An item that lies across
@@ -52,17 +53,18 @@ struct Span {
   int lo, hi, s_end;   // positions [0, s_end) and [lo, hi)
   int st, wt;          // tiles 0..st-1, then wt, wt + 1, ...
   int n;
-  __device__ __forceinline__ int tile(int i) const { return i < st ? i : wt + (i - st); }
+  __host__ __device__ __forceinline__ int tile(int i) const { return i < st ? i : wt + (i - st); }
 };
 
 template <int PT, bool kTree>
-__device__ __forceinline__ Span span_of(const ChunkParams& p, const ChunkSeq& s, int tf, int tl) {
+__host__ __device__ __forceinline__ Span span_of(const ChunkParams& p, const ChunkSeq& s, int tf, int tl) {
   Span x;
   const long long end = (long long)s.L + (kTree ? s.n : tl + 1);
   x.hi = (int)(end < p.max_pos ? end : p.max_pos);
   x.lo = 0;
   if (p.window > 0) {
-    const long long lo = (long long)s.L + (kTree ? s.d0 : tf) - p.window + 1;
+    long long lo = (long long)s.L + (kTree ? s.d0 : tf) - p.window + 1;
+    if (kTree && lo > s.L) lo = s.L;
     x.lo = lo < 0 ? 0 : lo > x.hi ? x.hi : (int)lo;
   }
   x.s_end = x.lo > 0 ? (p.sinks < x.lo ? p.sinks : x.lo) : 0;

@@ -1,0 +1,79 @@
+"""The tiles that the chunk attention walks, on the host: the kernels' own arithmetic, compiled for the CPU, against the definition of
+what a row sees."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2510_26577_b200 import build
+
+HARNESS = r"""
+#include "cast.h"
+#include "chunk_attn.h"
+using namespace cast;
+template <int PT, bool kTree>
+static void walk(const int* a, int* out) {
+  ChunkParams p = {};
+  p.max_pos = a[0]; p.window = a[1]; p.sinks = a[2];
+  ChunkSeq s = {};
+  s.L = a[3]; s.n = a[4]; s.d0 = (unsigned short)a[5];
+  const Span x = span_of<PT, kTree>(p, s, a[6], a[7]);
+  out[0] = x.lo; out[1] = x.hi; out[2] = x.s_end; out[3] = x.n;
+  for (int i = 0; i < x.n && i < 64; ++i) out[4 + i] = x.tile(i);
+}
+extern "C" CAST_API void span(int tile, int tree, const int* a, int* out) {
+  if (tile == 64) tree ? walk<64, true>(a, out) : walk<64, false>(a, out);
+  else tree ? walk<128, true>(a, out) : walk<128, false>(a, out);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    d = tmp_path_factory.mktemp("walk")
+    src, out = d / "walk.cu", d / "walk.so"
+    src.write_text(HARNESS)
+    subprocess.run([build._nvcc(), *build.NVCC_FLAGS, "-shared", "-o", str(out), str(src)], check=True, capture_output=True, text=True)
+    return ctypes.CDLL(str(out))
+
+
+def span(lib, tile, tree, max_pos, window, sinks, L, n, d0, tf, tl):
+    a, out = np.array([max_pos, window, sinks, L, n, d0, tf, tl], np.int32), np.zeros(68, np.int32)
+    lib.span(tile, int(tree), a.ctypes.data_as(ctypes.c_void_p), out.ctypes.data_as(ctypes.c_void_p))
+    assert out[3] <= 64
+    return out[0], out[1], out[2], out[4:4 + out[3]]
+
+
+def walked(positions, lo, hi, s_end, tiles, tile):
+    """Whether each position is loaded: in a tile of the walk and in the ranges that some row sees."""
+    return np.isin(positions // tile, tiles) & (((positions >= lo) & (positions < hi)) | (positions < s_end))
+
+
+@pytest.mark.parametrize("tile", [64, 128])
+def test_every_token_that_a_trees_row_sees_is_walked(lib, tile):
+    """Random trees, their later rows, short windows, sinks that reach into the tree."""
+    rng = np.random.default_rng(tile)
+    lost = 0
+    for _ in range(20000):
+        n = int(rng.integers(1, 40))
+        L, window, sinks = int(rng.integers(0, 150)), int(rng.integers(1, 8)), int(rng.integers(0, 170))
+        parent = [-1] + [int(rng.integers(max(0, t - 3), t)) for t in range(1, n)]
+        depth = np.zeros(n, np.int64)
+        for t in range(1, n):
+            depth[t] = depth[parent[t]] + 1
+        first = int(rng.integers(0, n))
+        seen = np.zeros(L + n, bool)
+        pos = np.arange(L)
+        for t in range(first, n):
+            seen[:L] |= (L + depth[t] - pos < window) | (pos < sinks)
+            j = t
+            while j >= 0:
+                seen[L + j] |= depth[t] - depth[j] < window or L + depth[j] < sinks
+                j = parent[j]
+        d0 = int(depth[first:].min()) if first else 0
+        lo, hi, s_end, tiles = span(lib, tile, True, 1 << 20, window, sinks, L, n, d0, first, n - 1)
+        at = np.flatnonzero(seen)
+        lost += not walked(at, lo, hi, s_end, tiles, tile).all()
+    assert lost == 0
