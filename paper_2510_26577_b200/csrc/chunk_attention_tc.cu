@@ -493,15 +493,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
             x.tf = first_token(p, cur, rb);
             const int tl = last_token(p, cur, rb);
             x.rows = (tl + 1 - x.tf) * p.G;
-            // (only at the edges: the sinks' last tile, the window's first, the last)
-            const int a1 = sp.st - 1 - tile0, b0 = sp.st - tile0, c1 = sp.n - 1 - tile0, here = stop - tile0;
-            auto half_seen = [&](int i, int f) {
-              const int pos0 = sp.tile(tile0 + i) * kTile + f * kStep;
-              return pos0 < sp.s_end || (pos0 < sp.hi && pos0 + kStep > sp.lo);
-            };
-            x.no1a = a1 >= 0 && a1 < here && !half_seen(a1, 1) ? a1 : -1;
-            x.no0 = b0 >= 0 && b0 < here && !half_seen(b0, 0) ? b0 : -1;
-            x.no1b = c1 > a1 && c1 < here && !half_seen(c1, 1) ? c1 : -1;
+            sp.unseen_halves<kTile>(tile0, stop, x.no0, x.no1a, x.no1b);
             x.pair = x.rows > a.tokens * p.G;
             const long long hm = (long long)cur.L + (kTree ? 0 : x.tf + 1);
             x.hi_min = (int)(hm < sp.hi ? hm : sp.hi);

@@ -54,6 +54,21 @@ struct Span {
   int st, wt;          // tiles 0..st-1, then wt, wt + 1, ...
   int n;
   __host__ __device__ __forceinline__ int tile(int i) const { return i < st ? i : wt + (i - st); }
+  // Whether some row sees a position of half `f` of tile i (tiles of PT positions).
+  template <int PT>
+  __host__ __device__ __forceinline__ bool half_seen(int i, int f) const {
+    const int pos0 = tile(i) * PT + f * (PT / 2);
+    return pos0 < s_end || (pos0 < hi && pos0 + PT / 2 > lo);
+  }
+  // Of the tiles [tile0, stop), counted from tile0: one whose first half no row sees, two whose second half none does (-1: none). Only at the edges: the
+  // sinks' last tile, the window's first, the last. Some row sees one half of every tile at least: the other roles of a kernel count on a step in each.
+  template <int PT>
+  __host__ __device__ __forceinline__ void unseen_halves(int tile0, int stop, int& no0, int& no1a, int& no1b) const {
+    const int a1 = st - 1 - tile0, b0 = st - tile0, c1 = n - 1 - tile0, here = stop - tile0;
+    no1a = a1 >= 0 && a1 < here && !half_seen<PT>(tile0 + a1, 1) ? a1 : -1;
+    no0 = b0 >= 0 && b0 < here && !half_seen<PT>(tile0 + b0, 0) ? b0 : -1;
+    no1b = c1 > a1 && c1 < here && !half_seen<PT>(tile0 + c1, 1) ? c1 : -1;
+  }
 };
 
 template <int PT, bool kTree>
@@ -72,7 +87,7 @@ __host__ __device__ __forceinline__ Span span_of(const ChunkParams& p, const Chu
   x.wt = (int)((uint32_t)x.lo / PT);
   if (x.wt < x.st) x.wt = x.st;
   const int wt1 = (int)((uint32_t)(x.hi + PT - 1) / PT);
-  x.n = x.st + (wt1 > x.wt ? wt1 - x.wt : 0);
+  x.n = x.st + (x.lo < x.hi && wt1 > x.wt ? wt1 - x.wt : 0);  // (rows wholly past the capacity: lo = hi, and a tile they both lie in is none)
   return x;
 }
 

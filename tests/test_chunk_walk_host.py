@@ -22,6 +22,7 @@ static void walk(const int* a, int* out) {
   const Span x = span_of<PT, kTree>(p, s, a[6], a[7]);
   out[0] = x.lo; out[1] = x.hi; out[2] = x.s_end; out[3] = x.n;
   for (int i = 0; i < x.n && i < 64; ++i) out[4 + i] = x.tile(i);
+  x.template unseen_halves<PT>(a[8], a[9] < 0 ? x.n : a[9], out[68], out[69], out[70]);
 }
 extern "C" CAST_API void span(int tile, int tree, const int* a, int* out) {
   if (tile == 64) tree ? walk<64, true>(a, out) : walk<64, false>(a, out);
@@ -39,11 +40,11 @@ def lib(tmp_path_factory):
     return ctypes.CDLL(str(out))
 
 
-def span(lib, tile, tree, max_pos, window, sinks, L, n, d0, tf, tl):
-    a, out = np.array([max_pos, window, sinks, L, n, d0, tf, tl], np.int32), np.zeros(68, np.int32)
+def span(lib, tile, tree, max_pos, window, sinks, L, n, d0, tf, tl, cut=(0, -1), halves=False):
+    a, out = np.array([max_pos, window, sinks, L, n, d0, tf, tl, *cut], np.int32), np.zeros(71, np.int32)
     lib.span(tile, int(tree), a.ctypes.data_as(ctypes.c_void_p), out.ctypes.data_as(ctypes.c_void_p))
     assert out[3] <= 64
-    return out[0], out[1], out[2], out[4:4 + out[3]]
+    return (out[0], out[1], out[2], out[4:4 + out[3]]) + ((out[68:],) if halves else ())
 
 
 def walked(positions, lo, hi, s_end, tiles, tile):
@@ -77,3 +78,33 @@ def test_every_token_that_a_trees_row_sees_is_walked(lib, tile):
         at = np.flatnonzero(seen)
         lost += not walked(at, lo, hi, s_end, tiles, tile).all()
     assert lost == 0
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("edge", [0, 1, 63, 64, 65, 127])
+def test_every_tile_has_a_half_that_some_row_sees(lib, tree, edge):
+    """Around and past the capacity too, wherever it lies in a tile: a tile both of whose halves are passed over is one whose place in the ring
+    nobody gives back. And what is passed over is what no row sees, by the definition."""
+    rng = np.random.default_rng(edge)
+    for _ in range(6000):
+        max_pos = 128 * int(rng.integers(1, 6)) + edge
+        n = int(rng.integers(1, 129 if tree else 700))
+        L = int(rng.integers(0, 2 * max_pos))
+        window, sinks = int(rng.integers(0, 400)), int(rng.choice([0, 1, 4, 64, 130, 1000]))
+        tf = int(rng.integers(0, n))
+        tl = n - 1 if tree else min(n - 1, tf + int(rng.integers(0, 200)))
+        d0 = int(rng.integers(0, tf + 1)) if tree else 0
+        lo, hi, s_end, tiles, _ = span(lib, 128, tree, max_pos, window, sinks, L, n, d0, tf, tl, halves=True)
+        tile0 = int(rng.integers(0, len(tiles) + 1))
+        stop = int(rng.integers(tile0, len(tiles) + 1))
+        *_, (no0, no1a, no1b) = span(lib, 128, tree, max_pos, window, sinks, L, n, d0, tf, tl, cut=(tile0, stop), halves=True)
+        for i, t in enumerate(tiles[tile0:stop]):
+            pos = 128 * int(t) + np.arange(128)
+            if tree:  # (a bound on what the rows see: all that any tree's could)
+                seen = (pos < L + n) & ((pos < sinks) | (pos > L + d0 - window) | (pos >= L)) if window else pos < L + n
+            else:
+                seen = (pos <= L + tl) & ((pos < sinks) | (pos > L + tf - window)) if window else pos <= L + tl
+            half = (seen & (pos < max_pos)).reshape(2, 64).any(1)
+            skipped = np.array([i == no0, i in (no1a, no1b)])
+            assert not skipped.all(), (max_pos, n, L, window, sinks, tf, tl)
+            assert not (half & skipped).any() and half.any()

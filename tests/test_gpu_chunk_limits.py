@@ -53,3 +53,54 @@ def test_deep_trees_later_rows_short_windows(binding, seed):  # noqa: F811
         first.append(int(rng.integers(n // 2, n)))
     x = Tree(seed, "f32" if seed % 4 == 3 else "bf16", 2 * G, 2, D, [16, 0, 24, 8][seed % 4], L, parents, int(rng.integers(1, 6)), sinks, first)
     x.check(x.run(binding))
+
+
+class Past(Batch):
+    """The same in a cache that ends at position `cut`, before some sequences do: what lies behind it is not seen."""
+
+    def __init__(self, cut, *args, **kw):
+        self.cut = cut
+        super().__init__(*args, **kw)
+        p = self.paged
+        p.positions = cut
+        if self.page:
+            assert cut % self.page == 0
+            p.cap = cut // self.page
+            p.table, self.table = p.table[:, :p.cap], self.table[:, :p.cap]
+        else:
+            p.cap, p.shape = cut, (self.B, cut)
+            self.k, self.v = self.k[:, :cut].contiguous(), self.v[:, :cut].contiguous()
+
+    def seen(self, b):
+        return super().seen(b)[:, :self.cut]
+
+    def attend(self, binding):
+        tokens = self.rows if self.tree is not None else 8
+        ctx = binding.CastContext(max_batch=self.B, vocab=1000, top_k=4, max_depth=6, total_token=tokens, max_tree=tokens)
+        outs = []
+        for _ in range(2):
+            outs.append(self.run(binding, ctx, check=False))
+            status, b = ctx.cast_poll_status()
+            assert status == 7 and self.L[b] + self.n[b] > self.cut
+        assert torch.equal(outs[0].view(torch.uint8), outs[1].view(torch.uint8))
+        return outs[0]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,page,cut,L,n,window,sinks,packed", [
+    ("bf16", 32, 8, 128, 16, 192, [100, 50, 128, 10], [512, 60, 1, 100], 64, 0, False),   # the capacity in the middle of a tile
+    ("bf16", 32, 8, 128, 64, 320, [300, 0, 200, 319], [500, 320, 100, 40], 100, 0, True),
+    ("bf16", 16, 16, 64, 8, 128 * 3 + 8, [380, 100, 0, 391], [300, 290, 10, 1], 33, 4, False),
+    ("bf16", 8, 8, 128, 0, 190, [100, 0, 189, 5], [400, 189, 300, 1], 65, 130, False),
+    ("bf16", 8, 8, 64, 0, 256 + 64, [100, 0, 189, 300], [400, 300, 400, 90], 1, 3, True),
+    ("bf16", 28, 4, 128, 16, 128, [100, 127, 64], [30, 5, 600], 64, 0, False),
+    ("f32", 4, 2, 64, 16, 96, [70, 10, 95], [60, 40, 9], 20, 2, False),
+    ("f32", 4, 2, 128, 0, 100, [90, 10, 95], [130, 40, 9], 32, 0, True),
+])
+def test_chunks_past_the_capacity_under_a_window(binding, dtype, Hq, Hkv, D, page, cut, L, n, window, sinks, packed):  # noqa: F811
+    """Rows whose windows begin behind the capacity see the sinks alone, or nothing and give zeros; every other row what it should."""
+    x = Past(cut, cut, dtype, Hq, Hkv, D, page, L, n, window, sinks, packed)
+    out = x.attend(binding)
+    x.check(out)
+    for b in range(x.B):
+        blind = x.rows_of(b)[~x.seen(b).any(1)]
+        assert bool((out[blind] == 0).all())
