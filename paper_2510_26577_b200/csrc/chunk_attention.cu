@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_attn_cc_kernel(const ChunkP
       }
       // whether a position of this tile that was loaded is hidden from a row of the item (a bound on it, the same for all)
       const int tf = s.F + row0 / G, tl = s.F + (row0 + rows_here - 1) / G;
-      const bool part = kTree ? pbase + kPT > s.L || pbase < s.L + CAST_MAX_TREE + 1 - (p.window > 0 ? p.window : 0x3fffffff)
+      const bool part = kTree ? pbase + kPT > s.L || (p.window > 0 && (long long)pbase < (long long)s.L + CAST_MAX_TREE + 1 - p.window)
                               : (long long)pbase + kPT > (long long)s.L + tf || (p.window > 0 && (long long)pbase <= (long long)s.L + tl - p.window);
       auto products = [&](auto kPart) {
 #pragma unroll 4

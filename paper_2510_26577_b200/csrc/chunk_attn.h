@@ -44,7 +44,7 @@ struct ChunkParams {
 
 // A sequence's live rows and what its items walk.
 struct ChunkSeq {
-  int L, n, off;          // prefix, tokens, row of token 0
+  int L, n, off;          // prefix (up to 2^31 - 1, whatever the capacity), tokens, row of token 0
   unsigned short F, d0;   // tree: first output token, least depth of an output token
 };
 
@@ -159,10 +159,7 @@ __device__ __forceinline__ void plan_warp(const ChunkParams& p, ChunkSeq (&seq)[
     }
     if (bad && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_TREE, b);
     s.F = (unsigned short)(kTree ? min(max(F[j], 0), s.n) : 0);
-    if (s.n > s.F && (long long)s.L + s.n > p.max_pos) {
-      if (blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);
-      s.L = min(s.L, p.max_pos);
-    }
+    if (s.n > s.F && (long long)s.L + s.n > p.max_pos && blockIdx.x == 0) report(p.st, CAST_ERR_BAD_PAGE, b);  // (L stays: windows hang on it)
     if (kTree && p.first_row) {  // (a whole tree has its root, at depth 0)
       for (unsigned left = __ballot_sync(0xffffffffu, s.n > s.F); left; left &= left - 1) {
         const int l = __ffs(left) - 1;

@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_chunk_attention import Batch, binding  # noqa: F401  (the fixture)
+import chunk_oracle as co
+from test_gpu_chunk_attention import HALF, Batch, binding, dev  # noqa: F401  (the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +105,40 @@ def test_chunks_past_the_capacity_under_a_window(binding, dtype, Hq, Hkv, D, pag
     for b in range(x.B):
         blind = x.rows_of(b)[~x.seen(b).any(1)]
         assert bool((out[blind] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page,window,sinks", [(16, 60, 0), (0, 60, 5), (16, 0, 0), (0, 1000, 0)])
+def test_a_prefix_past_the_capacity_keeps_its_windows(binding, dtype, page, window, sinks):  # noqa: F811
+    """Rows at kv_len + t, wherever the cache ends: a window of 60 from position 230 on reaches back to 171 and no further."""
+    x = Past(192, 5, dtype, 8, 2, 128, page, [230, 100, 192, 700], [20, 40, 33, 3], window, sinks)
+    x.check(x.attend(binding))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tree", [False, True])
+def test_lengths_up_to_the_largest_int(binding, dtype, tree):  # noqa: F811
+    for window in (0, 50, 2 ** 31 - 1):
+        x = Batch(4, dtype, 8, 2, 128, 16, [100, 60, 9], [20, 20, 20], window, tree=tree)
+        x.table = x.paged.table  # (every entry is looked at below)
+        x.k.nan_to_num_(nan=1.0, posinf=2.0, neginf=3.0)
+        x.v.nan_to_num_(nan=1.0, posinf=2.0, neginf=3.0)
+        good = x.run(binding)
+        x.L[1] = 2 ** 31 - 1
+        ctx = binding.CastContext(max_batch=3, vocab=1000, top_k=4, max_depth=6, total_token=20, max_tree=20)
+        out = x.run(binding, ctx, check=False)
+        assert ctx.cast_poll_status() == (7, 1)
+        assert torch.equal(out[:20], good[:20]) and torch.equal(out[40:], good[40:])
+        mine = out[20:40]
+        assert bool(torch.isfinite(mine).all())
+        if window == 50:
+            assert bool((mine == 0).all())
+        if window == 0:  # every row sees the whole cache; the tolerance is Batch.check's
+            pos = np.arange(x.paged.positions)
+            pg, sl = (dev(a).long() for a in x.paged.at(1, pos))
+            for h in range(2):
+                k, v = (c[pg, sl, h].double().cpu().numpy() for c in (x.k, x.v))
+                want, spread, size = co.attend(x.q[20:40, 4 * h:4 * h + 4].double().cpu().numpy(), k, v, np.ones((20, len(pos)), bool), 128 ** -0.5)
+                e = 133 * 2.0 ** -24 * size[..., None] + 2.0 ** -21
+                tol = HALF[dtype] * np.abs(want) + ((HALF["bf16"] if dtype == "bf16" else 0) + 2 * e + len(pos) * 2.0 ** -24) * spread
+                assert (np.abs(mine[:, 4 * h:4 * h + 4].double().cpu().numpy() - want) <= tol * 1.01).all()
