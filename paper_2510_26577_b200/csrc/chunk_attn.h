@@ -347,8 +347,8 @@ __device__ __forceinline__ uint32_t tree_word(const ChunkParams& p, const ChunkS
       if (depth - dj >= p.window && (long long)s.L + dj >= p.sinks) a &= ~(1u << bit);
     }
   }
-  // bits past the tree see nothing
-  const int valid = s.n - w * 32;
+  // bits past the tree or the capacity see nothing
+  const int valid = min(s.n, max(p.max_pos - s.L, 0)) - w * 32;
   return valid >= 32 ? a : valid <= 0 ? 0u : a & ((1u << valid) - 1u);
 }
 

@@ -107,6 +107,20 @@ def test_chunks_past_the_capacity_under_a_window(binding, dtype, Hq, Hkv, D, pag
         assert bool((out[blind] == 0).all())
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,page,cut,L,n,window,sinks", [
+    ("bf16", 8, 2, 128, 16, 160, [150, 100, 160, 155], [40, 60, 12, 5], 0, 0),    # some tokens of the tree, all, one
+    ("bf16", 8, 8, 64, 0, 100, [95, 0, 100, 30], [10, 100, 7, 90], 0, 0),         # the next sequence's rows lie behind
+    ("bf16", 64, 8, 128, 24, 192, [191, 190, 10], [64, 20, 3], 7, 3),
+    ("bf16", 28, 4, 64, 8, 64, [60, 40, 3], [90, 70, 2], 2, 70),
+    ("bf16", 32, 8, 128, 16, 96, [96, 110, 200, 20], [12, 30, 9, 4], 40, 0),      # the prefix itself past the capacity
+    ("f32", 4, 2, 64, 16, 96, [90, 60, 120], [20, 40, 9], 0, 0),
+    ("f32", 4, 2, 128, 0, 100, [90, 110, 95], [20, 40, 3], 32, 5),
+])
+def test_trees_past_the_capacity(binding, dtype, Hq, Hkv, D, page, cut, L, n, window, sinks):  # noqa: F811
+    x = Past(cut, cut + window, dtype, Hq, Hkv, D, page, L, n, window, sinks, tree=True)
+    x.check(x.attend(binding))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page,window,sinks", [(16, 60, 0), (0, 60, 5), (16, 0, 0), (0, 1000, 0)])
 def test_a_prefix_past_the_capacity_keeps_its_windows(binding, dtype, page, window, sinks):  # noqa: F811
