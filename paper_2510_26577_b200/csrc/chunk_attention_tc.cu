@@ -1145,10 +1145,10 @@ bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspa
   a.q_tokens = a.tokens < most ? a.tokens : most;
   a.box = kTile;
   while (p.g.page_size % a.box != 0) a.box /= 2;
-  int lg = 0;
-  while (p.g.page_size > (1 << lg)) ++lg;
-  a.page_shift = 31 + lg;  // (exact for positions below 2^31: the multiplier is at most page_size - 1 too large in 2^shift)
-  a.page_mul = p.g.page_size ? (uint32_t)(((1ull << a.page_shift) + p.g.page_size - 1) / p.g.page_size) : 0u;
+  FastPaging fast;
+  fast_paging(p.g, p.B, p.Hkv, &fast);  // (what it says of 32-bit rows does not matter here: the copies count pages and slots)
+  a.page_shift = fast.shift;
+  a.page_mul = fast.mul;
   a.scale_log2 = p.scale * 1.4426950408889634f;
   // Pairs of row blocks share their tiles' loads. Where there are fewer of them than SMs, blocks by themselves spread over twice as many, and their lanes take half of the
   // positions each (one sequence of 8192, 60 tokens, 32/8 heads under a window of 1024: 36 -> 26 us).

@@ -24,6 +24,11 @@ static void walk(const int* a, int* out) {
   for (int i = 0; i < x.n && i < 64; ++i) out[4 + i] = x.tile(i);
   x.template unseen_halves<PT>(a[8], a[9] < 0 ? x.n : a[9], out[68], out[69], out[70]);
 }
+extern "C" CAST_API int page(int page_size, int pos) {
+  FastPaging f;
+  fast_paging({nullptr, page_size, 1, 1}, 1, 1, &f);
+  return (int)(((unsigned long long)(uint32_t)pos * f.mul) >> f.shift);
+}
 extern "C" CAST_API void span(int tile, int tree, const int* a, int* out) {
   if (tile == 64) tree ? walk<64, true>(a, out) : walk<64, false>(a, out);
   else tree ? walk<128, true>(a, out) : walk<128, false>(a, out);
@@ -108,3 +113,15 @@ def test_every_tile_has_a_half_that_some_row_sees(lib, tree, edge):
             skipped = np.array([i == no0, i in (no1a, no1b)])
             assert not skipped.all(), (max_pos, n, L, window, sinks, tf, tl)
             assert not (half & skipped).any() and half.any()
+
+
+def test_pages_of_any_size_divide_exactly(lib):
+    """The constants that stand for a division by the page size, up to pages of 2^31 - 2^16 positions."""
+    rng = np.random.default_rng(1)
+    sizes = {1, 2, 3, 2 ** 31 - 2 ** 16} | {(1 << e) + d for e in range(1, 31) for d in (-1, 0, 1, 8)} - {0}
+    for size in sorted(sizes | set(rng.integers(1, 2 ** 31 - 2 ** 16, 200).tolist())):
+        most = 2 ** 31 - 1
+        k = int(rng.integers(1, most // size + 1))
+        for pos in {0, size - 1, size, k * size - 1, k * size, most - 1, most, int(rng.integers(0, most))}:
+            if 0 <= pos <= most:
+                assert lib.page(size, pos) == pos // size, (size, pos)

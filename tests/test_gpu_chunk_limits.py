@@ -156,3 +156,15 @@ def test_lengths_up_to_the_largest_int(binding, dtype, tree):  # noqa: F811
                 e = 133 * 2.0 ** -24 * size[..., None] + 2.0 ** -21
                 tol = HALF[dtype] * np.abs(want) + ((HALF["bf16"] if dtype == "bf16" else 0) + 2 * e + len(pos) * 2.0 ** -24) * spread
                 assert (np.abs(mine[:, 4 * h:4 * h + 4].double().cpu().numpy() - want) <= tol * 1.01).all()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("page", [2 ** 30 + 8, 2 ** 30 + 128, 2 ** 31 - 2 ** 16])
+def test_pages_beyond_2_to_the_30(binding, page, tree):  # noqa: F811
+    """One page per cache, of which a part is there and a part of that is read: as the same rows without pages."""
+    x = Batch(6, "bf16", 8, 2, 64, 0, [200], [40], 60, 3, tree=tree)
+    x.k, x.v = (torch.cat([c, c.new_full((1, 512, 2, 64), float("nan"))], 1) for c in (x.k, x.v))
+    x.paged.cap = x.k.shape[1]
+    good = x.run(binding)
+    x.page, x.table, x.paged.cap, x.paged.pages = page, np.zeros((1, 1), np.int32), 1, 1
+    assert torch.equal(x.run(binding).view(torch.int16), good.view(torch.int16))
