@@ -168,3 +168,17 @@ def test_pages_beyond_2_to_the_30(binding, page, tree):  # noqa: F811
     good = x.run(binding)
     x.page, x.table, x.paged.cap, x.paged.pages = page, np.zeros((1, 1), np.int32), 1, 1
     assert torch.equal(x.run(binding).view(torch.int16), good.view(torch.int16))
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("score,size", [(37.25, 42), (37.25, -42), (-45.0, 42), (-45.0, -42)])
+def test_values_of_any_size_that_is_promised(binding, tree, score, size):  # noqa: F811
+    """Scores that keep a step's weights just within 2^60 of the reference (64 weights of 2^53.7, or of 2^-64.9, over 40 000 positions), and
+    values of 2^42 and 2^-42."""
+    x = Batch(8, "bf16", 4, 2, 64, 16, [40000, 300], [3, 40], 0, 0, tree=tree, scale=1.0)
+    x.q[~torch.isnan(x.q)] = 0.0
+    x.q[..., 0] = torch.where(torch.isnan(x.q[..., 0]), x.q[..., 0], torch.ones_like(x.q[..., 0]))
+    x.k[..., 0] = score
+    x.v *= 2.0 ** size
+    x.poison()
+    x.check(x.run(binding))
