@@ -125,3 +125,22 @@ def test_pages_of_any_size_divide_exactly(lib):
         for pos in {0, size - 1, size, k * size - 1, k * size, most - 1, most, int(rng.integers(0, most))}:
             if 0 <= pos <= most:
                 assert lib.page(size, pos) == pos // size, (size, pos)
+
+
+def test_the_kernels_wait_before_they_read_and_release_behind_their_allocation():
+    """What test_dependent_launch_host.py asks of the other kernels: a wait before anything is read, tensor memory behind it, and the
+    dependents released by the warp that has it."""
+    from test_dependent_launch_host import _body, _source
+    kernel = _body(_source("chunk_attention_tc.cu"), "chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p")
+    steps = ("griddepcontrol.wait", "if (warp == 10) {", "tcgen05.alloc", "tcgen05.relinquish_alloc_permit", "griddepcontrol.launch_dependents")
+    at = [kernel.index(x) for x in steps]
+    assert at == sorted(at) and all(kernel.count(x) == 1 for x in (steps[0], *steps[2:]))
+    assert at[-1] < at[1] + len(_body(kernel[at[1]:], "if (warp == 10)"))
+    for name, head, inputs in (("chunk_attention_tc.cu", "chunk_attn_tc_kernel(const", ("p.kv_len[", "plan_warp<", "depth_of(")),
+                               ("chunk_attention.cu", "chunk_attn_cc_kernel(const", ("make_plan<", "depth_of(")),
+                               ("append_kv.cu", "append_kernel(const", ("p.n_rows[", "p.start[", "p.inv_freq[", "p.q_weight", "p.position["))):
+        body = _body(_source(name), head)
+        wait = body.index("griddepcontrol.wait")
+        assert "return" not in body[:wait] and body.count("griddepcontrol.wait") == 1
+        assert all(x not in body[:wait] for x in inputs) and any(x in body[wait:] for x in inputs)
+        assert wait < body.index("griddepcontrol.launch_dependents")
