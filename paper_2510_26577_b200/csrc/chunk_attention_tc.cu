@@ -1,7 +1,7 @@
 // Tensor-core path of cast_chunk_attention and cast_tree_attention_window: bf16, heads of 128 or 64 dims (sm_100a: tcgen05 + TMEM + TMA).
 //
 // One CTA per SM works its stretch of the line of tiles (chunk_attn.h). A tile is 128 positions, taken in two steps of 64; a block of 128 query rows against a step is two
-// products: S = Q K^T (128 x 64 x HD) into tensor memory, then, with the weights P written over the scores as bf16, O += P V with P from tensor memory and V as
+// products: S = Q K^T (128 x 64 x HD) into tensor memory, then, with the weights P written over the scores as bf16 (64 dims: two terms), O += P V with P from tensor memory and V as
 // it lies in the cache (MN-major). Tensor memory holds two lanes of that, each with two buffers of scores and an output, so that a lane's next scores are there
 // when its softmax has done with a step. An item's rows decide how the two lanes share it:
 //   more than one block of rows (prompts, wide trees): lane 0 and lane 1 take a block each, and the K and V tiles serve both;
@@ -54,6 +54,11 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 template <int HD>
 struct Mem {
   static constexpr int kHalves = HD / 64;
+  // The weights enter P V as bf16, of 64 dims as two bf16 terms, as in the tree attention without a window. (Two terms are a product and some instructions of the softmax
+  // more. 64 dims: decoding of 64 sequences of 512-4096 111 -> 114 us per layer, two prompts of 4096, 16/16 heads, 164 -> 180. 128 dims, where they are one term: decoding 127 -> 136,
+  // one prompt of 4096 172 -> 190, 2 x 32768 + 1000 948 -> 1097, one tree under a window 26 -> 31, for an error of 0.00166 instead of 0.00235 of an output
+  // that is itself rounded to bf16.)
+  static constexpr bool kSplitP = HD == 64;
   static constexpr int kStagesK = HD == 64 ? 4 : 2, kStagesV = HD == 64 ? 5 : 3;
   static constexpr int kQ = kHalves * kRegQ, kTileBytes = kHalves * kRegKV;
   static constexpr int kAtQ = 0;                                // two slots
@@ -136,11 +141,12 @@ __device__ __forceinline__ void exp2_pair(unsigned long long x, float& p0, float
 }
 
 // 32 scores of this thread's row: P = 2^(s * scale + r) as bf16 pairs, the sum of the unrounded weights as a packed pair. Unmasked, kShare of 16 pairs go past the
-// special-function unit, which bounds the rest (16 exponentials a cycle and SM where the products of a step take 4 cycles for as many).
-constexpr int kShare = 4;
-template <bool kMasked>
+// special-function unit, which bounds the rest (16 exponentials a cycle and SM where the products of a step take 4 cycles for as many). kSplit: `lk` receives what the
+// rounding of P left over, as bf16 pairs again, and every exponential is the unit's: a weight in the product is right to 2^-17. Where `mine` is false, pk and lk keep what they have.
+template <bool kMasked, bool kSplit>
 __device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long sc2, unsigned long long ref2, uint32_t seen,
-                                      unsigned long long& sum, unsigned long long& check, uint32_t* pk) {
+                                      unsigned long long& sum, unsigned long long& check, uint32_t* pk, uint32_t* lk, bool mine = true) {
+  constexpr int kShare = kSplit ? 0 : 4;
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     const unsigned long long x = fma_f2(pack_f2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sc2, ref2);
@@ -158,7 +164,14 @@ __device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long sc2,
     }
     sum = add_f2(sum, pack_f2(p0, p1));
     const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-    pk[e] = *reinterpret_cast<const uint32_t*>(&h);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
+    if (kSplit) {
+      float r0, r1;
+      unpack_f2(add_f2(pack_f2(p0, p1), pack_f2(-__uint_as_float(w << 16), -__uint_as_float(w & 0xffff0000u))), r0, r1);
+      const __nv_bfloat162 l = __floats2bfloat162_rn(r0, r1);
+      lk[e] = mine ? *reinterpret_cast<const uint32_t*>(&l) : lk[e];
+    }
+    pk[e] = mine ? w : pk[e];
   }
 }
 
@@ -691,8 +704,8 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
       tc_fence_after();
       const uint64_t d = dv + (uint64_t)(stage * (M::kTileBytes >> 4) + ((e0 >> 4) & 1) * (kStep * 128 >> 4));
 #pragma unroll
-      for (int ks = 0; ks < kStep / 16; ++ks)
-        umma_bf16_ts(tm + kColO, tm + kColS + buf * kStep + ks * 8, d + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
+      for (int ks = 0; ks < kStep / 16 * (M::kSplitP ? 2 : 1); ++ks)  // (split: the same values again, under what was left over)
+        umma_bf16_ts(tm + kColO, tm + kColS + buf * kStep + ks * 8, d + (uint64_t)(ks % (kStep / 16) * (2048 >> 4)), idesc_pv, 1u);
       umma_commit(&ms.pv_done[h][buf]);
       if (e0 & 8) umma_commit(&ms.v_free[stage]);
       e0 = e1;
@@ -845,7 +858,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           }
           return row_ok ? v : 0u;
         };
-        uint32_t pk[32];
+        uint32_t pk[32], lk[32];  // (lk: split weights alone)
         float l0, l1;
         {
           unsigned long long sum_a = pack_f2(0.f, 0.f), sum_b = sum_a, check = sum_a;
@@ -853,11 +866,11 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           uint32_t x[64];
           tmem_get64(t_s, x);
           if (plain) {
-            weigh<false>(x, sc2, ref2, 0u, sum_a, check, pk);
-            weigh<false>(x + 32, sc2, ref2, 0u, sum_b, check, pk + 16);
+            weigh<false, M::kSplitP>(x, sc2, ref2, 0u, sum_a, check, pk, lk);
+            weigh<false, M::kSplitP>(x + 32, sc2, ref2, 0u, sum_b, check, pk + 16, lk + 16);
           } else {
-            weigh<true>(x, sc2, ref2, seen_word(0), sum_a, check, pk);
-            weigh<true>(x + 32, sc2, ref2, seen_word(1), sum_b, check, pk + 16);
+            weigh<true, M::kSplitP>(x, sc2, ref2, seen_word(0), sum_a, check, pk, lk);
+            weigh<true, M::kSplitP>(x + 32, sc2, ref2, seen_word(1), sum_b, check, pk + 16, lk + 16);
           }
           unpack_f2(add_f2(add_f2(sum_a, sum_b), check), l0, l1);
           l0 += l1;
@@ -901,12 +914,10 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           float again = 0.f;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            uint32_t x[32], q[16];
+            uint32_t x[32];
             unsigned long long sum = pack_f2(0.f, 0.f), check = sum;
             tmem_get32(t_s + j * 32, x);
-            weigh<true>(x, sc2, pack_f2(ref, ref), seen_word(j), sum, check, q);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) pk[16 * j + e] = mine ? q[e] : pk[16 * j + e];
+            weigh<true, M::kSplitP>(x, sc2, pack_f2(ref, ref), seen_word(j), sum, check, pk + 16 * j, lk + 16 * j, mine);
             float s0, s1;
             unpack_f2(sum, s0, s1);
             again += s0 + s1;
@@ -948,6 +959,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           }
         }
         tmem_st32(t_s, pk);
+        if (M::kSplitP) tmem_st32(t_s + kStep / 2, lk);
         l_run += l0;
         tmem_wait_st();
         tc_fence_before();
