@@ -325,6 +325,7 @@ cast_status launch_cc(cast_ctx* c, ChunkParams& p, cudaStream_t s) {
   p.block_rows = kRB;
   p.block_tokens = kRB % p.G == 0 ? kRB / p.G : 0;
   p.min_units = kItemCost + 1;  // (a tile is 5 us here, more than what a split costs; 3 sequences of 20-131 tokens under a window of 256, 8/8 heads of 64 dims: 38 us, from two tiles on 45)
+  p.join = 0.f;  // (tiles are long enough here that every part pays)
   const int grid = 2 * c->num_sms < kChunkGrid ? 2 * c->num_sms : kChunkGrid;
   p.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(c->chunk_ws) + kTicketBytes);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)kChunkGrid * 2 * kRB * D);

@@ -1168,8 +1168,9 @@ bool chunk_attention_tc_launch(cast_ctx* c, ChunkParams& p, int D, void* workspa
   p.block_tokens = pairs < c->num_sms ? a.tokens : 2 * a.tokens;
   p.block_rows = p.block_tokens * p.G;
   p.min_units = kItemCost + 2;
-  // Only few items can be cut into more parts than pay (131 072 positions, one kv-head: 32 tokens 175 -> 95 us, one token 122 -> 73); with more of them the rule would cost a small call 0.5 us.
-  p.join = (long long)p.B * p.Hkv <= 4 ? 2.f : 0.f;
+  // No more parts of an item than its join pays for (131 072 positions, one kv-head: 32 tokens 175 -> 95 us, one token 122 -> 73; 8192 positions, 12 tokens, 5
+  // kv-heads 38 -> 35, 8 40 -> 36). With so many items that each has few parts anyway the rule changes nothing and costs nothing that shows.
+  p.join = 2.f;
   const long long rows = p.row_start ? p.rows : (long long)p.B * p.rows;
   CUtensorMap mq, mk, mv;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)p.Hq, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)p.Hq * D * 2};
