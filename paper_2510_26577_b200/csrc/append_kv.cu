@@ -12,7 +12,8 @@
 //   registers in flight (with it: 61 us, and more registers in flight were slower, at 65 to 86, for they cost warps).
 // - A lane has two chunks of eight bytes, half a rotation apart in the halves layout, so that a dim meets its partner in the lane; cosine, sine
 //   and weight become one factor each for a dim and its partner, in registers, once per row and tensor (formed per head: 124 us; with
-//   the head and row found by division: 149). A rotation that is no whole number of chunks reads the partner from the ring.
+//   the head and row found by division: 149). A rotation that is no whole number of chunks reads the partner from the ring
+//   (36 of 128 dims, the same rows: 80 us). In fp32 the same rows take 96 us, 87 % of a copy's rate.
 // A small call is a chain of two reads of memory behind its launch: 7 us.
 // The live rows are enumerated on the device: sequences without rows cost nothing.
 #include "kv_q4.h"

@@ -6,7 +6,7 @@
 // both in fp32 in shared memory; S = Q K^T by packed multiply-adds, an online softmax, O += P V in registers. Positions that no row of the
 // item sees are neither loaded nor looked up (pages outside the window may be gone) and stand as zeros; a tile that some rows see only in
 // part takes the products with hidden positions out one by one, so that no value of a hidden row, NaN or infinity, reaches a row's output.
-// Bound by the chain of a tile: products by packed multiply-adds from shared memory, a warp's softmax, four barriers, 5 us in all, so small calls spread over all CTAs tile by tile.
+// Bound by the chain of a tile: products by packed multiply-adds from shared memory, a warp's softmax, three barriers, 5 us in all, so small calls spread over all CTAs tile by tile.
 #include <math.h>
 
 #include "chunk_attn.h"

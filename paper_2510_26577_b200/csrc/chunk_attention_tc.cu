@@ -22,11 +22,12 @@
 // positions are masked by select.
 //
 // What it measures (bf16, heads of 128) and what bounds it:
-//   two sequences of 32768 + 1000 new tokens, 28/4 heads: 0.93 ms, 1030 TFLOP/s, 63 % of a dense product's rate. A step of both lanes is worth 1020 cycles of softmax (exponentials,
+//   two sequences of 32768 + 1000 new tokens, 28/4 heads: 0.95 ms, 1005 TFLOP/s, 62 % of a dense product's rate. A step of both lanes is worth 1020 cycles of softmax (exponentials,
 //     masks, sums, rounding: 64 columns of 256 rows) behind a chain of 760 from scores to weights; softmax alone takes 0.75 ms, products and issuers alone 0.70. Issue slots 46 % busy, tensor pipe 44 %;
-//   one prompt of 4096, 32/8 heads: 167 us, 824 TFLOP/s: the same, with half of the diagonal's tiles masked, and starts and ends;
-//   64 sequences of 512-4096, one token each, 32/8 heads: 125 us, 4.8 TB/s, 74 % of a copy's rate, whatever the pages (16 scattered or in order, 128, none);
-//   one sequence of 8192, 60 tokens of a tree under a window of 1024: 24 us, a chain: launch and plan 3.8, first scores 2, two to four tiles of 1.1 to 1.5, output 2, the join of an
+//   one prompt of 4096, 32/8 heads: 172 us, 800 TFLOP/s: the same, with half of the diagonal's tiles masked, and starts and ends;
+//   64 sequences of 512-4096, one token each, 32/8 heads: 128 us, 4.7 TB/s, 72 % of a copy's rate, whatever the pages (16 scattered or in order, 128). Over uniform batches a call is 20 us of
+//     start, 2 an item of an SM and 1.47 a tile of an SM, which is memory's rate; with 64 dims 19, 4 and 1.16, where memory would take 0.74;
+//   one sequence of 8192, 60 tokens of a tree under a window of 1024: 25 us, a chain: launch and plan 3.8, first scores 2, two to four tiles of 1.1 to 1.5, output 2, the join of an
 //     item's partials 6.
 #include <math.h>
 
@@ -141,7 +142,8 @@ __device__ __forceinline__ void exp2_pair(unsigned long long x, float& p0, float
 }
 
 // 32 scores of this thread's row: P = 2^(s * scale + r) as bf16 pairs, the sum of the unrounded weights as a packed pair. Unmasked, kShare of 16 pairs go past the
-// special-function unit, which bounds the rest (16 exponentials a cycle and SM where the products of a step take 4 cycles for as many). kSplit: `lk` receives what the
+// special-function unit, which bounds the rest (16 exponentials a cycle and SM where the products of a step take 4 cycles for as many; two layers of a prompt of 4096 353 -> 344 us, calls bound by memory
+// or their start the same). kSplit: `lk` receives what the
 // rounding of P left over, as bf16 pairs again, and every exponential is the unit's: a weight in the product is right to 2^-17. Where `mine` is false, pk and lk keep what they have.
 template <bool kMasked, bool kSplit>
 __device__ __forceinline__ void weigh(const uint32_t* s, unsigned long long sc2, unsigned long long ref2, uint32_t seen,
