@@ -378,7 +378,7 @@ extern "C" cast_status cast_append_kv(cast_ctx* c, const void* q, size_t q_strid
   p.g = {page_table, page_size, seq_capacity, num_pages};
   // (the count of live rows, with a grid's step behind it, is 32-bit)
   if (B > c->cfg.max_batch || (long long)B * rows > kMaxPositions || (k && p.g.max_pos() > kMaxPositions) ||
-      (long long)Hq + 2ll * Hkv > 65536)
+      (q ? (long long)Hq : 0) + (k ? 2ll * Hkv : 0) > 65536)
     return CAST_ERR_CAPACITY;
   p.q = (const unsigned char*)q; p.k = (const unsigned char*)k; p.v = (const unsigned char*)v;
   p.q_stride = q_stride_bytes; p.k_stride = k_stride_bytes; p.v_stride = v_stride_bytes;
