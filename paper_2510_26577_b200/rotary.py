@@ -28,6 +28,8 @@ def inverse_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: str = "
     (yarn and llama3 need it)."""
     if rot_dim < 2 or rot_dim % 2 or not base > 0 or not factor > 0:
         raise ValueError(f"rot_dim {rot_dim}, base {base}, factor {factor}")
+    if scaling == "yarn" and not (base > 1 and beta_fast > 0 and beta_slow > 0):
+        raise ValueError(f"yarn: base {base}, beta_fast {beta_fast}, beta_slow {beta_slow}")
     if scaling in ("yarn", "llama3") and context < 1:
         raise ValueError(f"{scaling} needs the context that the model was trained on")
     if scaling == "ntk":
