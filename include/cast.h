@@ -563,7 +563,8 @@ CAST_API cast_status cast_reserve_chunk_attention(cast_ctx* ctx, cast_dtype dtyp
  * Sums and softmax in fp32. A weight of a bf16 call enters the product with 64 dims as two bf16 terms, right to 2^-17; with 128 it is right to 2^-13 (a quarter of the
  * exponentials are a cubic) and rounded to bf16 once on its way. (bf16: weights are kept relative to a reference that may be off by 2^60 either way, and up to 2^25 steps of
  * them are summed: values of up to 2^42 in size cannot overflow, those of 2^-42 still keep all
- * their bits, and a weight of less than 2^-66 of its row's sum may come out as anything up to that.) What a row does not see reaches no output of it, NaN
+ * their bits, and a weight of less than 2^-66 of its row's sum may come out as anything up to that;
+ * scores (q . k) * scale of up to 2^28 in size.) What a row does not see reaches no output of it, NaN
  * and infinities included; a row that sees nothing gives zeros. The same inputs give the same bits. Never reads early.
  * Other arguments and errors as for cast_tree_attention; needs cast_reserve_chunk_attention, the context's device as the current one (INVALID_ARG)
  * and q, out, caches aligned to 16 bytes. INVALID_ARG: window or sinks below 0. CAPACITY: B beyond max_batch; positions of a sequence, B * rows or rows * Hq / Hkv past

@@ -182,3 +182,34 @@ def test_values_of_any_size_that_is_promised(binding, tree, score, size):  # noq
     x.v *= 2.0 ** size
     x.poison()
     x.check(x.run(binding))
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("order", [1, -1])
+def test_scores_of_any_size_that_is_promised(binding, dtype, D, tree, order):  # noqa: F811
+    """Scores of 2^28 and -2^28, exact in 32 bits: the weights are equal among the largest that a row sees and zero elsewhere, also where
+    all that it sees stands at -2^28."""
+    x = Batch(9, dtype, 8, 2, D, 16, [500, 70, 300], [40, 30, 5], 0, 0, tree=tree, scale=1.0)
+    x.q[~torch.isnan(x.q)] = 0.0
+    x.q[..., 0] = torch.where(torch.isnan(x.q[..., 0]), x.q[..., 0], torch.full_like(x.q[..., 0], 2.0 ** 14))
+    x.k.zero_()
+    for b, (top, first, last) in enumerate(((2.0 ** 14, 100, 230), (-2.0 ** 14, 0, 100), (2.0 ** 14, 3, 4))):
+        pos = np.arange(int(x.L[b] + x.n[b]))
+        pg, sl = (dev(a).long() for a in x.paged.at(b, pos))
+        inside = dev((pos >= first) & (pos < last))
+        x.k[pg, sl, :, 0] = torch.where(inside, top, -2.0 ** 14 if order > 0 else 0.0).to(x.k.dtype)[:, None]
+        x.v[pg, sl] = torch.randn((len(pos), 2, D), device="cuda").to(x.v.dtype)
+    out = x.run(binding)
+    got = out.double().cpu().numpy()
+    for b in range(3):
+        seen = x.seen(b)
+        pos = np.arange(seen.shape[1])
+        pg, sl = (dev(a).long() for a in x.paged.at(b, pos))
+        s, v = x.k[pg, sl, 0, 0].double().cpu().numpy(), x.v[pg, sl].double().cpu().numpy()
+        for r, row in enumerate(x.rows_of(b)):
+            at = seen[r] & (s == s[seen[r]].max())
+            want, spread = v[at].mean(0), np.abs(v[at]).mean(0)  # the tolerance: half a step of the output and of a weight, sums in 32 bits
+            tol = HALF[dtype] * np.abs(want) + (HALF["bf16"] if dtype == "bf16" else 0) * spread + (len(pos) + 8) * 2.0 ** -24 * spread
+            err = np.abs(got[row].reshape(2, 4, D) - want[:, None])
+            assert (err <= tol[:, None] * 1.01).all(), (b, r, err.max())
