@@ -56,7 +56,7 @@ template <int HD>
 struct Mem {
   static constexpr int kHalves = HD / 64;
   // The weights enter P V as bf16, of 64 dims as two bf16 terms, as in the tree attention without a window. (Two terms are a product and some instructions of the softmax
-  // more. 64 dims: decoding of 64 sequences of 512-4096 111 -> 114 us per layer, two prompts of 4096, 16/16 heads, 164 -> 180. 128 dims, where they are one term: decoding 127 -> 136,
+  // more. 64 dims: decoding of 64 sequences of 512-4096 111 -> 114 us per layer, trees of 6-12 tokens under a window of 2048 114 -> 129, two prompts of 4096, 16/16 heads, 164 -> 179. 128 dims, where they are one term: decoding 127 -> 136,
   // one prompt of 4096 172 -> 190, 2 x 32768 + 1000 948 -> 1097, one tree under a window 26 -> 31, for an error of 0.00166 instead of 0.00235 of an output
   // that is itself rounded to bf16.)
   static constexpr bool kSplitP = HD == 64;
@@ -97,6 +97,7 @@ struct Misc {
   uint32_t tmem;
   int last[3];  // this CTA joins the partials: of lane 0's block, lane 1's, of a single block
   uint32_t bad[M::kStagesV][kTile / 32];  // positions of the V tile that the softmax threads take over
+  alignas(16) uint32_t anc[M::kSplitP ? 2 * kRows : 1][4];  // a tree row's mask, where two terms leave no registers for it (spilled, those trees took 139 us per layer)
   float2 row[kRows];                      // what the threads of a row tell one another at an item's end
   Item item[kItems];
 };
@@ -808,6 +809,7 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
 #pragma unroll
         for (int j = 0; j < 4; ++j) aw[j] = tree_word(p, s, tok, depth, j);
       }
+      if (kTree && M::kSplitP) *reinterpret_cast<uint4*>(ms.anc[tid]) = make_uint4(aw[0], aw[1], aw[2], aw[3]);  // (this thread's alone)
       const int hi_all = __reduce_min_sync(0xffffffffu, row_ok ? rs.hi : 0x7fffffff), lo_all = __reduce_max_sync(0xffffffffu, row_ok ? rs.lo : 0);
       float ref = row_ok ? 0.f : -INFINITY, l_run = 0.f;  // a row that is none: its P is 0 for every finite score
       if (warp_live && ok) {
@@ -855,7 +857,10 @@ chunk_attn_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constan
           uint32_t v = bits_below(rs.hi - base) & (~bits_below(rs.lo - base) | bits_below(rs.sinks - base));
           if (kTree) {
             const int st = base - it.L, wi = st >> 5, sh = st & 31;  // (arithmetic shift)
-            auto word = [&](int x) { return x == 0 ? aw[0] : x == 1 ? aw[1] : x == 2 ? aw[2] : x == 3 ? aw[3] : 0u; };
+            auto word = [&](int x) -> uint32_t {
+              if constexpr (M::kSplitP) return (unsigned)x < 4u ? ms.anc[tid][x] : 0u;
+              return x == 0 ? aw[0] : x == 1 ? aw[1] : x == 2 ? aw[2] : x == 3 ? aw[3] : 0u;
+            };
             v |= __funnelshift_r(word(wi), word(wi + 1), sh);
           }
           return row_ok ? v : 0u;
