@@ -123,7 +123,7 @@ __device__ __forceinline__ bool to_be_cleaned(const Item& it, int pos0) {
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
 
 // 2^x of a pair without the special-function unit: x = n + f with n the nearest integer (Cody and Waite's reduction; adding 1.5 2^23 rounds and leaves n in the low bits), 2^f
-// by a cubic (minimax on [-1/2, 1/2] by Remez's exchange, 7.5e-5 off at most: 2^-13.7, where P is rounded to 2^-9), n into the exponent. x below -126
+// by a cubic (minimax on [-1/2, 1/2] by Remez's exchange, 7.5e-5 off at most: 2^-13.7, where P is rounded by up to 2^-8), n into the exponent. x below -126
 // gives 2^-126. Nothing of it is right for x above 127, infinities or NaN: `check` gets x * 0, which makes the sum no number there, and the step is then done again.
 __device__ __forceinline__ void exp2_pair(unsigned long long x, float& p0, float& p1, unsigned long long& check) {
   const unsigned long long magic = pack_f2(12582912.f, 12582912.f), one = pack_f2(1.f, 1.f), minus = pack_f2(-1.f, -1.f);
